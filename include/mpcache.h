@@ -9,6 +9,12 @@
  *   - gather + softmax attention over the selected clusters (Alg. 1 steps 3-4);
  *   - decode-time growth of the kept cache (App. A.3: each decoded token's k, v are appended);
  *   - the commonality score of adjacent layers' top-k sets (Sec. 3, Observation 3).
+ * Beside them stand the operators of serving from a paged cache, for the same models:
+ *   - appending new tokens' keys and values to a paged cache, rotated by their positions, in the
+ *     element type or in 8 bits with a scale for each page and head (mpc_paged_append);
+ *   - attention of one or more new tokens over such a cache (mpc_paged_attn);
+ *   - attention of a prompt's rows over its keys (mpc_prompt_attn);
+ *   both with an optional sliding window and first tokens that stay visible.
  * mpc_prefill runs the first two steps as one call; mpc_decode_step runs selection and attention
  * as one launch (mpc_decode_step_status reads its workspace's error word).
  *
@@ -108,11 +114,61 @@ typedef struct {
   int32_t share_start;
 } mpc_evict_cfg;
 
-enum { MPC_OP_STATIC_EVICT = 0, MPC_OP_SELECT = 1, MPC_OP_DECODE_ATTN = 2, MPC_OP_DECODE_STEP = 3 };
+/* Element strides of an [L][B][H][n][d] tensor's first four axes (the last one has stride 1). Each is
+ * non-negative and a whole number of 16 bytes; that of an axis of one entry is not read. */
+typedef struct {
+  int64_t layer, batch, head, token;
+} mpc_strides;
 
-/* Workspace bytes needed by `op` (MPC_OP_*) for these dims. `T_or_Ts` is T for static eviction
- * and Ts otherwise; `cfg` points to the op's config struct (mpc_evict_cfg for static eviction,
- * mpc_select_cfg for selection and the decode step) or is NULL for MPC_OP_DECODE_ATTN. Returns 0
+/* Page formats. SAME: rows of the element type. E4M3: 8-bit floating point codes (4 exponent bits, 3
+ * mantissa bits, largest value 448, no infinities) with one fp32 scale for each (page, kv head), for K
+ * and V apart: a row's value is code * scale. */
+typedef enum { MPC_PAGE_SAME = 0, MPC_PAGE_E4M3 = 1 } mpc_page_format;
+
+/* A paged cache. Row j of sequence b lies in page table[b][j / page_size], at row j % page_size.
+ * With MPC_PAGE_E4M3 the pages hold complete pages only: the tail, a ring in the element type, has row
+ * j of sequence b in slot j % (2 * page_size), and the rows of a page that is not complete are read there. */
+typedef struct {
+  int32_t page_size;        /* rows of a page: 16, 32, 64, 128 or 256                              */
+  int32_t n_pages;          /* P: pages of a layer's pool                                          */
+  int32_t max_pages;        /* M: table entries of a sequence; M * page_size rows at most (2^30)   */
+  int32_t format;           /* mpc_page_format                                                     */
+  void *k_pages, *v_pages;  /* [L][P][Hkv][page_size][d], dtype or codes                            */
+  float *k_scale, *v_scale; /* [L][P][Hkv], MPC_PAGE_E4M3 only (else ignored, as the tails)         */
+  void *k_tail, *v_tail;    /* [L][B][Hkv][2 * page_size][d], dtype                                 */
+  const int32_t* table;     /* [B][M] page ids, the same for every layer                           */
+  const int32_t* lens;      /* [B] rows in the cache, those of the call's new tokens included      */
+} mpc_paged_kv;
+
+/* Rotary positions: table [n_pos][rot_dim / 2][2] of (cos, sin). HALF pairs channel i with channel
+ * i + rot_dim / 2, INTERLEAVED channel 2 i with 2 i + 1; channels from rot_dim on pass unchanged. */
+typedef enum { MPC_ROPE_INTERLEAVED = 0, MPC_ROPE_HALF = 1 } mpc_rope_style;
+typedef struct {
+  const float* table;
+  int32_t n_pos;
+  int32_t rot_dim; /* a multiple of 16, at most d */
+  int32_t style;   /* mpc_rope_style */
+} mpc_rope;
+
+/* Which keys a row at position p sees: j <= p and, with window > 0, (j > p - window or j < sinks). */
+typedef struct {
+  float sm_scale; /* softmax scale (1/sqrt(d)) */
+  int32_t window; /* 0: no window */
+  int32_t sinks;  /* first rows that stay visible behind the window (>= 0) */
+} mpc_attn_cfg;
+
+enum {
+  MPC_OP_STATIC_EVICT = 0,
+  MPC_OP_SELECT = 1,
+  MPC_OP_DECODE_ATTN = 2,
+  MPC_OP_DECODE_STEP = 3,
+  MPC_OP_PAGED_ATTN = 4
+};
+
+/* Workspace bytes needed by `op` (MPC_OP_*) for these dims. `T_or_Ts` is T for static eviction, n_new
+ * for the paged attention and Ts otherwise; `cfg` points to the op's config struct (mpc_evict_cfg for
+ * static eviction, mpc_select_cfg for selection and the decode step, mpc_paged_kv, of which only the
+ * sizes are read, for the paged attention) or is NULL for MPC_OP_DECODE_ATTN. Returns 0
  * when the op needs no workspace or the arguments are invalid. The size for static eviction never falls
  * with a dimension, T or the window, so one made for the longest prompt serves the shorter ones. */
 size_t mpc_workspace_bytes(int32_t op, const mpc_dims* dims, int32_t T_or_Ts, const void* cfg);
@@ -291,6 +347,57 @@ mpc_status mpc_append_kv(const mpc_dims* dims, int32_t Ts, int32_t n_tail, const
  * once. Requires 0 <= m < L, k <= 1024. No workspace. */
 mpc_status mpc_commonality(int32_t L, int32_t units, int32_t k, int32_t m, const int32_t* idx, double* out,
                            void* stream);
+
+/* Appends the new tokens of a batch to a paged cache, with the rotation of their positions applied to
+ * K (and, where given, to the queries) on the way.
+ * Sequence b has n_valid[b] new tokens (NULL: n_new each; values are brought into [0, n_new]); token t
+ * becomes row j = lens[b] - n_valid[b] + t and has position pos0[b] + t (NULL: j). Rows outside
+ * [0, M * page_size) are not written, nor are pages whose table entry lies outside [0, P).
+ *   y0 = x0 c - x1 s, y1 = x0 s + x1 c for every channel pair, each operation rounded in fp32 and the
+ *   result rounded once to the element type; a position outside the rotary table gives NaN.
+ *   k, v   [L][B][Hkv][n_new][d] (k_strides, v_strides; NULL: contiguous)
+ *   q      [L][B][Hq][n_new][d] or NULL; its rotated rows go to q_out (rows from n_valid[b] on are left
+ *          as they were), which may be q itself and may not overlap anything otherwise;
+ *   rope   NULL: no rotation (q must then be NULL too).
+ * MPC_PAGE_SAME writes the rows into their pages. MPC_PAGE_E4M3 writes a page when its last row arrives,
+ * from its rows in the element type (earlier calls' from the tail): scale = the least 2^e, e in
+ * [-126, 127], with amax <= 448 * 2^e over the finite values of the page and head (2^0 where all are
+ * zero), code = value / scale to nearest even; NaN becomes NaN and an infinity the largest code of its
+ * sign. New rows of the page of the last row and of the page before it also go to the tail, so the
+ * cache is the same however its tokens are divided over calls, and up to page_size of the newest rows can
+ * be taken back by lowering lens[b].
+ * No two table entries that a call writes to may name one page. No workspace. */
+mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                            const mpc_rope* rope, const int32_t* pos0, const void* k, const mpc_strides* k_strides,
+                            const void* v, const mpc_strides* v_strides, const void* q, const mpc_strides* q_strides,
+                            void* q_out, const mpc_strides* q_out_strides, void* stream);
+
+/* Attention of each sequence's newest n_valid[b] tokens (one, some drafted ones, a chunk of a prompt) over
+ * a paged cache that holds them already: row t stands at position p = lens[b] - n_valid[b] + t among the
+ * rows of the cache and sees the rows j that cfg names (and that the cache has: 0 <= j < lens[b],
+ * j < M * page_size, and a page whose table entry lies inside [0, P); rows read from the tail need no entry).
+ *   out = sum_j w_j v_j / sum_j w_j, w_j = exp(sm_scale q . k_j); lse = ln sum_j w_j (natural logarithm).
+ * A row without any weight (it sees nothing, or only scores of -infinity) gives out = 0, lse = -infinity; a
+ * NaN or +infinity among the scores that a row sees makes its out and lse NaN. Nothing that a row does not
+ * see reaches it, whatever it holds. Rows from n_valid[b] on are left as they were.
+ *   q, out [L][B][Hq][n_new][d] (strides; NULL: contiguous); lse [L][B][Hq][n_new] float or NULL.
+ * fp32 scores, sums and accumulation; 16-bit types multiply weights rounded to 16 bits with the values.
+ * ws: mpc_workspace_bytes(MPC_OP_PAGED_ATTN, dims, n_new, kv) bytes, zero-filled before its first use;
+ * every completed call leaves it ready for the next (calls sharing it must not overlap). */
+mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                          const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, void* out,
+                          const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* The same attention of a prompt's rows over its keys, in plain tensors: row t of sequence b stands at
+ * position k_lens[b] - q_lens[b] + t and sees keys 0 <= j < k_lens[b] as cfg names them; q_lens / k_lens
+ * [B] int32 (NULL: Tq / T each; values are brought into [0, Tq] / [0, T]). Rows from q_lens[b] on are left as
+ * they were. Weights, empty rows and NaN as in mpc_paged_attn.
+ *   q, out [L][B][Hq][Tq][d], k, v [L][B][Hkv][T][d] (strides; NULL: contiguous);
+ *   lse [L][B][Hq][Tq] float or NULL. No workspace. */
+mpc_status mpc_prompt_attn(const mpc_dims* dims, int32_t Tq, int32_t T, const int32_t* q_lens, const int32_t* k_lens,
+                           const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, const void* k,
+                           const mpc_strides* k_strides, const void* v, const mpc_strides* v_strides, void* out,
+                           const mpc_strides* out_strides, float* lse, void* stream);
 
 /* Owner layer of absolute layer `l` under the sharing rule above. */
 int32_t mpc_owner_layer(int32_t l, int32_t period, int32_t start);

@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmpcache.so")
 
 MPC_OK, MPC_EINVAL, MPC_ESHAPE, MPC_EUNSUPPORTED, MPC_EWORKSPACE, MPC_EHIP = range(6)
-MPC_OP_STATIC_EVICT, MPC_OP_SELECT, MPC_OP_DECODE_ATTN, MPC_OP_DECODE_STEP = range(4)
+MPC_OP_STATIC_EVICT, MPC_OP_SELECT, MPC_OP_DECODE_ATTN, MPC_OP_DECODE_STEP, MPC_OP_PAGED_ATTN = range(5)
 DTYPE_CODE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -36,6 +36,24 @@ class MpcEvictCfg(ctypes.Structure):
                 ("share_start", ctypes.c_int32)]
 
 
+class MpcStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("layer", "batch", "head", "token")]
+
+
+class MpcPagedKv(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("page_size", "n_pages", "max_pages", "format")] +
+                [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "k_tail", "v_tail", "table",
+                                                "lens")])
+
+
+class MpcRope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("style", ctypes.c_int32)]
+
+
+class MpcAttnCfg(ctypes.Structure):
+    _fields_ = [("sm_scale", ctypes.c_float), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
 class MpcError(RuntimeError):
     def __init__(self, fn, status, msg):
         super().__init__(f"{fn}: status {status} ({msg})")
@@ -46,7 +64,7 @@ _LIB = None
 EXPORTS = ("mpc_workspace_bytes", "mpc_static_evict", "mpc_static_evict_noalloc", "mpc_static_evict_noalloc_limit",
            "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters",
            "mpc_sparse_decode_attn", "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality",
-           "mpc_owner_layer",
+           "mpc_paged_append", "mpc_paged_attn", "mpc_prompt_attn", "mpc_owner_layer",
            "mpc_status_string", "mpc_last_error")
 
 
@@ -74,7 +92,11 @@ def lib():
         L.mpc_append_kv.argtypes = [P(MpcDims), I, I, P(MpcSelectCfg)] + [V] * 6 + [P(I), P(I), V]
         L.mpc_decode_step_status.argtypes = [V, ctypes.c_size_t, I, P(I)]
         L.mpc_commonality.argtypes = [I, I, I, I, V, V, V]
-        for fn in ("mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
+        KV, S, A = P(MpcPagedKv), P(MpcStrides), P(MpcAttnCfg)
+        L.mpc_paged_append.argtypes = [P(MpcDims), KV, I, V, P(MpcRope), V] + [V, S] * 4 + [V]
+        L.mpc_paged_attn.argtypes = [P(MpcDims), KV, I, V, A] + [V, S] * 2 + [V, V, ctypes.c_size_t, V]
+        L.mpc_prompt_attn.argtypes = [P(MpcDims), I, I, V, V, A] + [V, S] * 4 + [V, V]
+        for fn in ("mpc_paged_append", "mpc_paged_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
                    "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality"):
             getattr(L, fn).restype = ctypes.c_int
         L.mpc_owner_layer.argtypes = [I, I, I]
@@ -330,3 +352,202 @@ def mpc_decode_step_status(ws, clear=False):
     _check("mpc_decode_step_status", lib().mpc_decode_step_status(_ptr(ws), ws.numel() * ws.element_size(),
                                                                   int(bool(clear)), ctypes.byref(flags)))
     return flags.value
+
+
+ROPE_STYLE = {"interleaved": 0, "half": 1}
+PAGE_FORMAT = {"same": 0, "e4m3": 1}
+
+
+def _rows(t, what, kv_dtype, heads=None):
+    """A tensor [L][B][H][n][d] (or [L][B][H][d], n = 1): (pointer, strides or None where contiguous, n). The last axis
+    must have stride 1; the other strides are the caller's."""
+    if t.dim() == 4:
+        t = t.unsqueeze(3)
+    if t.dim() != 5 or not t.is_cuda or t.dtype != kv_dtype:
+        raise ValueError(f"{what} must be a CUDA tensor [L][B][H][n][d] of type {kv_dtype}")
+    if heads is not None and t.shape[2] != heads:
+        raise ValueError(f"{what} must have {heads} heads")
+    if t.is_contiguous():
+        return ctypes.c_void_p(t.data_ptr()), None, t.shape
+    if t.stride(4) != 1:
+        raise ValueError(f"{what}: the channels of a row must be contiguous")
+    return ctypes.c_void_p(t.data_ptr()), ctypes.byref(MpcStrides(*t.stride()[:4])), t.shape
+
+
+def _batch_ints(t, what, B, device):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous int32 tensor [{B}] on {device}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _on(device, stream, *tensors):
+    """The stream of a call on `device` (its current one by default); every tensor has to lie there."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"a tensor on {t.device} in a call on {device}")
+    if stream is None:
+        return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    if stream.device != device:
+        raise ValueError(f"a stream of {stream.device} in a call on {device}")
+    return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _call(fn, device, *args):
+    """One library call with `device` as the current one, which its launches go to."""
+    if device.index == torch.cuda.current_device():
+        _check(fn, getattr(lib(), fn)(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(fn, getattr(lib(), fn)(*args))
+
+
+class PagedKV:
+    """A paged cache over the caller's tensors, as mpc_paged_append and mpc_paged_attn take it.
+
+    k_pages, v_pages [L][P][Hkv][page][d] of the element type, or torch.float8_e4m3fn codes with k_scale, v_scale
+    [L][P][Hkv] float32 and the rings k_tail, v_tail [L][B][Hkv][2 page][d] of the element type; table [B][M] int32 page
+    ids; lens [B] int32, rows of each sequence with those of the next call's new tokens. The tables and lengths live on the
+    device: a caller writes them there, and a captured graph reads what they hold at its replay."""
+
+    def __init__(self, k_pages, v_pages, table, lens, *, k_scale=None, v_scale=None, k_tail=None, v_tail=None):
+        codes = k_pages.dtype == torch.float8_e4m3fn
+        extra = (k_scale, v_scale, k_tail, v_tail)
+        if codes != all(t is not None for t in extra) or (not codes and any(t is not None for t in extra)):
+            raise ValueError("scales and tails belong to float8_e4m3fn pages, all four of them")
+        _contig(k_pages, v_pages, table, lens, *extra)
+        if k_pages.dim() != 5 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
+            raise ValueError("k_pages and v_pages must be alike, [L][P][Hkv][page][d]")
+        self.L, P, self.Hkv, self.page, self.d = k_pages.shape
+        self.dtype = k_tail.dtype if codes else k_pages.dtype
+        if self.dtype not in DTYPE_CODE:
+            raise TypeError(f"unsupported dtype {self.dtype}")
+        if table.dtype != torch.int32 or table.dim() != 2 or lens.dtype != torch.int32 or lens.shape != table.shape[:1]:
+            raise ValueError("table must be int32 [B][M] and lens int32 [B]")
+        self.B, M = table.shape
+        if codes:
+            ring = (self.L, self.B, self.Hkv, 2 * self.page, self.d)
+            if k_tail.shape != ring or v_tail.shape != ring or v_tail.dtype != k_tail.dtype:
+                raise ValueError(f"k_tail and v_tail must be alike, {list(ring)}")
+            if any(t.shape != k_pages.shape[:3] or t.dtype != torch.float32 for t in (k_scale, v_scale)):
+                raise ValueError("k_scale and v_scale must be float32 [L][P][Hkv]")
+        self.device = k_pages.device
+        if any(t is not None and t.device != self.device for t in (v_pages, table, lens) + extra):
+            raise ValueError("the cache's tensors must lie on one device")
+        self.k_pages, self.v_pages, self.table, self.lens = k_pages, v_pages, table, lens
+        self.k_scale, self.v_scale, self.k_tail, self.v_tail = extra
+        p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.c = MpcPagedKv(self.page, P, M, PAGE_FORMAT["e4m3" if codes else "same"], p(k_pages), p(v_pages), p(k_scale),
+                            p(v_scale), p(k_tail), p(v_tail), p(table), p(lens))
+        self.ref = ctypes.byref(self.c)
+
+    def dims(self, n_q_heads):
+        return MpcDims(batch=self.B, layer0=0, n_layers=self.L, n_q_heads=n_q_heads, n_kv_heads=self.Hkv, head_dim=self.d,
+                       dtype=DTYPE_CODE[self.dtype])
+
+
+def paged_kv(*, n_layers, batch, n_kv_heads, head_dim, dtype, n_pages, max_pages, page_size=64, fp8=False, device="cuda"):
+    """An empty PagedKV: table entries -1 (no page), lengths 0."""
+    dev = torch.device(device)
+    new = lambda t, *shape: torch.zeros(shape, dtype=t, device=dev)  # noqa: E731
+    pool = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+    ring = (n_layers, batch, n_kv_heads, 2 * page_size, head_dim)
+    extra = {}
+    if fp8:
+        extra = dict(k_scale=new(torch.float32, *pool[:3]), v_scale=new(torch.float32, *pool[:3]), k_tail=new(dtype, *ring),
+                     v_tail=new(dtype, *ring))
+    t = torch.float8_e4m3fn if fp8 else dtype
+    table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=dev)
+    return PagedKV(new(t, *pool), new(t, *pool), table, new(torch.int32, batch), **extra)
+
+
+def _like(shape, kv, n, what):
+    if shape[0] != kv.L or shape[1] != kv.B or shape[3] != n or shape[4] != kv.d:
+        raise ValueError(f"{what} must be [{kv.L}][{kv.B}][H][{n}][{kv.d}]")
+
+
+def mpc_paged_append(k, v, kv, *, q=None, q_out=None, rope=None, rope_style="interleaved", pos0=None, n_valid=None,
+                     stream=None):
+    """k, v [L][B][Hkv][n][d] (or [L][B][Hkv][d]), any strides, into the cache `kv` at the rows before kv.lens. rope
+    [n_pos][rot_dim / 2][2] float32 (cos, sin) rotates K, and q [L][B][Hq][n][d] into q_out (q itself by default), by the
+    positions pos0 [B] + t (the row numbers by default). n_valid [B]: new tokens of each sequence (n by default)."""
+    kp, ks, shape = _rows(k, "k", kv.dtype, kv.Hkv)
+    n = shape[3]
+    _like(shape, kv, n, "k")
+    vp, vs, shape = _rows(v, "v", kv.dtype, kv.Hkv)
+    _like(shape, kv, n, "v")
+    Hq, qp, qs, op, os_, r = kv.Hkv, None, None, None, None, None
+    if rope is not None:
+        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous():
+            raise ValueError("rope must be contiguous float32 [n_pos][rot_dim / 2][2]")
+        r = ctypes.byref(MpcRope(rope.data_ptr(), rope.shape[0], 2 * rope.shape[1], ROPE_STYLE[rope_style]))
+    if q is not None:
+        q_out = q if q_out is None else q_out
+        qp, qs, shape = _rows(q, "q", kv.dtype)
+        Hq = shape[2]
+        _like(shape, kv, n, "q")
+        op, os_, shape = _rows(q_out, "q_out", kv.dtype, Hq)
+        _like(shape, kv, n, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out is given without q")
+    st = _on(kv.device, stream, k, v, q, q_out, rope)
+    _call("mpc_paged_append", kv.device, ctypes.byref(kv.dims(Hq)), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
+          r, _batch_ints(pos0, "pos0", kv.B, kv.device), kp, ks, vp, vs, qp, qs, op, os_, st)
+
+
+def paged_attn_workspace_bytes(q, kv):
+    """Workspace bytes of mpc_paged_attn for queries shaped like q [L][B][Hq][n][d] (or [L][B][Hq][d])."""
+    return lib().mpc_workspace_bytes(MPC_OP_PAGED_ATTN, ctypes.byref(kv.dims(q.shape[2])), q.shape[3] if q.dim() == 5 else 1,
+                                     kv.ref)
+
+
+def _lse_of(lse, shape):
+    if lse is None:
+        return None
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != shape[0] * shape[1] * shape[2] * shape[3]:
+        raise ValueError("lse must be contiguous float32 [L][B][Hq][n]")
+    return ctypes.c_void_p(lse.data_ptr())
+
+
+def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse=None, ws=None, stream=None):
+    """Attention of the newest tokens' queries q [L][B][Hq][n][d] (or [L][B][Hq][d]) over the cache `kv`, which holds their
+    keys and values already -> out (shaped like q), lse [L][B][Hq][n] float32. window, sinks: a row at position p sees
+    the rows j <= p with j > p - window (0: all) or j < sinks. ws: from workspace(paged_attn_workspace_bytes(q, kv)),
+    reused by later calls of the same shape (made for the call by default)."""
+    qp, qs, shape = _rows(q, "q", kv.dtype)
+    n = shape[3]
+    _like(shape, kv, n, "q")
+    op, os_, oshape = _rows(out, "out", kv.dtype, shape[2])
+    _like(oshape, kv, n, "out")
+    if ws is None:
+        ws = workspace(paged_attn_workspace_bytes(q, kv), kv.device)
+    _contig(ws)
+    st = _on(kv.device, stream, q, out, lse, ws)
+    cfg = MpcAttnCfg(sm_scale, window, sinks)
+    _call("mpc_paged_attn", kv.device, ctypes.byref(kv.dims(shape[2])), kv.ref, n,
+          _batch_ints(n_valid, "n_valid", kv.B, kv.device), ctypes.byref(cfg), qp, qs, op, os_, _lse_of(lse, shape),
+          ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), st)
+
+
+def mpc_prompt_attn(q, k, v, out, *, sm_scale, window=0, sinks=0, q_lens=None, k_lens=None, lse=None, stream=None):
+    """Attention of a prompt's rows q [L][B][Hq][Tq][d] over its keys k, v [L][B][Hkv][T][d] (any strides) -> out (shaped like
+    q), lse [L][B][Hq][Tq] float32: row t of sequence b stands at position k_lens[b] - q_lens[b] + t (T, Tq by default);
+    window, sinks as in mpc_paged_attn."""
+    if q.dtype not in DTYPE_CODE:
+        raise TypeError(f"unsupported dtype {q.dtype}")
+    if q.dim() != 5 or k.dim() != 5:
+        raise ValueError("q, k, v and out must be [L][B][H][n][d]")
+    qp, qs, shape = _rows(q, "q", q.dtype)
+    op, os_, oshape = _rows(out, "out", q.dtype)
+    kp, ks, kshape = _rows(k, "k", q.dtype)
+    vp, vs, vshape = _rows(v, "v", q.dtype)
+    if oshape != shape or vshape != kshape or kshape[:2] != shape[:2] or kshape[4] != shape[4]:
+        raise ValueError("out must be shaped like q, and k and v like q but for their heads and rows")
+    L, B, Hq, Tq, d = shape
+    dev = q.device
+    st = _on(dev, stream, k, v, out, lse)
+    dims = MpcDims(batch=B, layer0=0, n_layers=L, n_q_heads=Hq, n_kv_heads=kshape[2], head_dim=d, dtype=DTYPE_CODE[q.dtype])
+    cfg = MpcAttnCfg(sm_scale, window, sinks)
+    _call("mpc_prompt_attn", dev, ctypes.byref(dims), Tq, kshape[3], _batch_ints(q_lens, "q_lens", B, dev),
+          _batch_ints(k_lens, "k_lens", B, dev), ctypes.byref(cfg), qp, qs, kp, ks, vp, vs, op, os_, _lse_of(lse, shape), st)

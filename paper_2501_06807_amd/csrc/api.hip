@@ -12,6 +12,7 @@
 #include "decode_attn.h"
 #include "evict.h"
 #include "fused.h"
+#include "paged.h"
 #include "select.h"
 
 namespace {
@@ -133,6 +134,110 @@ DecodeWs decode_ws(const mpc_dims* d, bool per_q_head) {
 // enough for either layout, so that one size serves every selection rule
 size_t decode_ws_bytes(const mpc_dims* d) { return std::max(decode_ws(d, false).total, decode_ws(d, true).total); }
 
+// A tensor [L][B][heads][n][d]: its byte strides. One that is written may not lie on itself.
+mpc_status rows_of(const mpc_dims* d, const char* what, const void* p, const mpc_strides* s, int heads, int n, bool written,
+                   mpc::Rows* r) {
+  const int64_t e = elt_size(d->dtype), D = d->head_dim;
+  if (!p) return fail(MPC_EINVAL, "%s is NULL", what);
+  if (!aligned16(p)) return fail(MPC_EINVAL, "%s must be 16-byte aligned", what);
+  r->p = (char*)p;
+  if (!s) {
+    r->token = D * e;
+    r->head = n * r->token;
+    r->batch = heads * r->head;
+    r->layer = d->batch * r->batch;
+    return MPC_OK;
+  }
+  struct Axis {
+    int64_t stride, size;
+  } ax[4] = {{s->layer, d->n_layers}, {s->batch, d->batch}, {s->head, heads}, {s->token, n}};
+  for (Axis& a : ax) {
+    if (a.size == 1) a.stride = 0;
+    // below 2^46 bytes for a whole axis: no tensor is larger, and no sum of offsets wraps
+    if (a.stride < 0 || a.stride * e % 16 || a.stride > ((int64_t)1 << 46) / (e * a.size))
+      return fail(MPC_EINVAL, "%s: strides must be non-negative whole numbers of 16 bytes", what);
+  }
+  r->layer = ax[0].stride * e;
+  r->batch = ax[1].stride * e;
+  r->head = ax[2].stride * e;
+  r->token = ax[3].stride * e;
+  if (written) {
+    std::sort(ax, ax + 4, [](const Axis& x, const Axis& y) { return x.stride < y.stride; });
+    int64_t span = D;  // elements from the first to behind the last of the axes so far
+    for (const Axis& a : ax) {
+      if (a.size == 1) continue;
+      if (a.stride < span) return fail(MPC_ESHAPE, "%s: rows that are written overlap", what);
+      span += (a.size - 1) * a.stride;
+    }
+  }
+  return MPC_OK;
+}
+
+// Sizes of a paged cache.
+mpc_status check_pages(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new) {
+  if (!kv) return fail(MPC_EINVAL, "kv is NULL");
+  const int G = d->n_q_heads / d->n_kv_heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return fail(MPC_EUNSUPPORTED, "group size %d not in {1, 2, 4, 8}", G);
+  if (n_new <= 0 || n_new > mpc::kMaxRows) return fail(MPC_EINVAL, "n_new %d not in [1, 2^30]", n_new);
+  if (kv->n_pages <= 0 || kv->max_pages <= 0) return fail(MPC_EINVAL, "n_pages and max_pages must be positive");
+  if (kv->format != MPC_PAGE_SAME && kv->format != MPC_PAGE_E4M3) return fail(MPC_EINVAL, "unknown page format %d", kv->format);
+  const int p = kv->page_size;
+  if (p != 16 && p != 32 && p != 64 && p != 128 && p != 256)
+    return fail(MPC_EUNSUPPORTED, "page_size %d not in {16, 32, 64, 128, 256}", p);
+  if ((int64_t)kv->max_pages * p > mpc::kMaxRows) return fail(MPC_EUNSUPPORTED, "more than 2^30 rows to a sequence");
+  return MPC_OK;
+}
+
+mpc_status paged_cache(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid, mpc::PagedCache* c) {
+  mpc_status s = check_pages(d, kv, n_new);
+  if (s != MPC_OK) return s;
+  const bool codes = kv->format == MPC_PAGE_E4M3;
+  if (!kv->k_pages || !kv->v_pages || !kv->table || !kv->lens)
+    return fail(MPC_EINVAL, "a required pointer of the paged cache is NULL");
+  if (codes && (!kv->k_scale || !kv->v_scale || !kv->k_tail || !kv->v_tail))
+    return fail(MPC_EINVAL, "8-bit pages need scales and tails");
+  if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages) || (codes && (!aligned16(kv->k_tail) || !aligned16(kv->v_tail))))
+    return fail(MPC_EINVAL, "the paged cache's pages and tails must be 16-byte aligned");
+  c->k = (char*)kv->k_pages;
+  c->v = (char*)kv->v_pages;
+  c->ks = codes ? kv->k_scale : nullptr;
+  c->vs = codes ? kv->v_scale : nullptr;
+  c->k_tail = codes ? (char*)kv->k_tail : nullptr;
+  c->v_tail = codes ? (char*)kv->v_tail : nullptr;
+  c->table = kv->table;
+  c->lens = kv->lens;
+  c->n_valid = n_valid;
+  c->page = kv->page_size;
+  c->log_page = __builtin_ctz((unsigned)kv->page_size);
+  c->n_pages = kv->n_pages;
+  c->max_pages = kv->max_pages;
+  c->L = d->n_layers;
+  c->B = d->batch;
+  c->Hkv = d->n_kv_heads;
+  c->n_new = n_new;
+  return MPC_OK;
+}
+
+// What both attentions take apart from their keys.
+mpc_status attn_args(const mpc_dims* d, const mpc_attn_cfg* cfg, int n, const void* q, const mpc_strides* qs, const void* out,
+                     const mpc_strides* os, float* lse, mpc::AttnArgs* a) {
+  if (!cfg) return fail(MPC_EINVAL, "cfg is NULL");
+  if (!std::isfinite(cfg->sm_scale)) return fail(MPC_EINVAL, "bad sm_scale");
+  if (cfg->window < 0 || cfg->sinks < 0) return fail(MPC_EINVAL, "window and sinks must be >= 0");
+  mpc_status s = rows_of(d, "q", q, qs, d->n_q_heads, n, false, &a->q);
+  if (s == MPC_OK) s = rows_of(d, "out", out, os, d->n_q_heads, n, true, &a->out);
+  a->lse = lse;
+  a->L = d->n_layers;
+  a->B = d->batch;
+  a->Hq = d->n_q_heads;
+  a->Hkv = d->n_kv_heads;
+  a->n = n;
+  a->window = std::min(cfg->window, mpc::kMaxRows);
+  a->sinks = std::min(cfg->sinks, mpc::kMaxRows);
+  a->qscale = cfg->sm_scale * 1.44269504088896340736f;
+  return s;
+}
+
 // Fused decode-step workspace: the error word, per-owner-head state and consumer counts, then the
 // split-K partials.
 struct StepWs {
@@ -182,6 +287,11 @@ size_t mpc_workspace_bytes(int32_t op, const mpc_dims* dims, int32_t T_or_Ts, co
   if (op == MPC_OP_DECODE_STEP) {
     if (!cfg) return 0;
     return step_ws(dims, (const mpc_select_cfg*)cfg).total;
+  }
+  if (op == MPC_OP_PAGED_ATTN) {
+    const mpc_paged_kv* kv = (const mpc_paged_kv*)cfg;
+    if (!kv || check_pages(dims, kv, T_or_Ts) != MPC_OK) return 0;
+    return 0;
   }
   return 0;
 }
@@ -723,6 +833,80 @@ mpc_status mpc_append_kv(const mpc_dims* dims, int32_t Ts, int32_t n_tail, const
   if ((s = launched(mpc::launch_append_rows(ap, st), "append")) != MPC_OK) return s;
   if (Ts_out) *Ts_out = Ts_new;
   if (n_tail_out) *n_tail_out = seal ? 1 : n_tail + 1;
+  return ok();
+}
+
+mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                            const mpc_rope* rope, const int32_t* pos0, const void* k, const mpc_strides* k_strides,
+                            const void* v, const mpc_strides* v_strides, const void* q, const mpc_strides* q_strides,
+                            void* q_out, const mpc_strides* q_out_strides, void* stream) {
+  mpc_status s = check_dims(dims);
+  if (s != MPC_OK) return s;
+  mpc::PagedAppendArgs a{};
+  if ((s = paged_cache(dims, kv, n_new, n_valid, &a.c)) != MPC_OK) return s;
+  if (rope) {
+    if (!rope->table || rope->n_pos <= 0) return fail(MPC_EINVAL, "the rotary table is NULL or empty");
+    if (!aligned16(rope->table)) return fail(MPC_EINVAL, "the rotary table must be 16-byte aligned");
+    if (rope->style != MPC_ROPE_INTERLEAVED && rope->style != MPC_ROPE_HALF)
+      return fail(MPC_EINVAL, "unknown rotary style %d", rope->style);
+    if (rope->rot_dim <= 0 || rope->rot_dim % 16 || rope->rot_dim > dims->head_dim)
+      return fail(MPC_ESHAPE, "rot_dim %d not a multiple of 16 in [16, head_dim]", rope->rot_dim);
+    a.rope = {(const float2*)rope->table, rope->n_pos, rope->rot_dim, rope->style == MPC_ROPE_HALF};
+  }
+  if ((s = rows_of(dims, "k", k, k_strides, dims->n_kv_heads, n_new, false, &a.k)) != MPC_OK) return s;
+  if ((s = rows_of(dims, "v", v, v_strides, dims->n_kv_heads, n_new, false, &a.v)) != MPC_OK) return s;
+  if (q) {
+    if (!rope) return fail(MPC_EINVAL, "q is given without a rotation");
+    if ((s = rows_of(dims, "q", q, q_strides, dims->n_q_heads, n_new, false, &a.q)) != MPC_OK) return s;
+    if ((s = rows_of(dims, "q_out", q_out, q_out_strides, dims->n_q_heads, n_new, true, &a.q_out)) != MPC_OK) return s;
+    a.Hq = dims->n_q_heads;
+  } else if (q_out) {
+    return fail(MPC_EINVAL, "q_out is given without q");
+  }
+  a.pos0 = pos0;
+  a.np = (n_new + kv->page_size - 2) / kv->page_size + 1;
+  clear_stale_error();
+  if ((s = launched(mpc::launch_paged_append(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged append")) != MPC_OK)
+    return s;
+  return ok();
+}
+
+mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                          const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, void* out,
+                          const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  mpc_status s = check_dims(dims);
+  if (s != MPC_OK) return s;
+  mpc::PagedAttnArgs a{};
+  if ((s = paged_cache(dims, kv, n_new, n_valid, &a.c)) != MPC_OK) return s;
+  if ((s = attn_args(dims, cfg, n_new, q, q_strides, out, out_strides, lse, &a)) != MPC_OK) return s;
+  (void)ws;
+  (void)ws_bytes;
+  clear_stale_error();
+  if ((s = launched(mpc::launch_paged_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged attention")) != MPC_OK)
+    return s;
+  return ok();
+}
+
+mpc_status mpc_prompt_attn(const mpc_dims* dims, int32_t Tq, int32_t T, const int32_t* q_lens, const int32_t* k_lens,
+                           const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, const void* k,
+                           const mpc_strides* k_strides, const void* v, const mpc_strides* v_strides, void* out,
+                           const mpc_strides* out_strides, float* lse, void* stream) {
+  mpc_status s = check_dims(dims);
+  if (s != MPC_OK) return s;
+  const int G = dims->n_q_heads / dims->n_kv_heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return fail(MPC_EUNSUPPORTED, "group size %d not in {1, 2, 4, 8}", G);
+  if (Tq <= 0 || T <= 0) return fail(MPC_EINVAL, "Tq and T must be positive");
+  if (Tq > mpc::kMaxRows || T > mpc::kMaxRows) return fail(MPC_EUNSUPPORTED, "more than 2^30 rows");
+  mpc::PromptAttnArgs a{};
+  if ((s = attn_args(dims, cfg, Tq, q, q_strides, out, out_strides, lse, &a)) != MPC_OK) return s;
+  if ((s = rows_of(dims, "k", k, k_strides, dims->n_kv_heads, T, false, &a.k)) != MPC_OK) return s;
+  if ((s = rows_of(dims, "v", v, v_strides, dims->n_kv_heads, T, false, &a.v)) != MPC_OK) return s;
+  a.q_lens = q_lens;
+  a.k_lens = k_lens;
+  a.T = T;
+  clear_stale_error();
+  if ((s = launched(mpc::launch_prompt_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "prompt attention")) != MPC_OK)
+    return s;
   return ok();
 }
 

@@ -1,0 +1,60 @@
+// Device helpers of the paged cache: 8-bit codes, page scales, row addresses.
+#pragma once
+#include "paged.h"
+
+namespace mpc {
+namespace dev {
+
+// Pairs of e4m3 codes and fp32 values (v_cvt_pk_*_fp8: to nearest even, subnormals kept).
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+__device__ __forceinline__ void decode4(uint32_t w, float* out) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  out[0] = lo[0];
+  out[1] = lo[1];
+  out[2] = hi[0];
+  out[3] = hi[1];
+}
+
+// Exponent s of a page's scale 2^s: the least with amax <= 448 * 2^s = 1.75 * 2^(s + 8), read off the bits of amax.
+__device__ __forceinline__ int scale_exponent(uint32_t amax_bits) {
+  if (amax_bits == 0) return 0;
+  const int s = (int)(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return max(s, -126);
+}
+__device__ __forceinline__ float pow2(int s) { return __uint_as_float((uint32_t)(s + 127) << 23); }
+
+// Magnitude bits of a finite value, 0 for the others: page maxima are taken over the finite values.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  return u < 0x7F800000u ? u : 0u;
+}
+// A value in units of its page's scale, as the code conversion takes it: infinities to the largest code.
+__device__ __forceinline__ float to_code_range(float x, float inv) {
+  const float y = x * inv;
+  return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+}
+
+// Eight consecutive channels as floats.
+template <class DT>
+__device__ __forceinline__ void load8(const char* p, float* out) {
+  unpack<DT>(ldg16(p), out);
+  if constexpr (DT::kVec == 4) unpack<DT>(ldg16(p + 16), out + 4);
+}
+
+// Page id of logical page pg of sequence b, or -1 where the table or the pool has none.
+__device__ __forceinline__ int page_id(const PagedCache& c, int b, int pg) {
+  if (pg < 0 || pg >= c.max_pages) return -1;
+  const int id = c.table[(size_t)b * c.max_pages + pg];
+  return (unsigned)id < (unsigned)c.n_pages ? id : -1;
+}
+// Index of (layer, page, head) in the pool.
+__device__ __forceinline__ size_t page_unit(const PagedCache& c, int l, int id, int h) {
+  return ((size_t)l * c.n_pages + id) * c.Hkv + h;
+}
+
+}  // namespace dev
+}  // namespace mpc
