@@ -188,6 +188,11 @@ mpc_status check_pages(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new)
   return MPC_OK;
 }
 
+mpc::PagedPlan plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n) {
+  return mpc::paged_plan(d->dtype, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
+                         kv->max_pages * kv->page_size);
+}
+
 mpc_status paged_cache(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid, mpc::PagedCache* c) {
   mpc_status s = check_pages(d, kv, n_new);
   if (s != MPC_OK) return s;
@@ -291,7 +296,8 @@ size_t mpc_workspace_bytes(int32_t op, const mpc_dims* dims, int32_t T_or_Ts, co
   if (op == MPC_OP_PAGED_ATTN) {
     const mpc_paged_kv* kv = (const mpc_paged_kv*)cfg;
     if (!kv || check_pages(dims, kv, T_or_Ts) != MPC_OK) return 0;
-    return 0;
+    const mpc::PagedPlan p = plan_of(dims, kv, T_or_Ts);
+    return p.blocks < ((long long)1 << 31) ? p.ws_bytes : 0;
   }
   return 0;
 }
@@ -879,8 +885,17 @@ mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
   mpc::PagedAttnArgs a{};
   if ((s = paged_cache(dims, kv, n_new, n_valid, &a.c)) != MPC_OK) return s;
   if ((s = attn_args(dims, cfg, n_new, q, q_strides, out, out_strides, lse, &a)) != MPC_OK) return s;
-  (void)ws;
-  (void)ws_bytes;
+  const mpc::PagedPlan p = plan_of(dims, kv, n_new);
+  if (p.blocks >= ((long long)1 << 31)) return fail(MPC_EUNSUPPORTED, "more than 2^31 key blocks in a call");
+  if (!ws || ws_bytes < p.ws_bytes)
+    return fail(MPC_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, p.ws_bytes);
+  if (!aligned16(ws)) return fail(MPC_EINVAL, "ws must be 16-byte aligned");
+  a.cnt = (int*)ws;
+  a.part = (float*)((char*)ws + p.cnt_bytes);
+  a.row_tiles = p.row_tiles;
+  a.groups = p.groups;
+  a.part_rows = p.part_rows;
+  a.grid = p.grid;
   clear_stale_error();
   if ((s = launched(mpc::launch_paged_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged attention")) != MPC_OK)
     return s;

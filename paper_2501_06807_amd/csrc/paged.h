@@ -55,7 +55,21 @@ struct AttnArgs {
 
 struct PagedAttnArgs : AttnArgs {
   PagedCache c;
+  int* cnt;       // arrivals of each unit, zero between launches
+  float* part;    // [grid][2][part_rows][D + 2]: accumulator, maximum and sum of a unit's part
+  int row_tiles;  // 16-row tiles of a unit
+  int groups;     // units of a kv head: its query rows over those of a unit
+  int part_rows, grid;
 };
+struct PagedPlan {
+  int row_tiles, groups, part_rows, grid;
+  long long blocks;  // at most, for sequences as long as the table
+  size_t cnt_bytes, ws_bytes;
+};
+PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap);
+hipError_t launch_paged_attn_fp32(const PagedAttnArgs& a, int D, hipStream_t st);
+hipError_t launch_paged_attn_fp16(const PagedAttnArgs& a, int D, hipStream_t st);
+hipError_t launch_paged_attn_bf16(const PagedAttnArgs& a, int D, hipStream_t st);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 
 struct PromptAttnArgs : AttnArgs {
