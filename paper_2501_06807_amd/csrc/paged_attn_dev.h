@@ -346,10 +346,10 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
   struct Seq {
     int valid, len, rows, start, groups, full, tiles, skip, at, nb;  // tiles of pages: [0, skip) and [at, at + tiles - skip)
   };
-  auto seq = [&](int b) {
+  auto seq_of = [&](int len, int valid) {
     Seq s;
-    s.valid = c.valid(b);
-    s.len = c.len(b);
+    s.valid = min(max(valid, 0), c.n_new);
+    s.len = min(max(len, 0), kMaxRows);
     s.rows = min(s.len, c.cap());
     s.start = s.len - s.valid;
     s.groups = (G * s.valid + RW - 1) / RW;
@@ -366,13 +366,16 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     s.nb = max(1, (s.tiles + tail + kPagedWaves - 1) / kPagedWaves);
     return s;
   };
+  auto seq_lane = [&](int b) { return seq_of(c.lens[b], c.n_valid ? c.n_valid[b] : c.n_new); };  // a sequence to a lane
+  auto seq = [&](int b) { return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new); };
   const int per_group = a.L * a.Hkv;
   auto blocks_of = [&](const Seq& s) { return (unsigned)(s.groups * per_group) * (unsigned)s.nb; };
   unsigned total = 0;  // below 2^31, as the host has checked for the longest sequences
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const int b = b0 + lane;
-    total += wave_sum(b < a.B ? blocks_of(seq(b)) : 0u);
+    total += wave_sum(b < a.B ? blocks_of(seq_lane(b)) : 0u);
   }
+  total = __builtin_amdgcn_readfirstlane(total);
   if (total == 0) return;
   const unsigned per = (total + gridDim.x - 1) / gridDim.x;
   if ((unsigned long long)blockIdx.x * per >= total) return;
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
   unsigned base = 0;  // blocks of the sequences before b
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const int i = b0 + lane;
-    const unsigned mine = i < a.B ? blocks_of(seq(i)) : 0u;
+    const unsigned mine = i < a.B ? blocks_of(seq_lane(i)) : 0u;
     unsigned sum = mine;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -399,6 +402,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     base += __shfl(sum, kWave - 1);
   }
   b = __builtin_amdgcn_readfirstlane(b);
+  base = __builtin_amdgcn_readfirstlane(base);
 
   PagedWave<DT, D, CODES, RT> w;
   Seq s = seq(b);
@@ -445,16 +449,19 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
 
     // this wave's tiles of the run, a tile of every block; those of pages first
     auto page_tile = [&](int i) { return i < s.skip ? i : i - s.skip + s.at; };
-    // page ids of a tile's halves, -1 where there is none
-    auto ids_of = [&](int i, int* id) {
-      const int k0 = page_tile(i) * TL::TK;
+    auto page_at = [&](int i, int hf) { return (page_tile(i) * TL::TK + 16 * hf) >> c.log_page; };
+    // table entries of a tile's halves, and the page ids that they give (-1 where there is none)
+    auto entries_of = [&](int i, int* e) {
 #pragma unroll
-      for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = page_id(c, b, (k0 + 16 * hf) >> c.log_page);
+      for (int hf = 0; hf < TL::HALVES; ++hf) e[hf] = page_entry(c, b, page_at(i, hf));
+    };
+    auto ids_of = [&](int i, const int* e, int* id) {
+#pragma unroll
+      for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = page_of_entry(c, e[hf], page_at(i, hf));
     };
     // row 0 of a tile's half in the pool (page 0 where it has no page: its rows are not used)
     auto place = [&](int i, int hf, int id) {
-      const int use = __builtin_amdgcn_readfirstlane(max(id, 0));
-      return page_unit(c, l, use, h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
+      return page_unit(c, l, max(id, 0), h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
     };
     auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks) {
 #pragma unroll
@@ -463,7 +470,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
         const char* p = c.k + row * TL::RB + col * TL::RB + g * 16;
 #pragma unroll
         for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
-        if constexpr (CODES) ks[hf] = c.ks[row >> c.log_page];
+        if constexpr (CODES) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
       }
     };
     auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs) {
@@ -473,7 +480,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
         const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::VW * 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
-        if constexpr (CODES) vs[hf] = c.vs[row >> c.log_page];
+        if constexpr (CODES) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
       }
     };
     using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
@@ -485,19 +492,22 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       uint4 k[TL::HALVES][TL::KL];
       uint32_t v[TL::VK][TL::VW];
       float ks[TL::HALVES], vs[TL::HALVES];
-      int id[TL::HALVES], next[TL::HALVES];
-      ids_of(i, id);
+      int id[TL::HALVES], next[TL::HALVES], entry[TL::HALVES];
+      entries_of(i, entry);
+      ids_of(i, entry, id);
       load_k(i, id, k, ks);
       load_v(i, id, v, vs);
-      ids_of(min(i + kPagedWaves, i_end - 1), next);
+      auto after = [&](int n) { return n + kPagedWaves < i_end ? n + kPagedWaves : n; };
+      entries_of(after(i), entry);
       for (;;) {
-        const int i1 = i + kPagedWaves;
+        // the last tile asks for itself again, so that every pass has the same loads in flight and waits for its own only
+        const int i1 = after(i);
         const int k0 = page_tile(i) * TL::TK, k1 = k0 + TL::TK - 1;
         bool have[TL::HALVES], all = true;
         float sc[TL::HALVES], vf[TL::HALVES];
 #pragma unroll
         for (int hf = 0; hf < TL::HALVES; ++hf) {
-          have[hf] = __builtin_amdgcn_readfirstlane(id[hf]) >= 0 && k0 + 16 * hf < s.full;
+          have[hf] = id[hf] >= 0 && k0 + 16 * hf < s.full;
           all = all && have[hf];
         }
         const bool edge = !(all && k1 < s.full && k1 <= lo && (!a.window || k0 > hi - a.window || k1 < a.sinks));
@@ -508,22 +518,21 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
           sc[hf] = CODES ? (have[hf] ? a.qscale * ks[hf] : 0.f) : a.qscale;
           vf[hf] = CODES ? (have[hf] ? vs[hf] : 0.f) : 1.f;
         }
-        if (i1 < i_end) load_k(i1, next, k, ks);
+        ids_of(i1, entry, next);
+        load_k(i1, next, k, ks);
+        entries_of(after(i1), entry);
         float p[RT][TL::VK];
         w.weights(sr, sc, CODES ? vf : nullptr, a, edge, k0, s.full, have, p);
         Operand x;
         w.template operands<false>(v, x);
-        if (i1 < i_end) {
-          load_v(i1, next, v, vs);
+        load_v(i1, next, v, vs);
 #pragma unroll
-          for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
-          ids_of(min(i1 + kPagedWaves, i_end - 1), next);
-        }
+        for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
         if constexpr (TL::F)
           w.add_values(x, p, a, edge, k0, s.full, have, lo, hi);
         else
           w.template add_values<typename TL::PV>(x, p, a, edge, k0, s.full, have, lo, hi);
-        if (i1 >= i_end) break;
+        if (i1 == i) break;
         i = i1;
       }
     }

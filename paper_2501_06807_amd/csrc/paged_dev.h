@@ -45,11 +45,26 @@ __device__ __forceinline__ void load8(const char* p, float* out) {
   if constexpr (DT::kVec == 4) unpack<DT>(ldg16(p + 16), out + 4);
 }
 
+// A value that the launch does not write, at an address that is the same over the wave: through the scalar cache, so that
+// it has a counter of its own and waiting for it does not wait for the rows in flight.
+template <class T>
+__device__ __forceinline__ T load_uniform(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
 // Page id of logical page pg of sequence b, or -1 where the table or the pool has none.
 __device__ __forceinline__ int page_id(const PagedCache& c, int b, int pg) {
   if (pg < 0 || pg >= c.max_pages) return -1;
   const int id = c.table[(size_t)b * c.max_pages + pg];
   return (unsigned)id < (unsigned)c.n_pages ? id : -1;
+}
+// The same in two steps for b and pg (not negative) that are the same over the wave: the table's entry, asked for early, and
+// what it says.
+__device__ __forceinline__ int page_entry(const PagedCache& c, int b, int pg) {
+  return load_uniform(c.table + (size_t)b * c.max_pages + min(pg, c.max_pages - 1));
+}
+__device__ __forceinline__ int page_of_entry(const PagedCache& c, int entry, int pg) {
+  return pg < c.max_pages && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
 }
 // Index of (layer, page, head) in the pool.
 __device__ __forceinline__ size_t page_unit(const PagedCache& c, int l, int id, int h) {
