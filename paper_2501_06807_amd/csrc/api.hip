@@ -893,6 +893,7 @@ mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
   a.cnt = (int*)ws;
   a.part = (float*)((char*)ws + p.cnt_bytes);
   a.row_tiles = p.row_tiles;
+  a.log_g = __builtin_ctz((unsigned)(dims->n_q_heads / dims->n_kv_heads));
   a.groups = p.groups;
   a.part_rows = p.part_rows;
   a.grid = p.grid;

@@ -129,6 +129,16 @@ __device__ __forceinline__ float ld_coherent(const float* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Two neighbouring floats at a time (8-byte aligned).
+__device__ __forceinline__ void st_coherent2(float* p, float x, float y) {
+  __hip_atomic_store((unsigned long long*)p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 ld_coherent2(const float* p) {
+  const unsigned long long u = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+}
+
 // Two-wide dot product of packed 16-bit pairs accumulated into fp32: c + a.lo * b.lo + a.hi * b.hi
 // (the products of 16-bit values are exact in fp32).
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));

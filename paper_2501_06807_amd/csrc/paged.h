@@ -53,11 +53,17 @@ struct AttnArgs {
   float qscale;  // sm_scale * log2(e)
 };
 
+// Waves of a workgroup of the paged attention: eight where a wave may take half of a SIMD's registers, four where it takes
+// all of them.
+__host__ __device__ constexpr int paged_waves(int row_tiles) { return row_tiles == 1 ? 8 : 4; }
+constexpr unsigned kMinRun = 4;  // key blocks of a workgroup, at least
+
 struct PagedAttnArgs : AttnArgs {
   PagedCache c;
   int* cnt;       // arrivals of each unit, zero between launches
   float* part;    // [grid][2][part_rows][D + 2]: accumulator, maximum and sum of a unit's part
   int row_tiles;  // 16-row tiles of a unit
+  int log_g;      // G = 2^log_g
   int groups;     // units of a kv head: its query rows over those of a unit
   int part_rows, grid;
 };

@@ -5,8 +5,8 @@
 
 namespace mpc {
 
-// Units of one 16-row tile where the rows fit, else of two. The grid is two workgroups to a compute unit (what the
-// registers of the one-tile kernel allow), or one, or fewer where even the longest sequences have fewer blocks.
+// Units of one 16-row tile where the rows fit, else of two. The grid is one workgroup to a compute unit (eight waves, what
+// the registers allow), or fewer where even the longest sequences have fewer runs of blocks.
 PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap) {
   PagedPlan p{};
   const long long rows = (long long)(Hq / Hkv) * n;
@@ -15,10 +15,10 @@ PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int
   p.groups = (int)((rows + unit_rows - 1) / unit_rows);
   p.part_rows = (int)std::min<long long>(rows, unit_rows);
   const int tile = dtype == MPC_FP32 ? 16 : 32;
-  const long long nb = (cap / tile + 2 + 3) / 4;
+  const long long nb = cap / (tile * paged_waves(p.row_tiles)) + 2;  // complete pages' tiles and the tail's may each be cut short
   const long long units = (long long)L * B * Hkv * p.groups;
   p.blocks = units * nb;
-  p.grid = (int)std::min<long long>(p.row_tiles == 1 ? 2 * kNumCU : kNumCU, p.blocks);
+  p.grid = (int)std::min<long long>(kNumCU, (p.blocks + kMinRun - 1) / kMinRun);
   p.cnt_bytes = ((size_t)units * sizeof(int) + 255) & ~(size_t)255;
   p.ws_bytes = p.cnt_bytes + (size_t)p.grid * 2 * p.part_rows * (D + 2) * sizeof(float);
   return p;

@@ -1,8 +1,8 @@
 // Attention of new tokens over a paged cache on the matrix cores.
 //
 // A work unit is one (sequence, layer, kv head) and a group of 16 RT of its query rows (the G heads of the group times the
-// new tokens), which K and V are read once for. Its keys come in tiles (32 keys, 16 in fp32), four tiles (a wave each) to a
-// block. The grid divides the blocks of all units evenly, whatever the lengths: a workgroup takes a run of blocks, and a
+// new tokens), which K and V are read once for. Its keys come in tiles (32 keys, 16 in fp32), a tile for each wave of the
+// workgroup to a block. The grid divides the blocks of all units evenly, whatever the lengths: a workgroup takes a run of blocks, and a
 // unit that several of them share is joined by the last one to arrive. Lengths are read on the device, so a captured
 // graph follows them.
 //
@@ -18,7 +18,6 @@
 namespace mpc {
 namespace dev {
 
-constexpr int kPagedWaves = 4;
 
 template <class DT, int D, bool CODES, int RT>
 struct PagedTile {
@@ -331,15 +330,16 @@ struct PagedWave {
 };
 
 template <class DT, int D, bool CODES, int RT>
-__global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_attn(PagedAttnArgs a) {
+__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAttnArgs a) {
   using TL = PagedTile<DT, D, CODES, RT>;
-  constexpr int NT = TL::NT, RW = 16 * RT;
+  constexpr int NT = TL::NT, RW = 16 * RT, NW = paged_waves(RT), THREADS = NW * kWave;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int G = a.Hq / a.Hkv;
-  __shared__ __align__(16) f32x4 s_o[2][RT * NT][kWave];
-  __shared__ float s_ml[kPagedWaves][RT][2][kWave];
+  const int G = 1 << a.log_g;
+  __shared__ __align__(16) f32x4 s_o[NW / 2][NT][kWave];
+  __shared__ float s_ml[NW][RT][2][kWave];
+  __shared__ float s_join[2][RW];
   __shared__ int s_last;
 
   // Work of sequence b: units (layer, kv head, row group) of nb blocks each.
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     s.len = min(max(len, 0), kMaxRows);
     s.rows = min(s.len, c.cap());
     s.start = s.len - s.valid;
-    s.groups = (G * s.valid + RW - 1) / RW;
+    s.groups = ((s.valid << a.log_g) + RW - 1) / RW;
     s.full = CODES ? s.rows & ~(c.page - 1) : s.rows;
     const int all = (s.full + TL::TK - 1) / TL::TK;
     s.skip = all;
@@ -363,29 +363,39 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     }
     s.tiles = s.skip + all - s.at;
     const int tail = (s.rows - s.full + TL::TK - 1) / TL::TK;
-    s.nb = max(1, (s.tiles + tail + kPagedWaves - 1) / kPagedWaves);
+    s.nb = max(1, (s.tiles + tail + NW - 1) / NW);
     return s;
   };
-  auto seq_lane = [&](int b) { return seq_of(c.lens[b], c.n_valid ? c.n_valid[b] : c.n_new); };  // a sequence to a lane
   auto seq = [&](int b) { return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new); };
   const int per_group = a.L * a.Hkv;
   auto blocks_of = [&](const Seq& s) { return (unsigned)(s.groups * per_group) * (unsigned)s.nb; };
-  unsigned total = 0;  // below 2^31, as the host has checked for the longest sequences
+  // all blocks (below 2^31, as the host has checked for the longest sequences), sequences to lanes
+  unsigned total = 0, mine = 0;
+  int my_len = 0, my_valid = 0;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int b = b0 + lane;
-    total += wave_sum(b < a.B ? blocks_of(seq_lane(b)) : 0u);
+    const bool in = b0 + lane < a.B;
+    my_len = in ? c.lens[b0 + lane] : 0;
+    my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
+    mine = blocks_of(seq_of(my_len, my_valid));
+    total += wave_sum(mine);
   }
   total = __builtin_amdgcn_readfirstlane(total);
   if (total == 0) return;
-  const unsigned per = (total + gridDim.x - 1) / gridDim.x;
+  // A run is at least kMinRun blocks: below that, joining parts takes longer than the blocks themselves.
+  const unsigned per = max((total + gridDim.x - 1) / gridDim.x, kMinRun);
   if ((unsigned long long)blockIdx.x * per >= total) return;
   const unsigned first = blockIdx.x * per, last = min(first + per, total);
   // the sequence of the first block
   int b = 0;
   unsigned base = 0;  // blocks of the sequences before b
-  for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int i = b0 + lane;
-    const unsigned mine = i < a.B ? blocks_of(seq_lane(i)) : 0u;
+  Seq s;
+  for (int b0 = 0;; b0 += kWave) {
+    if (a.B > kWave) {
+      const bool in = b0 + lane < a.B;
+      my_len = in ? c.lens[b0 + lane] : 0;
+      my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
+      mine = blocks_of(seq_of(my_len, my_valid));
+    }
     unsigned sum = mine;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -394,18 +404,16 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     }
     const unsigned long long past = __ballot(base + sum > first);
     if (past) {
-      const int at = __ffsll((long long)past) - 1;
+      const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)past) - 1);
       b = b0 + at;
-      base += __shfl(sum - mine, at);
+      base += __builtin_amdgcn_readlane(sum - mine, at);
+      s = seq_of(__builtin_amdgcn_readlane(my_len, at), __builtin_amdgcn_readlane(my_valid, at));
       break;
     }
-    base += __shfl(sum, kWave - 1);
+    base += __builtin_amdgcn_readlane(sum, kWave - 1);
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  base = __builtin_amdgcn_readfirstlane(base);
 
   PagedWave<DT, D, CODES, RT> w;
-  Seq s = seq(b);
   unsigned x = first;
   while (x < last) {
     while (x >= base + blocks_of(s)) {
@@ -419,32 +427,8 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
     const unsigned unit0 = x - blk;  // the unit's first block
 
     // rows: token t, head hq of the group, in the order t * G + hq
-    const int r0 = rg * RW, r_end = min(G * s.valid, r0 + RW);
-    const int lo = s.start + r0 / G, hi = s.start + (r_end - 1) / G;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = r0 + 16 * rt + col;
-      const bool ok = r < r_end;
-      const int t = ok ? r / G : 0, hq = h * G + (ok ? r - t * G : 0);
-      w.pos[rt] = ok ? s.start + t : -kMaxRows;
-      const char* row = a.q.at(l, b, hq, t);
-      if constexpr (TL::F) {
-#pragma unroll
-        for (int i = 0; i < TL::QF; i += 4) {
-          const uint4 y = ldg16(row + TL::q_channel(i, g) * 4);
-          w.q[rt][i] = ok ? __uint_as_float(y.x) : 0.f;
-          w.q[rt][i + 1] = ok ? __uint_as_float(y.y) : 0.f;
-          w.q[rt][i + 2] = ok ? __uint_as_float(y.z) : 0.f;
-          w.q[rt][i + 3] = ok ? __uint_as_float(y.w) : 0.f;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < TL::QF; ++i) {
-          const uint4 y = ldg16(row + TL::q_channel(i, g) * 2);
-          w.q[rt][i] = ok ? y : make_uint4(0, 0, 0, 0);
-        }
-      }
-    }
+    const int r0 = rg * RW, r_end = min(s.valid << a.log_g, r0 + RW);
+    const int lo = s.start + (r0 >> a.log_g), hi = s.start + ((r_end - 1) >> a.log_g);
     w.clear();
 
     // this wave's tiles of the run, a tile of every block; those of pages first
@@ -484,8 +468,34 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       }
     };
     using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
-    int i = blk * kPagedWaves + wave;
-    const int i_end = min(blk_end * kPagedWaves, s.tiles);
+    auto load_queries = [&]() {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + 16 * rt + col;
+        const bool ok = r < r_end;
+        const int t = ok ? r >> a.log_g : 0, hq = h * G + (ok ? r - t * G : 0);
+        w.pos[rt] = ok ? s.start + t : -kMaxRows;
+        const char* row = a.q.at(l, b, hq, t);
+        if constexpr (TL::F) {
+#pragma unroll
+          for (int i = 0; i < TL::QF; i += 4) {
+            const uint4 y = ldg16(row + TL::q_channel(i, g) * 4);
+            w.q[rt][i] = ok ? __uint_as_float(y.x) : 0.f;
+            w.q[rt][i + 1] = ok ? __uint_as_float(y.y) : 0.f;
+            w.q[rt][i + 2] = ok ? __uint_as_float(y.z) : 0.f;
+            w.q[rt][i + 3] = ok ? __uint_as_float(y.w) : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < TL::QF; ++i) {
+            const uint4 y = ldg16(row + TL::q_channel(i, g) * 2);
+            w.q[rt][i] = ok ? y : make_uint4(0, 0, 0, 0);
+          }
+        }
+      }
+    };
+    int i = blk * NW + wave;
+    const int i_end = min(blk_end * NW, s.tiles);
     if (i < i_end) {
       // A tile's keys are dead after the scores and its values after the transpose: the next tile's loads go out there,
       // into the same registers, and are waited for a tile's work later.
@@ -497,7 +507,8 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       ids_of(i, entry, id);
       load_k(i, id, k, ks);
       load_v(i, id, v, vs);
-      auto after = [&](int n) { return n + kPagedWaves < i_end ? n + kPagedWaves : n; };
+      load_queries();
+      auto after = [&](int n) { return n + NW < i_end ? n + NW : n; };
       entries_of(after(i), entry);
       for (;;) {
         // the last tile asks for itself again, so that every pass has the same loads in flight and waits for its own only
@@ -536,12 +547,15 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
         i = i1;
       }
     }
+    else {
+      load_queries();
+    }
     if constexpr (CODES) {
       // rows of the page that is not complete, from the ring
-      const int t_end = blk_end * kPagedWaves;
-      int n = blk * kPagedWaves + wave;
-      if (n < s.tiles) n += (s.tiles - n + kPagedWaves - 1) / kPagedWaves * kPagedWaves;
-      for (; n < t_end; n += kPagedWaves) {
+      const int t_end = blk_end * NW;
+      int n = blk * NW + wave;
+      if (n < s.tiles) n += (s.tiles - n + NW - 1) / NW * NW;
+      for (; n < t_end; n += NW) {
         const int k0 = s.full + (n - s.tiles) * TL::TK;
         if (k0 >= s.rows) break;
         const size_t ring = (((size_t)l * c.B + b) * c.Hkv + h) * (2 * c.page);
@@ -584,32 +598,29 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       M[rt] = -INFINITY;
       Lsum[rt] = 0.f;
 #pragma unroll
-      for (int n = 0; n < kPagedWaves; ++n) M[rt] = fmaxf(M[rt], s_ml[n][rt][0][lane]);
+      for (int n = 0; n < NW; ++n) M[rt] = fmaxf(M[rt], s_ml[n][rt][0][lane]);
       const float b0 = M[rt] == -INFINITY ? 0.f : M[rt];
 #pragma unroll
-      for (int n = 0; n < kPagedWaves; ++n) Lsum[rt] += s_ml[n][rt][1][lane] * fast_exp2(s_ml[n][rt][0][lane] - b0);
+      for (int n = 0; n < NW; ++n) Lsum[rt] += s_ml[n][rt][1][lane] * fast_exp2(s_ml[n][rt][0][lane] - b0);
       const float move = fast_exp2(w.m[rt] - b0);
 #pragma unroll
       for (int t = 0; t < NT; ++t) w.o[rt][t] *= move;
     }
-    if (wave >= 2)
+    // half of the waves to the other half, until one has everything
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+    for (int n = NW / 2; n > 0; n /= 2) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) s_o[wave - 2][rt * NT + t][lane] = w.o[rt][t];
-    __syncthreads();
-    if (wave < 2)
+      for (int rt = 0; rt < RT; ++rt) {
+        if (wave >= n && wave < 2 * n)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+          for (int t = 0; t < NT; ++t) s_o[wave - n][t][lane] = w.o[rt][t];
+        __syncthreads();
+        if (wave < n)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) w.o[rt][t] += s_o[wave][rt * NT + t][lane];
-    __syncthreads();
-    if (wave == 1)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) s_o[0][rt * NT + t][lane] = w.o[rt][t];
-    __syncthreads();
+          for (int t = 0; t < NT; ++t) w.o[rt][t] += s_o[wave][t][lane];
+        if (rt + 1 < RT || n > 1) __syncthreads();
+      }
+    }
 
     const unsigned w0 = unit0 / per, w1 = (unit0 + s.nb - 1) / per;  // workgroups that share the unit
     const bool alone = w0 == w1;
@@ -621,7 +632,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       for (int rt = 0; rt < RT; ++rt) {
         const int r = 16 * rt + col;
         if (r >= n_rows) continue;
-        const int t = (r0 + r) / G, hq = h * G + (r0 + r) - t * G;
+        const int t = (r0 + r) >> a.log_g, hq = h * G + (r0 + r) - t * G;
         const float inv = Lsum[rt] == 0.f ? 0.f : 1.f / Lsum[rt];
         char* out = a.out.at(l, b, hq, t);
 #pragma unroll
@@ -629,7 +640,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
           float y[NT];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            y[n] = w.o[rt][n][e] + s_o[0][rt * NT + n][lane][e];
+            y[n] = w.o[rt][n][e];
             if (alone) y[n] = Lsum[rt] == 0.f ? 0.f : y[n] * inv;
           }
           const int ch = (4 * g + e) * NT;
@@ -643,7 +654,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
             }
           } else {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) st_coherent(part + r * (D + 2) + ch + n, y[n]);
+            for (int n = 0; n < NT; n += 2) st_coherent2(part + r * (D + 2) + ch + n, y[n], y[n + 1]);
           }
         }
         if (g == 0) {
@@ -652,8 +663,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
               a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
                   Lsum[rt] == 0.f ? -INFINITY : (M[rt] + __log2f(Lsum[rt])) * 0.69314718055994531f;
           } else {
-            st_coherent(part + r * (D + 2) + D, M[rt]);
-            st_coherent(part + r * (D + 2) + D + 1, Lsum[rt]);
+            st_coherent2(part + r * (D + 2) + D, M[rt], Lsum[rt]);
           }
         }
       }
@@ -663,7 +673,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       // read with device-coherent loads.
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      const int share = (int)(w1 - w0) + 1;
+      const int share = __builtin_amdgcn_readfirstlane((int)(w1 - w0) + 1);
       int* cnt = a.cnt + ((size_t)b * per_group + lh) * a.groups + rg;
       if (threadIdx.x == 0) {
         const int n = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -672,52 +682,89 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
       }
       __syncthreads();
       if (s_last) {
-        for (int item = threadIdx.x; item < n_rows * (D / 4); item += kPagedWaves * kWave) {
-          const int r = item / (D / 4), e = item % (D / 4) * 4;
-          float mx = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-          constexpr int AHEAD = 8;  // parts in flight
-          for (int n0 = 0; n0 < share; n0 += AHEAD) {
-            float pm[AHEAD], pl[AHEAD], po[AHEAD][4];
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) {
-              pm[n] = -INFINITY;
-              pl[n] = 0.f;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) po[n][k] = 0.f;
-              if (n0 + n < share) {
-                // the first sharer's part is its second one unless its run starts with the unit
-                const int second = n0 + n == 0 && w0 * per < unit0;
-                const float* p = a.part + ((size_t)(w0 + n0 + n) * 2 + second) * a.part_rows * (D + 2) + r * (D + 2);
-                pm[n] = ld_coherent(p + D);
-                pl[n] = ld_coherent(p + D + 1);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) po[n][k] = ld_coherent(p + e + k);
-              }
-            }
-            float top = mx;
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) top = fmaxf(top, pm[n]);
-            const float b0 = top == -INFINITY ? 0.f : top, move = fast_exp2(mx - b0);
-            sum *= move;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[k] *= move;
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) {
-              const float f = fast_exp2(pm[n] - b0);
-              sum += pl[n] * f;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) acc[k] += po[n][k] * f;
-            }
+        // the first sharer's part is its second one unless its run starts with the unit
+        const float* part0 = a.part + ((size_t)w0 * 2 + (w0 * per < unit0 ? 1 : 0)) * a.part_rows * (D + 2);
+        const float* part1 = a.part + (size_t)w0 * 2 * a.part_rows * (D + 2);
+        const unsigned step = 2 * a.part_rows * (D + 2);
+        auto part_of = [&](int n) { return n == 0 ? part0 : part1 + (size_t)(n * step); };
+        float* s_m = (float*)&s_o[0][0][0];  // maxima of `fit` parts, all rows
+        const int fit = (int)(sizeof(s_o) / sizeof(float)) / n_rows;
+        // a wave to a row, a lane to a part: the row's maximum and sum
+        for (int r = wave; r < n_rows; r += NW) {
+          float mx = -INFINITY, sum = 0.f;
+          for (int n = lane; n < share; n += kWave) {
+            const float2 ml = ld_coherent2(part_of(n) + r * (D + 2) + D);
+            if (n < fit) s_m[n * n_rows + r] = ml.x;
+            const float top = fmaxf(mx, ml.x), b0 = top == -INFINITY ? 0.f : top;
+            sum = sum * fast_exp2(mx - b0) + ml.y * fast_exp2(ml.x - b0);
             mx = top;
           }
-          const int t = (r0 + r) / G, hq = h * G + (r0 + r) - t * G;
+          float top = mx;
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+          const float b0 = top == -INFINITY ? 0.f : top;
+          sum = wave_sum(sum * fast_exp2(mx - b0));
+          if (lane == 0) {
+            s_join[0][r] = b0;
+            s_join[1][r] = sum;
+          }
+        }
+        // a thread to two channels of a row, the parts divided over `ways` threads where there are enough
+        const int items = n_rows * (D / 2);
+        constexpr int AHEAD = 8;  // parts in flight
+        for (int i0 = 0; i0 < items; i0 += THREADS) {
+          const int ways = i0 == 0 && 2 * items <= THREADS ? THREADS / items : 1;
+          const int item = i0 + (ways > 1 ? threadIdx.x % items : threadIdx.x), way = ways > 1 ? threadIdx.x / items : 0;
+          const bool mine = item < items && way < ways;
+          const int r = mine ? item / (D / 2) : 0, e = item % (D / 2) * 2;
+          float x0 = 0.f, x1 = 0.f;
+          for (int c0 = 0; c0 < share; c0 += fit) {
+            __syncthreads();
+            if (c0 > 0 || i0 > 0) {
+              for (int n = threadIdx.x; n < min(fit, share - c0) * n_rows; n += THREADS)
+                s_m[n] = ld_coherent(part_of(c0 + n / n_rows) + n % n_rows * (D + 2) + D);
+              __syncthreads();
+            }
+            const float b0 = s_join[0][r];
+            const int c1 = mine ? min(share, c0 + fit) : 0;
+            for (int n0 = c0 + way; n0 < c1; n0 += AHEAD * ways) {
+              float2 y[AHEAD];
+#pragma unroll
+              for (int n = 0; n < AHEAD; ++n) y[n] = ld_coherent2(part_of(min(n0 + n * ways, c1 - 1)) + r * (D + 2) + e);
+#pragma unroll
+              for (int n = 0; n < AHEAD; ++n) {
+                const int k = n0 + n * ways;
+                const float f = k < c1 ? fast_exp2(s_m[(min(k, c1 - 1) - c0) * n_rows + r] - b0) : 0.f;
+                x0 = k < c1 ? fmaf(y[n].x, f, x0) : x0;
+                x1 = k < c1 ? fmaf(y[n].y, f, x1) : x1;
+              }
+            }
+          }
+          if (ways > 1) {
+            __syncthreads();
+            float2* s_x = (float2*)&s_o[0][0][0];
+            s_x[threadIdx.x] = make_float2(x0, x1);
+            __syncthreads();
+            if (way > 0) continue;
+            for (int n = 1; n < ways; ++n) {
+              x0 += s_x[item + n * items].x;
+              x1 += s_x[item + n * items].y;
+            }
+          }
+          if (!mine) continue;
+          const float b0 = s_join[0][r], sum = s_join[1][r];
+          const int t = (r0 + r) >> a.log_g, hq = h * G + (r0 + r) - t * G;
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
           char* out = a.out.at(l, b, hq, t) + e * TL::KB;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) store_elt<DT>(out, k, sum == 0.f ? 0.f : acc[k] * inv);
+          x0 = sum == 0.f ? 0.f : x0 * inv;
+          x1 = sum == 0.f ? 0.f : x1 * inv;
+          if constexpr (TL::F)
+            *(float2*)out = make_float2(x0, x1);
+          else
+            *(uint32_t*)out = pack2<DT>(x0, x1);
           if (e == 0 && a.lse)
             a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
-                sum == 0.f ? -INFINITY : (mx + __log2f(sum)) * 0.69314718055994531f;
+                sum == 0.f ? -INFINITY : (b0 + __log2f(sum)) * 0.69314718055994531f;
         }
       }
     }
@@ -728,7 +775,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, RT == 1 ? 2 : 1) void k_paged_a
 
 template <class DT, int D, bool CODES, int RT>
 hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_attn<DT, D, CODES, RT>), dim3((unsigned)a.grid), dim3(kPagedWaves * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attn<DT, D, CODES, RT>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
   return hipGetLastError();
 }
 
