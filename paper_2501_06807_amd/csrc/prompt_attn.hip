@@ -1,51 +1,348 @@
 // Attention of a prompt's rows over its keys, with an optional sliding window and sinks.
-#include "attn_rows.h"
+//
+// 16-bit types (k_prompt): a workgroup of four waves (or two groups of four, which halve the keys) takes 128 rows of one
+// query head, a wave 32 of them. Tiles of keys go through LDS, double-buffered, the next one in registers meanwhile.
+// A wave computes S^T = K Q^T in 32x32x16 products: a lane then holds 16 scores of one row for each 32 keys, the other
+// half of the row's lying 32 lanes on, and its weights, packed to 16 bits, are the operand of O^T += V^T P^T as they
+// stand; V comes from LDS through the transposing reads of gfx950 (four keys of one channel to a lane).
+// The row's reference (what its exponents are taken against) moves only when a score passes it by 2^8, so that the
+// accumulators are seldom rescaled; weights are at most 2^8, their sum and the accumulators fp32.
+#include "attn_mma.h"
 
 namespace mpc {
 namespace {
 
 using namespace dev;
 
-template <class DT, int D>
-struct PlainKeys {
-  const PromptAttnArgs& a;
-  int l, b, h, rows;
-  __device__ int limit() const { return rows; }
-  __device__ bool has(int) const { return true; }
-  __device__ void load8(int j, bool is_v, int e, float* out) const {
-    dev::load8<DT>((is_v ? a.v : a.k).at(l, b, h, j) + e * DT::kElt, out);
-  }
-};
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-template <class DT, int D>
-__global__ __launch_bounds__(kRowWaves* kWave) void k_prompt_rows(PromptAttnArgs a) {
-  __shared__ float s_q[kRowWaves][D];
-  const int w = threadIdx.x / kWave;
-  const int64_t r = (int64_t)blockIdx.x * kRowWaves + w;
-  if (r >= (int64_t)a.L * a.B * a.Hq * a.n) return;
-  const int t = (int)(r % a.n), u = (int)(r / a.n);
-  const int hq = u % a.Hq, b = u / a.Hq % a.B, l = u / a.Hq / a.B;
-  const int q_len = a.q_lens ? min(max(a.q_lens[b], 0), a.n) : a.n;
-  const int k_len = a.k_lens ? min(max(a.k_lens[b], 0), a.T) : a.T;
+template <class DT>
+__device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, f32x16 c) {
+  if constexpr (DT::kCode == MPC_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kRowsWave = 32, kRowsGroup = 4 * kRowsWave;
+constexpr int kXcds = 8;
+constexpr float kSlack = 8.f;  // log2 of how far a weight may pass 1 before its row's reference moves
+
+// Workgroup ids are dealt round-robin over the dies; each die gets one contiguous range of items, so that the query
+// blocks and heads that read the same keys share its L2.
+__device__ __forceinline__ unsigned by_die(unsigned id, unsigned n) {
+  const unsigned q = n / kXcds, r = n % kXcds, x = id % kXcds, slot = id / kXcds;
+  return x < r ? x * (q + 1) + slot : r * (q + 1) + (x - r) * q + slot;
+}
+
+// The tiles of KT keys that rows at positions lo .. hi may see: [0, skip) and [at, at + n - skip).
+struct Tiles {
+  int n, skip, at;
+};
+__device__ __forceinline__ Tiles tiles_of(const AttnArgs& a, int lo, int hi, int rows, int KT) {
+  Tiles t;
+  const int all = max(0, (min(hi + 1, rows) + KT - 1) / KT);
+  t.skip = t.at = all;
+  if (a.window) {
+    t.skip = min((a.sinks + KT - 1) / KT, all);
+    t.at = max(t.skip, min(max(lo - a.window + 1, 0) / KT, all));
+  }
+  t.n = t.skip + all - t.at;
+  return t;
+}
+
+// Keys [k0, k1] as rows at positions lo .. hi see them: none, some, or every row all of them.
+enum { kNone, kSome, kAll };
+__device__ __forceinline__ int seen_by(const AttnArgs& a, int k0, int k1, int lo, int hi, int rows) {
+  if (k0 > hi || k0 >= rows || (a.window && k1 <= lo - a.window && k0 >= a.sinks)) return kNone;
+  return k1 <= lo && k1 < rows && (!a.window || k0 > hi - a.window || k1 < a.sinks) ? kAll : kSome;
+}
+
+// LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that eight rows' pieces of one column fall into
+// different banks, for the fragments of K (a chunk of 32 rows) and for the transposing reads of V (two chunks of four rows).
+template <int D>
+__device__ __forceinline__ int k_chunk(int row, int c) {
+  return row * (D / 8) + (c ^ (row & 7));
+}
+template <int D>
+__device__ __forceinline__ int v_chunk(int row, int c) {
+  return row * (D / 8) + (c ^ ((row & 3) << 1));
+}
+
+template <class DT, int D, int NS>
+__global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
+  constexpr int KT = 64 / NS, KB = KT / 32;  // keys of a tile, and its 32-key blocks
+  constexpr int CH = D / 8, KSTEPS = D / 16, DB = D / 32, THREADS = 256;
+  constexpr int PER = KT * CH / THREADS;  // chunks of K (and of V) that a thread stages
+  __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
+  const int tid = threadIdx.x % THREADS, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
+  const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int G = a.Hq / a.Hkv;
+
+  // item: (layer, sequence, kv head), then the blocks of rows from the last one on, then the heads of the group
+  const unsigned id = by_die(blockIdx.x, gridDim.x);
+  const unsigned nqb = (a.n + kRowsGroup - 1) / kRowsGroup;
+  const int gq = id % G, qb = nqb - 1 - id / G % nqb;
+  const unsigned u = id / G / nqb;
+  const int h = u % a.Hkv, b = u / a.Hkv % a.B, l = u / a.Hkv / a.B, hq = h * G + gq;
+  const int q_len = a.q_lens ? min(max(load_uniform(a.q_lens + b), 0), a.n) : a.n;
+  const int rows = a.k_lens ? min(max(load_uniform(a.k_lens + b), 0), a.T) : a.T;
+  if (qb * kRowsGroup >= q_len) return;
+  const int start = rows - q_len;
+  const int g_lo = start + qb * kRowsGroup, g_hi = start + min(q_len, (qb + 1) * kRowsGroup) - 1;
+  const Tiles tl = tiles_of(a, g_lo, g_hi, rows, KT);
+  const int r0 = qb * kRowsGroup + wave * kRowsWave, t = r0 + q32;
+  const int lo = start + r0, hi = min(lo + kRowsWave - 1, g_hi);  // the wave's rows; none where hi < lo
+  const int pos = start + t;
+
+  // a negative scale is taken into the queries
+  const float c = fabsf(a.qscale);
+  const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
+  uint4 q[KSTEPS];
+  {
+    const char* row = a.q.at(l, b, hq, min(t, q_len - 1)) + hl * 16;
+#pragma unroll
+    for (int i = 0; i < KSTEPS; ++i) {
+      uint4 x = ldg16(row + i * 32);
+      q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+    }
+  }
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float ref = -INFINITY, sum = 0.f;  // reference (in units of the exponent) and sum over this lane's keys
+
+  auto tile_of = [&](int i) { return i < tl.skip ? i : i - tl.skip + tl.at; };
+  uint4 kr[PER], vr[PER];
+  const char *kbase = a.k.at(l, b, h, 0), *vbase = a.v.at(l, b, h, 0);
+  auto fetch = [&](int i) {
+    const int k0 = tile_of(i) * KT;
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      const int x = tid + n * THREADS, row = min(k0 + x / CH, rows - 1);
+      kr[n] = ldg16(kbase + row * a.k.token + x % CH * 16);
+      vr[n] = ldg16(vbase + row * a.v.token + x % CH * 16);
+    }
+  };
+  auto stash = [&](int buf) {
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      const int x = tid + n * THREADS;
+      s_k[grp][buf][k_chunk<D>(x / CH, x % CH)] = kr[n];
+      s_v[grp][buf][v_chunk<D>(x / CH, x % CH)] = vr[n];
+    }
+  };
+  // the groups take every NS-th tile; all of them run the same number of rounds
+  const int rounds = (tl.n + NS - 1) / NS;
+  if (grp < tl.n) fetch(grp);
+  for (int n = 0; n < rounds; ++n) {
+    const int i = n * NS + grp, buf = n & 1;
+    if (i < tl.n) stash(buf);
+    __syncthreads();
+    if (i + NS < tl.n) fetch(i + NS);
+    if (i >= tl.n) continue;
+    const int k0 = tile_of(i) * KT;
+    const int seen = hi < lo ? kNone : seen_by(a, k0, k0 + KT - 1, lo, hi, rows);
+    if (seen == kNone) continue;
+    const uint4* sk = s_k[grp][buf];
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) s[kb] = mma32<DT>(sk[k_chunk<D>(kb * 32 + q32, 2 * ks + hl)], q[ks], s[kb]);
+    }
+    auto key = [&](int kb, int r) { return k0 + 32 * kb + 8 * (r >> 2) + 4 * hl + (r & 3); };
+    auto sees = [&](int j) { return j <= pos && j < rows && (!a.window || j > pos - a.window || j < a.sinks); };
+    if (seen == kSome) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!sees(key(kb, r))) s[kb][r] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+    if (__any(top * c > ref + kSlack || (ref == -INFINITY && top > -INFINITY))) {
+      top = xor_combine<32>(top, [](float x, float y) { return fmaxf(x, y); });
+      const float was = ref;
+      ref = top == -INFINITY ? ref : fmaxf(ref, top * c);
+      // exp2(-inf - 0) = 0: nothing was there to move
+      const float move = fast_exp2(was - (ref == -INFINITY ? 0.f : ref));
+      sum *= move;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= move;
+    }
+    const float base = ref == -INFINITY ? 0.f : ref;
+    uint32_t p[KB][8];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float w0 = fast_exp2(fmaf(s[kb][r], c, -base)), w1 = fast_exp2(fmaf(s[kb][r + 1], c, -base));
+        if (seen == kSome) {  // (a scale of zero makes NaN of a masked score)
+          w0 = sees(key(kb, r)) ? w0 : 0.f;
+          w1 = sees(key(kb, r + 1)) ? w1 : 0.f;
+        }
+        sum += w0 + w1;
+        p[kb][r / 2] = pack2<DT>(w0, w1);
+      }
+    // O^T += V^T P^T, 16 keys at a time: places 0..3 and 4..7 of half hl are keys 4 hl .. and 8 + 4 hl ..
+    const char* sv = (const char*)s_v[grp][buf];
+    const int vrow = 4 * hl + ((lane & 15) >> 2);  // row whose piece this lane asks for, and the piece's 16-byte chunk
+    const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const int j0 = k0 + 32 * kb + 16 * st;
+        const int part = seen == kAll ? kAll : seen_by(a, j0, j0 + 15, lo, hi, rows);
+        if (part == kNone) continue;
+        const uint4 w = make_uint4(p[kb][4 * st], p[kb][4 * st + 1], p[kb][4 * st + 2], p[kb][4 * st + 3]);
+        uint32_t v[DB][4];
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int row = 32 * kb + 16 * st + 8 * e + vrow;
+            const char* at = sv + v_chunk<D>(row, 4 * d + vcol) * 16 + vbyte;
+            const auto x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+            const uint2 y = __builtin_bit_cast(uint2, x);
+            v[d][2 * e] = y.x;
+            v[d][2 * e + 1] = y.y;
+          }
+        if (part == kSome) {
+          // keys that no row of the wave sees do not enter; values that are not finite, in keys that only some rows see, are
+          // added apart, to those rows
+          uint32_t keep[4];
+          bool bad = false;
+#pragma unroll
+          for (int n2 = 0; n2 < 4; ++n2) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int j = j0 + (n2 >= 2 ? 8 : 0) + 4 * hl + (n2 & 1) * 2 + e;
+              const bool any = j < rows && j <= hi && (!a.window || j > lo - a.window || j < a.sinks);
+              m |= any ? 0xFFFFu << 16 * e : 0u;
+            }
+            keep[n2] = m;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+              v[d][n2] &= keep[n2];
+              bad |= not_finite<DT>(v[d][n2]);
+            }
+          }
+          if (__any(bad)) {
+            float one[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) one[e] = sees(j0 + (e >= 4 ? 8 : 0) + 4 * hl + (e & 3)) ? 1.f : 0.f;
+            const uint4 w1 = make_uint4(pack2<DT>(one[0], one[1]), pack2<DT>(one[2], one[3]), pack2<DT>(one[4], one[5]), pack2<DT>(one[6], one[7]));
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+              uint32_t what[4];
+#pragma unroll
+              for (int n2 = 0; n2 < 4; ++n2) what[n2] = take_not_finite<DT>(v[d][n2]);
+              f32x16 y;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) y[r] = 0.f;
+              y = mma32<DT>(make_uint4(what[0], what[1], what[2], what[3]), w1, y);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[d][r] += not_finite_sum(y[r]);
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mma32<DT>(make_uint4(v[d][0], v[d][1], v[d][2], v[d][3]), w, o[d]);
+      }
+  }
+
+  sum = xor_combine<32>(sum, [](float x, float y) { return x + y; });
+  if constexpr (NS == 2) {
+    // the second group's part to the first, through the tiles' LDS
+    constexpr int HALF = DB / 2;
+    float* s_o = (float*)&s_k[0][0][0];  // [4 waves][HALF * 16][64 lanes] each for a half of the channels
+    float* s_st = (float*)&s_v[0][0][0];
+    const float mine = ref;
+    __syncthreads();
+    if (grp == 1) {
+      s_st[(wave * 2) * kWave + lane] = ref;
+      s_st[(wave * 2 + 1) * kWave + lane] = sum;
+    }
+    __syncthreads();
+    float f0 = 1.f, f1 = 0.f;
+    if (grp == 0) {
+      const float r1 = s_st[(wave * 2) * kWave + lane], sum1 = s_st[(wave * 2 + 1) * kWave + lane];
+      ref = fmaxf(mine, r1);
+      const float base = ref == -INFINITY ? 0.f : ref;
+      f0 = fast_exp2(mine - base);
+      f1 = fast_exp2(r1 - base);
+      sum = sum * f0 + sum1 * f1;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      __syncthreads();
+      if (grp == 1)
+#pragma unroll
+        for (int d = 0; d < HALF; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s_o[((wave * HALF + d) * 16 + r) * kWave + lane] = o[e * HALF + d][r];
+      __syncthreads();
+      if (grp == 0)
+#pragma unroll
+        for (int d = 0; d < HALF; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            o[e * HALF + d][r] = o[e * HALF + d][r] * f0 + s_o[((wave * HALF + d) * 16 + r) * kWave + lane] * f1;
+    }
+    if (grp == 1) return;
+  }
   if (t >= q_len) return;
-  const PlainKeys<DT, D> keys{a, l, b, hq / (a.Hq / a.Hkv), k_len};
-  attend_row<DT, D>(a, keys, l, b, hq, t, k_len - q_len + t, s_q[w]);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  char* out = a.out.at(l, b, hq, t);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = sum == 0.f ? 0.f : o[d][r + e] * inv;
+      *(uint2*)(out + (32 * d + 2 * r + 4 * hl) * 2) = make_uint2(pack2<DT>(y[0], y[1]), pack2<DT>(y[2], y[3]));
+    }
+  if (a.lse && hl == 0)
+    a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
+        sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * 0.69314718055994531f;
 }
 
 template <class DT, int D>
-hipError_t launch(const PromptAttnArgs& a, hipStream_t st) {
-  const int64_t blocks = ((int64_t)a.L * a.B * a.Hq * a.n + kRowWaves - 1) / kRowWaves;
-  if (blocks >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_prompt_rows<DT, D>), dim3((unsigned)blocks), dim3(kRowWaves * kWave), 0, st, a);
+hipError_t launch16(const PromptAttnArgs& a, hipStream_t st) {
+  const long long items = (long long)a.L * a.B * a.Hq * ((a.n + kRowsGroup - 1) / kRowsGroup);
+  if (items >= (1ll << 31)) return hipErrorInvalidValue;
+  // where one workgroup to a compute unit is all there is, two groups halve each one's keys
+  if (items <= kNumCU)
+    hipLaunchKernelGGL((k_prompt<DT, D, 2>), dim3((unsigned)items), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_prompt<DT, D, 1>), dim3((unsigned)items), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+hipError_t launch_prompt_attn_fp32(const PromptAttnArgs& a, int D, hipStream_t st);
+
 hipError_t launch_prompt_attn(const PromptAttnArgs& a, int dtype, int D, hipStream_t st) {
-  if (dtype == MPC_FP32) return D == 64 ? launch<F32, 64>(a, st) : launch<F32, 128>(a, st);
-  if (dtype == MPC_FP16) return D == 64 ? launch<F16, 64>(a, st) : launch<F16, 128>(a, st);
-  return D == 64 ? launch<BF16, 64>(a, st) : launch<BF16, 128>(a, st);
+  if (dtype == MPC_FP32) return launch_prompt_attn_fp32(a, D, st);
+  if (dtype == MPC_FP16) return D == 64 ? launch16<F16, 64>(a, st) : launch16<F16, 128>(a, st);
+  return D == 64 ? launch16<BF16, 64>(a, st) : launch16<BF16, 128>(a, st);
 }
 
 }  // namespace mpc
