@@ -36,19 +36,31 @@ __device__ __forceinline__ unsigned by_die(unsigned id, unsigned n) {
   return x < r ? x * (q + 1) + slot : r * (q + 1) + (x - r) * q + slot;
 }
 
-// The tiles of KT keys that rows at positions lo .. hi may see: [0, skip) and [at, at + n - skip).
+// The tiles of KT keys that rows at positions lo .. hi may see, as a list: first the `edge` ones, which some row may not see
+// whole (those of the sinks, at the window's start and at the diagonal), then those that every row sees. Keys may be taken in
+// any order.
 struct Tiles {
-  int n, skip, at;
+  int n, edge;
+  int skip, at, f0, f1;  // sinks [0, skip), window [at, ...) with [f0, f1) seen whole
+  __device__ int id(int i) const {
+    if (i >= edge) return f0 + i - edge;
+    if (i < skip) return i;
+    i += at - skip;
+    return i < f0 ? i : i - f0 + f1;
+  }
 };
 __device__ __forceinline__ Tiles tiles_of(const AttnArgs& a, int lo, int hi, int rows, int KT) {
   Tiles t;
   const int all = max(0, (min(hi + 1, rows) + KT - 1) / KT);
-  t.skip = t.at = all;
+  t.skip = t.at = t.f0 = 0;
   if (a.window) {
     t.skip = min((a.sinks + KT - 1) / KT, all);
     t.at = max(t.skip, min(max(lo - a.window + 1, 0) / KT, all));
+    t.f0 = max(t.at, min((max(hi - a.window + 1, 0) + KT - 1) / KT, all));
   }
-  t.n = t.skip + all - t.at;
+  t.f1 = max(t.f0, (max(min(lo, rows - 1), -1) + 1) / KT);
+  t.edge = t.skip + (t.f0 - t.at) + (all - t.f1);
+  t.n = t.edge + (t.f1 - t.f0);
   return t;
 }
 
@@ -59,11 +71,13 @@ __device__ __forceinline__ int seen_by(const AttnArgs& a, int k0, int k1, int lo
   return k1 <= lo && k1 < rows && (!a.window || k0 > hi - a.window || k1 < a.sinks) ? kAll : kSome;
 }
 
-// LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that eight rows' pieces of one column fall into
-// different banks, for the fragments of K (a chunk of 32 rows) and for the transposing reads of V (two chunks of four rows).
+// LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that 16 rows' pieces of one column fall into
+// different banks, for the fragments of K (a chunk of 32 rows), and for the transposing reads of V (two chunks of four rows).
+// Cycles to a wave's read, as the shader clock counts them: K 4.1 (eight rows apart only: 7.8, not exchanged: 48), V 4.0
+// (not exchanged: 8.0).
 template <int D>
 __device__ __forceinline__ int k_chunk(int row, int c) {
-  return row * (D / 8) + (c ^ (row & 7));
+  return row * (D / 8) + (c ^ (D == 128 ? row & 15 : row >> 1 & 7));
 }
 template <int D>
 __device__ __forceinline__ int v_chunk(int row, int c) {
@@ -72,7 +86,7 @@ __device__ __forceinline__ int v_chunk(int row, int c) {
 
 template <class DT, int D, int NS>
 __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
-  constexpr int KT = 64 / NS, KB = KT / 32;  // keys of a tile, and its 32-key blocks
+  constexpr int KT = 32, KB = KT / 32;  // keys of a tile, and its 32-key blocks
   constexpr int CH = D / 8, KSTEPS = D / 16, DB = D / 32, THREADS = 256;
   constexpr int PER = KT * CH / THREADS;  // chunks of K (and of V) that a thread stages
   __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
@@ -116,16 +130,32 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float ref = -INFINITY, sum = 0.f;  // reference (in units of the exponent) and sum over this lane's keys
 
-  auto tile_of = [&](int i) { return i < tl.skip ? i : i - tl.skip + tl.at; };
   uint4 kr[PER], vr[PER];
   const char *kbase = a.k.at(l, b, h, 0), *vbase = a.v.at(l, b, h, 0);
-  auto fetch = [&](int i) {
-    const int k0 = tile_of(i) * KT;
+  // this thread's chunks of a tile, from the tile's first row
+  int64_t k_off[PER], v_off[PER];
 #pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      const int x = tid + n * THREADS, row = min(k0 + x / CH, rows - 1);
-      kr[n] = ldg16(kbase + row * a.k.token + x % CH * 16);
-      vr[n] = ldg16(vbase + row * a.v.token + x % CH * 16);
+  for (int n = 0; n < PER; ++n) {
+    const int x = tid + n * THREADS;
+    k_off[n] = x / CH * a.k.token + x % CH * 16;
+    v_off[n] = x / CH * a.v.token + x % CH * 16;
+  }
+  auto fetch = [&](int i) {
+    const int k0 = tl.id(i) * KT;
+    if (k0 + KT <= rows) {
+      const char *kp = kbase + k0 * a.k.token, *vp = vbase + k0 * a.v.token;
+#pragma unroll
+      for (int n = 0; n < PER; ++n) {
+        kr[n] = ldg16(kp + k_off[n]);
+        vr[n] = ldg16(vp + v_off[n]);
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < PER; ++n) {
+        const int x = tid + n * THREADS, row = min(k0 + x / CH, rows - 1);
+        kr[n] = ldg16(kbase + row * a.k.token + x % CH * 16);
+        vr[n] = ldg16(vbase + row * a.v.token + x % CH * 16);
+      }
     }
   };
   auto stash = [&](int buf) {
@@ -136,30 +166,52 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
       s_v[grp][buf][v_chunk<D>(x / CH, x % CH)] = vr[n];
     }
   };
-  // the groups take every NS-th tile; all of them run the same number of rounds
-  const int rounds = (tl.n + NS - 1) / NS;
-  if (grp < tl.n) fetch(grp);
-  for (int n = 0; n < rounds; ++n) {
-    const int i = n * NS + grp, buf = n & 1;
-    if (i < tl.n) stash(buf);
-    __syncthreads();
-    if (i + NS < tl.n) fetch(i + NS);
-    if (i >= tl.n) continue;
-    const int k0 = tile_of(i) * KT;
-    const int seen = hi < lo ? kNone : seen_by(a, k0, k0 + KT - 1, lo, hi, rows);
-    if (seen == kNone) continue;
+  // One tile; EDGE: some row of the wave does not see some key of it.
+  auto tile = [&](auto edge, int k0, int buf) {
+    constexpr bool EDGE = decltype(edge)::value;
     const uint4* sk = s_k[grp][buf];
+    const char* sv = (const char*)s_v[grp][buf];
+    // places 0..3 and 4..7 of half hl in a product over 16 keys are keys 4 hl .. and 8 + 4 hl ..
+    const int vrow = 4 * hl + ((lane & 15) >> 2);  // row whose piece this lane asks for, and the piece's 16-byte chunk
+    const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
+    auto values = [&](int kb, int st, uint32_t (*v)[4]) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = 32 * kb + 16 * st + 8 * e + vrow;
+          const char* at = sv + v_chunk<D>(row, 4 * d + vcol) * 16 + vbyte;
+          const auto x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+          const uint2 y = __builtin_bit_cast(uint2, x);
+          v[d][2 * e] = y.x;
+          v[d][2 * e + 1] = y.y;
+        }
+    };
+    uint4 kf[KB][KSTEPS];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) kf[kb][ks] = sk[k_chunk<D>(kb * 32 + q32, 2 * ks + hl)];
+    // the values are asked for before the scores are taken, so that they are there when the weights are
+    uint32_t vf[KB][2][DB][4];
+    if constexpr (!EDGE) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) values(kb, st, vf[kb][st]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) s[kb] = mma32<DT>(sk[k_chunk<D>(kb * 32 + q32, 2 * ks + hl)], q[ks], s[kb]);
+      for (int ks = 0; ks < KSTEPS; ++ks) s[kb] = mma32<DT>(kf[kb][ks], q[ks], s[kb]);
     }
     auto key = [&](int kb, int r) { return k0 + 32 * kb + 8 * (r >> 2) + 4 * hl + (r & 3); };
     auto sees = [&](int j) { return j <= pos && j < rows && (!a.window || j > pos - a.window || j < a.sinks); };
-    if (seen == kSome) {
+    if constexpr (EDGE) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -190,38 +242,25 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         float w0 = fast_exp2(fmaf(s[kb][r], c, -base)), w1 = fast_exp2(fmaf(s[kb][r + 1], c, -base));
-        if (seen == kSome) {  // (a scale of zero makes NaN of a masked score)
+        if constexpr (EDGE) {  // (a scale of zero makes NaN of a masked score)
           w0 = sees(key(kb, r)) ? w0 : 0.f;
           w1 = sees(key(kb, r + 1)) ? w1 : 0.f;
         }
         sum += w0 + w1;
         p[kb][r / 2] = pack2<DT>(w0, w1);
       }
-    // O^T += V^T P^T, 16 keys at a time: places 0..3 and 4..7 of half hl are keys 4 hl .. and 8 + 4 hl ..
-    const char* sv = (const char*)s_v[grp][buf];
-    const int vrow = 4 * hl + ((lane & 15) >> 2);  // row whose piece this lane asks for, and the piece's 16-byte chunk
-    const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
+    // O^T += V^T P^T, 16 keys at a time
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         const int j0 = k0 + 32 * kb + 16 * st;
-        const int part = seen == kAll ? kAll : seen_by(a, j0, j0 + 15, lo, hi, rows);
-        if (part == kNone) continue;
+        const int part = EDGE ? seen_by(a, j0, j0 + 15, lo, hi, rows) : kAll;
+        if (EDGE && part == kNone) continue;
         const uint4 w = make_uint4(p[kb][4 * st], p[kb][4 * st + 1], p[kb][4 * st + 2], p[kb][4 * st + 3]);
-        uint32_t v[DB][4];
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int row = 32 * kb + 16 * st + 8 * e + vrow;
-            const char* at = sv + v_chunk<D>(row, 4 * d + vcol) * 16 + vbyte;
-            const auto x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-            const uint2 y = __builtin_bit_cast(uint2, x);
-            v[d][2 * e] = y.x;
-            v[d][2 * e + 1] = y.y;
-          }
-        if (part == kSome) {
+        uint32_t(*v)[4] = vf[kb][st];
+        if constexpr (EDGE) values(kb, st, v);
+        if (EDGE && part == kSome) {
           // keys that no row of the wave sees do not enter; values that are not finite, in keys that only some rows see, are
           // added apart, to those rows
           uint32_t keep[4];
@@ -264,7 +303,23 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = mma32<DT>(make_uint4(v[d][0], v[d][1], v[d][2], v[d][3]), w, o[d]);
       }
-  }
+  };
+  // the groups take every NS-th tile of the list; all of them run the same number of rounds, and change from edge tiles to
+  // whole ones in the same round (the edge form takes any tile)
+  const int rounds = (tl.n + NS - 1) / NS, edges = (tl.edge + NS - 1) / NS;
+  if (grp < tl.n) fetch(grp);
+  auto round = [&](auto edge, int n) {
+    const int i = n * NS + grp, buf = n & 1;
+    if (i < tl.n) stash(buf);
+    __syncthreads();
+    if (i + NS < tl.n) fetch(i + NS);
+    if (i >= tl.n || hi < lo) return;
+    const int k0 = tl.id(i) * KT;
+    if (decltype(edge)::value && seen_by(a, k0, k0 + KT - 1, lo, hi, rows) == kNone) return;
+    tile(edge, k0, buf);
+  };
+  for (int n = 0; n < edges; ++n) round(std::true_type{}, n);
+  for (int n = edges; n < rounds; ++n) round(std::false_type{}, n);
 
   sum = xor_combine<32>(sum, [](float x, float y) { return x + y; });
   if constexpr (NS == 2) {
