@@ -65,6 +65,11 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
   constexpr uint32_t lo = DT::kCode == MPC_BF16 ? 0x7F80u : 0x7C00u, hi = lo << 16;
   return (w & lo) == lo || (w & hi) == hi;
 }
+// Largest magnitude bits of the 16-bit values so far, by half, and whether they say that one was not finite.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t top, uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
+}
 // Takes the values that are not finite out of a word (zero in their place) and returns what they were.
 template <class DT>
 __device__ __forceinline__ uint32_t take_not_finite(uint32_t& w) {

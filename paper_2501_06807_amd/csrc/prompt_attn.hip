@@ -64,11 +64,9 @@ __device__ __forceinline__ Tiles tiles_of(const AttnArgs& a, int lo, int hi, int
   return t;
 }
 
-// Keys [k0, k1] as rows at positions lo .. hi see them: none, some, or every row all of them.
-enum { kNone, kSome, kAll };
-__device__ __forceinline__ int seen_by(const AttnArgs& a, int k0, int k1, int lo, int hi, int rows) {
-  if (k0 > hi || k0 >= rows || (a.window && k1 <= lo - a.window && k0 >= a.sinks)) return kNone;
-  return k1 <= lo && k1 < rows && (!a.window || k0 > hi - a.window || k1 < a.sinks) ? kAll : kSome;
+// Whether any row at positions lo .. hi sees any of the keys [k0, k1].
+__device__ __forceinline__ bool seen_by(const AttnArgs& a, int k0, int k1, int lo, int hi, int rows) {
+  return k0 <= hi && k0 < rows && (!a.window || k1 > lo - a.window || k0 < a.sinks);
 }
 
 // LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that 16 rows' pieces of one column fall into
@@ -90,6 +88,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   constexpr int CH = D / 8, KSTEPS = D / 16, DB = D / 32, THREADS = 256;
   constexpr int PER = KT * CH / THREADS;  // chunks of K (and of V) that a thread stages
   __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
+  __shared__ int s_bad[NS][2];  // the last round whose values, staged for an edge, were not all finite
   const int tid = threadIdx.x % THREADS, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
   const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -112,7 +111,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   const int pos = start + t;
 
   // a negative scale is taken into the queries
-  const float c = fabsf(a.qscale);
+  const float c = fmaxf(fabsf(a.qscale), 1e-30f);  // (zero times a masked score would be NaN)
   const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
   uint4 q[KSTEPS];
   {
@@ -166,8 +165,14 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
       s_v[grp][buf][v_chunk<D>(x / CH, x % CH)] = vr[n];
     }
   };
-  // One tile; EDGE: some row of the wave does not see some key of it.
-  auto tile = [&](auto edge, int k0, int buf) {
+  auto staged_not_finite = [&]() {
+    uint32_t top = 0;
+#pragma unroll
+    for (int n = 0; n < PER; ++n) top = max_magnitude(max_magnitude(max_magnitude(max_magnitude(top, vr[n].x), vr[n].y), vr[n].z), vr[n].w);
+    return not_finite<DT>(top);
+  };
+  // One tile; EDGE: some row of the wave may not see some key of it, and `bad` says that its values are not all finite.
+  auto tile = [&](auto edge, int k0, int buf, bool bad) {
     constexpr bool EDGE = decltype(edge)::value;
     const uint4* sk = s_k[grp][buf];
     const char* sv = (const char*)s_v[grp][buf];
@@ -194,12 +199,10 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
       for (int ks = 0; ks < KSTEPS; ++ks) kf[kb][ks] = sk[k_chunk<D>(kb * 32 + q32, 2 * ks + hl)];
     // the values are asked for before the scores are taken, so that they are there when the weights are
     uint32_t vf[KB][2][DB][4];
-    if constexpr (!EDGE) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) values(kb, st, vf[kb][st]);
-    }
+      for (int st = 0; st < 2; ++st) values(kb, st, vf[kb][st]);
     __builtin_amdgcn_sched_barrier(0);
     f32x16 s[KB];
 #pragma unroll
@@ -209,14 +212,27 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) s[kb] = mma32<DT>(kf[kb][ks], q[ks], s[kb]);
     }
-    auto key = [&](int kb, int r) { return k0 + 32 * kb + 8 * (r >> 2) + 4 * hl + (r & 3); };
-    auto sees = [&](int j) { return j <= pos && j < rows && (!a.window || j > pos - a.window || j < a.sinks); };
     if constexpr (EDGE) {
+      // the lane's keys lie (8 (r / 4) + r % 4) behind this one
+      const int j0 = k0 + 4 * hl;
+      if (k0 + KT - 1 > min(lo, rows - 1)) {
+        const int last = min(pos, rows - 1) - j0;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!sees(key(kb, r))) s[kb][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r)
+            if (32 * kb + 8 * (r >> 2) + (r & 3) > last) s[kb][r] = -INFINITY;
+      }
+      if (a.window && k0 <= hi - a.window && k0 + KT > a.sinks) {
+        const int gone = pos - a.window - j0, sinks = a.sinks - j0;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+            if (j <= gone && j >= sinks) s[kb][r] = -INFINITY;
+          }
+      }
     }
     float top = -INFINITY;
 #pragma unroll
@@ -241,11 +257,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
-        float w0 = fast_exp2(fmaf(s[kb][r], c, -base)), w1 = fast_exp2(fmaf(s[kb][r + 1], c, -base));
-        if constexpr (EDGE) {  // (a scale of zero makes NaN of a masked score)
-          w0 = sees(key(kb, r)) ? w0 : 0.f;
-          w1 = sees(key(kb, r + 1)) ? w1 : 0.f;
-        }
+        const float w0 = fast_exp2(fmaf(s[kb][r], c, -base)), w1 = fast_exp2(fmaf(s[kb][r + 1], c, -base));
         sum += w0 + w1;
         p[kb][r / 2] = pack2<DT>(w0, w1);
       }
@@ -254,43 +266,25 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const int j0 = k0 + 32 * kb + 16 * st;
-        const int part = EDGE ? seen_by(a, j0, j0 + 15, lo, hi, rows) : kAll;
-        if (EDGE && part == kNone) continue;
         const uint4 w = make_uint4(p[kb][4 * st], p[kb][4 * st + 1], p[kb][4 * st + 2], p[kb][4 * st + 3]);
         uint32_t(*v)[4] = vf[kb][st];
-        if constexpr (EDGE) values(kb, st, v);
-        if (EDGE && part == kSome) {
-          // keys that no row of the wave sees do not enter; values that are not finite, in keys that only some rows see, are
-          // added apart, to those rows
-          uint32_t keep[4];
-          bool bad = false;
-#pragma unroll
-          for (int n2 = 0; n2 < 4; ++n2) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int j = j0 + (n2 >= 2 ? 8 : 0) + 4 * hl + (n2 & 1) * 2 + e;
-              const bool any = j < rows && j <= hi && (!a.window || j > lo - a.window || j < a.sinks);
-              m |= any ? 0xFFFFu << 16 * e : 0u;
-            }
-            keep[n2] = m;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              v[d][n2] &= keep[n2];
-              bad |= not_finite<DT>(v[d][n2]);
-            }
-          }
-          if (__any(bad)) {
+        if constexpr (EDGE) {
+          // Values that are not finite, in keys that some row does not see, must not meet that row's weight of zero: they
+          // are added apart, to the rows that see them
+          if (bad) {
+            const int j0 = k0 + 32 * kb + 16 * st + 4 * hl;
             float one[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) one[e] = sees(j0 + (e >= 4 ? 8 : 0) + 4 * hl + (e & 3)) ? 1.f : 0.f;
+            for (int e = 0; e < 8; ++e) {
+              const int j = j0 + (e >= 4 ? 8 : 0) + (e & 3);
+              one[e] = j <= pos && j < rows && (!a.window || j > pos - a.window || j < a.sinks) ? 1.f : 0.f;
+            }
             const uint4 w1 = make_uint4(pack2<DT>(one[0], one[1]), pack2<DT>(one[2], one[3]), pack2<DT>(one[4], one[5]), pack2<DT>(one[6], one[7]));
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
               uint32_t what[4];
 #pragma unroll
-              for (int n2 = 0; n2 < 4; ++n2) what[n2] = take_not_finite<DT>(v[d][n2]);
+              for (int n = 0; n < 4; ++n) what[n] = take_not_finite<DT>(v[d][n]);
               f32x16 y;
 #pragma unroll
               for (int r = 0; r < 16; ++r) y[r] = 0.f;
@@ -308,15 +302,21 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   // whole ones in the same round (the edge form takes any tile)
   const int rounds = (tl.n + NS - 1) / NS, edges = (tl.edge + NS - 1) / NS;
   if (grp < tl.n) fetch(grp);
+  if (threadIdx.x < 2 * NS) (&s_bad[0][0])[threadIdx.x] = -1;
+  __syncthreads();
   auto round = [&](auto edge, int n) {
+    constexpr bool EDGE = decltype(edge)::value;
     const int i = n * NS + grp, buf = n & 1;
-    if (i < tl.n) stash(buf);
+    if (i < tl.n) {
+      if (EDGE && staged_not_finite()) s_bad[grp][buf] = n;
+      stash(buf);
+    }
     __syncthreads();
     if (i + NS < tl.n) fetch(i + NS);
     if (i >= tl.n || hi < lo) return;
     const int k0 = tl.id(i) * KT;
-    if (decltype(edge)::value && seen_by(a, k0, k0 + KT - 1, lo, hi, rows) == kNone) return;
-    tile(edge, k0, buf);
+    if (EDGE && !seen_by(a, k0, k0 + KT - 1, lo, hi, rows)) return;
+    tile(edge, k0, buf, EDGE && __builtin_amdgcn_readfirstlane(s_bad[grp][buf]) == n);
   };
   for (int n = 0; n < edges; ++n) round(std::true_type{}, n);
   for (int n = edges; n < rounds; ++n) round(std::false_type{}, n);
