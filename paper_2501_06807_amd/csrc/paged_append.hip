@@ -4,13 +4,13 @@
 // pair it rotates (vectors i and i + half the rotated ones), reads and writes each once, and may write in place.
 // Every product and sum of the rotation is rounded on its own (no fused multiply-add), so that the rows, and with
 // them the codes of a page, do not depend on how the compiler groups them.
-#include "paged_dev.h"
+#include "attn_mma.h"
 
 namespace mpc {
 namespace {
 
 using namespace dev;
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kMaxPageThreads = 1024;  // (a page of 256 rows of 128 in fp32, four items to a thread)
 
 template <class DT>
 struct Pair {
@@ -94,10 +94,10 @@ __device__ __forceinline__ void load_item(const char* row, const Item& it, const
 // Rows to rows: the queries, and K and V into pages of the element type. Heads run q, k, v.
 template <class DT, int D, bool KV>
 __device__ __forceinline__ void move_rows(const PagedAppendArgs& a, int64_t block) {
-  constexpr int NI = D / DT::kVec / 2, ROWS = kThreads / NI;
+  constexpr int NI = D / DT::kVec / 2;
   const PagedCache& c = a.c;
   const int heads = a.Hq + (KV ? 2 * c.Hkv : 0);
-  const int64_t r0 = block * ROWS;
+  const int64_t r0 = block * (blockDim.x / NI);
   const int64_t u0 = r0 / c.n_new;
   const unsigned t0 = (unsigned)(r0 - u0 * c.n_new) + threadIdx.x / NI;
   const int64_t u = u0 + t0 / (unsigned)c.n_new;
@@ -129,97 +129,138 @@ __device__ __forceinline__ void move_rows(const PagedAppendArgs& a, int64_t bloc
   *(uint4*)(dst + it.vb * 16) = y;
 }
 
-// One page of K or V of one (layer, sequence, head): codes once it is complete, and the ring rows of the new tokens in
-// the last two pages. The ring rows of later pages lie where the first page's earlier rows lay; the workgroup that reads
-// these writes those, after it.
-template <class DT, int D>
-__device__ __forceinline__ void append_page(const PagedAppendArgs& a, int64_t block) {
+// Largest magnitude of one item's values so far, as float bits, and whether one was not finite.
+template <class DT>
+__device__ __forceinline__ uint32_t item_max(uint32_t top, const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT::kElt == 4)
+      top = max(top, w[i] & 0x7FFFFFFFu);
+    else
+      top = max_magnitude(top, w[i]);  // both halves, still in the 16-bit type
+  }
+  return top;
+}
+template <class DT>
+__device__ __forceinline__ uint32_t finite_max(uint32_t top, const uint4& x) {
+  float f[DT::kVec];
+  unpack<DT>(x, f);
+#pragma unroll
+  for (int e = 0; e < DT::kVec; ++e) top = max(top, finite_bits(f[e]));
+  return top;
+}
+// The codes of a vector in units of the page's scale; clamped where some of the thread's values were not finite.
+template <class DT>
+__device__ __forceinline__ void store_codes(char* p, const uint4& x, float inv, bool odd) {
+  float f[DT::kVec];
+  unpack<DT>(x, f);
+#pragma unroll
+  for (int e = 0; e < DT::kVec; ++e) f[e] = odd ? to_code_range(f[e], inv) : f[e] * inv;
+  if constexpr (DT::kVec == 4)
+    *(uint32_t*)p = encode4(f[0], f[1], f[2], f[3]);
+  else
+    *(uint2*)p = make_uint2(encode4(f[0], f[1], f[2], f[3]), encode4(f[4], f[5], f[6], f[7]));
+}
+
+// One page of K or V of one (layer, sequence, head), a thread to IPT of its items: read (and rotated) once, kept in registers
+// for the page's maximum and its codes, which are written when the page is complete, and for the ring rows of the new
+// tokens in the last two pages. The ring rows of later pages lie where the first page's earlier rows lay; the workgroup that
+// reads these writes those, after it.
+template <class DT, int D, int IPT>
+__device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned block) {
   constexpr int NI = D / DT::kVec / 2, V = DT::kVec, RB = D * DT::kElt;
-  __shared__ uint32_t s_max[kThreads / kWave];
+  __shared__ uint32_t s_max[kMaxPageThreads / kWave];
   const PagedCache& c = a.c;
   const bool is_v = block & 1;
-  const int i = (int)((block >> 1) % a.np);
-  const int u = (int)((block >> 1) / a.np);
+  const unsigned pu = block >> 1;
+  const int i = pu % (unsigned)a.np, u = pu / (unsigned)a.np;
   const int h = u % c.Hkv, b = u / c.Hkv % c.B, l = u / c.Hkv / c.B;
-  const int valid = c.valid(b), len = c.len(b), start = len - valid;
+  const int len = min(max(load_uniform(c.lens + b), 0), kMaxRows);
+  const int valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
+  const int start = len - valid;
   if (valid == 0 || len == 0) return;
   const int p0 = max(start, 0) >> c.log_page, last = (len - 1) >> c.log_page, pg = p0 + i;
   if (pg > last || pg >= c.max_pages) return;
-  const Rows& in = is_v ? a.v : a.k;
+  const int entry = page_entry(c, b, pg);
+  const int pos0 = a.pos0 ? load_uniform(a.pos0 + b) : start;
+  const char* in = (is_v ? a.v : a.k).at(l, b, h, 0);
+  const int64_t step = (is_v ? a.v : a.k).token;
   char* ring = (is_v ? c.v_tail : c.k_tail) + (size_t)u * (2 * c.page) * RB;
-  const int items = c.page * NI;
   RopeArgs r = a.rope;
   if (is_v) r.table = nullptr;
-  auto load = [&](int n, int page, uint4& x, uint4& y) -> Item {
-    const int j = (page << c.log_page) + n / NI;
-    const Item it = item_of<DT>(n % NI, r.rot);
-    if (j >= start) {
-      const int t = j - start;
-      load_item<DT>(in.at(l, b, h, t), it, r, a.pos0 ? a.pos0[b] + t : j, x, y);
-    } else {
-      const char* row = ring + (size_t)(j & (2 * c.page - 1)) * RB;
-      x = ldg16(row + it.va * 16);
-      y = ldg16(row + it.vb * 16);
-    }
-    return it;
-  };
-  const int id = page_id(c, b, pg);
-  if (((pg + 1) << c.log_page) <= len && id >= 0) {
-    uint32_t top = 0;
-    for (int n = threadIdx.x; n < items; n += kThreads) {
-      uint4 x, y;
-      load(n, pg, x, y);
-      float f[V], g[V];
-      unpack<DT>(x, f);
-      unpack<DT>(y, g);
+  uint4 x[IPT], y[IPT];
+  Item it[IPT];
+  // the items of `page` that are wanted: its new rows, and the earlier ones from the ring
+  auto load = [&](int page, bool earlier) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) top = max(top, max(finite_bits(f[e]), finite_bits(g[e])));
+    for (int k = 0; k < IPT; ++k) {
+      const int n = threadIdx.x + k * blockDim.x, j = (page << c.log_page) + n / NI;
+      it[k] = item_of<DT>(n % NI, r.rot);
+      x[k] = y[k] = make_uint4(0, 0, 0, 0);
+      if (j >= start && j < len) {
+        load_item<DT>(in + (j - start) * step, it[k], r, pos0 + (j - start), x[k], y[k]);
+      } else if (j < start && earlier) {
+        const char* row = ring + (size_t)(j & (2 * c.page - 1)) * RB;
+        x[k] = ldg16(row + it[k].va * 16);
+        y[k] = ldg16(row + it[k].vb * 16);
+      }
+    }
+  };
+  auto keep = [&](int page) {
+#pragma unroll
+    for (int k = 0; k < IPT; ++k) {
+      const int j = (page << c.log_page) + (threadIdx.x + k * blockDim.x) / NI;
+      if (j < start || j >= len) continue;
+      char* row = ring + (size_t)(j & (2 * c.page - 1)) * RB;
+      *(uint4*)(row + it[k].va * 16) = x[k];
+      *(uint4*)(row + it[k].vb * 16) = y[k];
+    }
+  };
+  const int id = page_of_entry(c, entry, pg);
+  const bool whole = ((pg + 1) << c.log_page) <= len && id >= 0;
+  const bool kept = i <= 1 && pg >= last - 1;
+  if (!whole && !kept && !(i == 0 && last >= p0 + 2)) return;
+  load(pg, whole);
+  if (kept) keep(pg);
+  if (whole) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < IPT; ++k) top = item_max<DT>(item_max<DT>(top, x[k]), y[k]);
+    const bool odd = not_finite<DT>(top);
+    if (odd) {
+      top = 0;
+#pragma unroll
+      for (int k = 0; k < IPT; ++k) top = finite_max<DT>(finite_max<DT>(top, x[k]), y[k]);
+    } else if constexpr (DT::kElt == 2) {
+      const uint32_t m = max(top & 0xFFFFu, top >> 16);
+      top = __float_as_uint(DT::kCode == MPC_BF16 ? bf16_to_f32(m) : f16_to_f32(m));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    if (threadIdx.x % kWave == 0) s_max[threadIdx.x / kWave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) top = max(top, s_max[w]);
+    if (blockDim.x > kWave) {
+      if (threadIdx.x % kWave == 0) s_max[threadIdx.x / kWave] = top;
+      __syncthreads();
+      for (int w = 0; w < (int)blockDim.x / kWave; ++w) top = max(top, s_max[w]);
+    }
     const int e2 = scale_exponent(top);
     const float inv = pow2(-e2);
     const size_t unit = page_unit(c, l, id, h);
     char* dst = (is_v ? c.v : c.k) + unit * c.page * (size_t)D;
     if (threadIdx.x == 0) (is_v ? c.vs : c.ks)[unit] = pow2(e2);
-    for (int n = threadIdx.x; n < items; n += kThreads) {
-      uint4 x, y;
-      const Item it = load(n, pg, x, y);
-      float f[V], g[V];
-      unpack<DT>(x, f);
-      unpack<DT>(y, g);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        f[e] = to_code_range(f[e], inv);
-        g[e] = to_code_range(g[e], inv);
-      }
-      char* row = dst + (size_t)(n / NI) * D;
-#pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        *(uint32_t*)(row + it.va * V + e) = encode4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-        *(uint32_t*)(row + it.vb * V + e) = encode4(g[e], g[e + 1], g[e + 2], g[e + 3]);
-      }
+    for (int k = 0; k < IPT; ++k) {
+      char* row = dst + (size_t)((threadIdx.x + k * blockDim.x) / NI) * D;
+      store_codes<DT>(row + it[k].va * V, x[k], inv, odd);
+      store_codes<DT>(row + it[k].vb * V, y[k], inv, odd);
     }
   }
-  auto keep = [&](int page) {
-    for (int n = threadIdx.x; n < items; n += kThreads) {
-      const int j = (page << c.log_page) + n / NI;
-      if (j < start || j >= len) continue;
-      uint4 x, y;
-      const Item it = load(n, page, x, y);
-      char* row = ring + (size_t)(j & (2 * c.page - 1)) * RB;
-      *(uint4*)(row + it.va * 16) = x;
-      *(uint4*)(row + it.vb * 16) = y;
-    }
-  };
-  if (i <= 1 && pg >= last - 1) keep(pg);
   if (i == 0 && last >= p0 + 2) {
-    __syncthreads();
-    for (int page = max(p0 + 2, last - 1); page <= last && page < c.max_pages; ++page) keep(page);
+    __syncthreads();  // the earlier rows have been read
+    for (int page = max(p0 + 2, last - 1); page <= last && page < c.max_pages; ++page) {
+      load(page, false);
+      keep(page);
+    }
   }
 }
 
@@ -228,27 +269,34 @@ __global__ __launch_bounds__(kThreads) void k_append_rows_paged(PagedAppendArgs 
   move_rows<DT, D, true>(a, blockIdx.x);
 }
 
-template <class DT, int D>
-__global__ __launch_bounds__(kThreads) void k_append_pages(PagedAppendArgs a, unsigned pages) {
+// Pages first (they take longest), then the queries.
+template <class DT, int D, int IPT>
+__global__ __launch_bounds__(IPT == 1 ? 2 * kWave : kMaxPageThreads) void k_append_pages(PagedAppendArgs a, unsigned pages) {
   if (blockIdx.x < pages)
-    append_page<DT, D>(a, blockIdx.x);
+    append_page<DT, D, IPT>(a, blockIdx.x);
   else
     move_rows<DT, D, false>(a, blockIdx.x - pages);
 }
 
 template <class DT, int D>
 hipError_t launch(const PagedAppendArgs& a, hipStream_t st) {
-  constexpr int ROWS = kThreads / (D / DT::kVec / 2);
+  constexpr int NI = D / DT::kVec / 2;
   const PagedCache& c = a.c;
   const int64_t lb = (int64_t)c.L * c.B;
   const bool codes = c.ks != nullptr;
+  // a page's items are divided over threads four each, or one each where that would leave less than a wave
+  const int items = c.page * NI, ipt = items >= 4 * kWave ? 4 : 1;
+  const int threads = codes ? items / ipt : kThreads, per_block = threads / NI;
   const int64_t rows = lb * (a.Hq + (codes ? 0 : 2 * c.Hkv)) * c.n_new;
-  const int64_t moves = (rows + ROWS - 1) / ROWS, pages = codes ? lb * c.Hkv * a.np * 2 : 0;
+  const int64_t moves = (rows + per_block - 1) / per_block, pages = codes ? lb * c.Hkv * a.np * 2 : 0;
   if (moves + pages >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-  if (codes)
-    hipLaunchKernelGGL((k_append_pages<DT, D>), dim3((unsigned)(moves + pages)), dim3(kThreads), 0, st, a, (unsigned)pages);
+  const dim3 grid((unsigned)(moves + pages));
+  if (!codes)
+    hipLaunchKernelGGL((k_append_rows_paged<DT, D>), grid, dim3(threads), 0, st, a);
+  else if (ipt == 4)
+    hipLaunchKernelGGL((k_append_pages<DT, D, 4>), grid, dim3(threads), 0, st, a, (unsigned)pages);
   else
-    hipLaunchKernelGGL((k_append_rows_paged<DT, D>), dim3((unsigned)moves), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((k_append_pages<DT, D, 1>), grid, dim3(threads), 0, st, a, (unsigned)pages);
   return hipGetLastError();
 }
 
