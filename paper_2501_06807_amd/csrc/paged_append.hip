@@ -29,104 +29,132 @@ __device__ __forceinline__ Item item_of(int i, int rot) {
   return {2 * i, 2 * i + 1, false};
 }
 
+// The (cos, sin) pairs of an item at a position, as they lie in the table: of vector va's channels (HALF), or of the pairs
+// within both vectors.
 template <class DT>
-__device__ __forceinline__ void turn_pair(Pair<DT>& x, const Item& it, const RopeArgs& r, int pos) {
-#pragma clang fp contract(off)
+struct Angles {
+  float4 t[DT::kVec / 2];
+};
+template <class DT>
+__device__ __forceinline__ Angles<DT> angles_of(const RopeArgs& r, const Item& it, int pos) {
   constexpr int V = DT::kVec;
   const bool ok = pos >= 0 && pos < r.n_pos;
   const float2* cs = r.table + (size_t)(ok ? pos : 0) * (r.rot / 2);
-  const float bad = __uint_as_float(0x7FC00000u);
-  if (r.half) {
+  const float2 *lo = cs + it.va * (r.half ? V : V / 2), *hi = r.half ? lo + V / 2 : cs + it.vb * (V / 2);
+  Angles<DT> x;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float2 t = cs[it.va * V + i];
-      const float c = ok ? t.x : bad, s = ok ? t.y : bad;
-      const float a = x.a[i], b = x.b[i];
-      x.a[i] = a * c - b * s;
-      x.b[i] = a * s + b * c;
-    }
-  } else {
-    auto within = [&](float* y, int v) {
+  for (int i = 0; i < V / 4; ++i) {
+    x.t[i] = *(const float4*)(lo + 2 * i);
+    x.t[V / 4 + i] = *(const float4*)(hi + 2 * i);
+  }
+  if (!ok)
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float2 t = cs[v * (V / 2) + i];
-        const float c = ok ? t.x : bad, s = ok ? t.y : bad;
-        const float a = y[2 * i], b = y[2 * i + 1];
-        y[2 * i] = a * c - b * s;
-        y[2 * i + 1] = a * s + b * c;
-      }
-    };
-    within(x.a, it.va);
-    within(x.b, it.vb);
+    for (int i = 0; i < V / 2; ++i) x.t[i].x = x.t[i].y = x.t[i].z = x.t[i].w = __uint_as_float(0x7FC00000u);
+  return x;
+}
+
+template <class DT>
+__device__ __forceinline__ void turn_pair(Pair<DT>& x, bool half, const Angles<DT>& g) {
+#pragma clang fp contract(off)
+  constexpr int V = DT::kVec;
+  float c[V], s[V], u[V], v[V];  // pair i is (u[i], v[i])
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) {
+    c[2 * i] = g.t[i].x;
+    s[2 * i] = g.t[i].y;
+    c[2 * i + 1] = g.t[i].z;
+    s[2 * i + 1] = g.t[i].w;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float a = 2 * i < V ? x.a[2 * i < V ? 2 * i : 0] : x.b[2 * i < V ? 0 : 2 * i - V];
+    const float b = 2 * i < V ? x.a[2 * i < V ? 2 * i + 1 : 0] : x.b[2 * i < V ? 0 : 2 * i + 1 - V];
+    u[i] = half ? x.a[i] : a;
+    v[i] = half ? x.b[i] : b;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float a = u[i], b = v[i];
+    u[i] = a * c[i] - b * s[i];
+    v[i] = a * s[i] + b * c[i];
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    x.a[i] = half ? u[i] : i % 2 ? v[i / 2] : u[i / 2];
+    x.b[i] = half ? v[i] : i % 2 ? v[V / 2 + i / 2] : u[V / 2 + i / 2];
   }
 }
 
 template <class DT>
 __device__ __forceinline__ uint4 pack(const float* x) {
-  if constexpr (DT::kVec == 4) {
+  if constexpr (DT::kVec == 4)
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = DT::kCode == MPC_BF16 ? f32_to_bf16(x[2 * i]) : f32_to_f16(x[2 * i]);
-      const uint32_t hi = DT::kCode == MPC_BF16 ? f32_to_bf16(x[2 * i + 1]) : f32_to_f16(x[2 * i + 1]);
-      w[i] = lo | hi << 16;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
+  else
+    return make_uint4(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3]), pack2<DT>(x[4], x[5]), pack2<DT>(x[6], x[7]));
 }
 
-// One item of one row, rotated where `r` asks for it, as the element type holds it.
+// Both vectors of an item, turned, as the element type holds them.
 template <class DT>
-__device__ __forceinline__ void load_item(const char* row, const Item& it, const RopeArgs& r, int pos, uint4& a, uint4& b) {
-  a = ldg16(row + it.va * 16);
-  b = ldg16(row + it.vb * 16);
-  if (!r.table || !it.turn) return;
+__device__ __forceinline__ void turn_item(uint4& a, uint4& b, bool half, const Angles<DT>& g) {
   Pair<DT> x;
   unpack<DT>(a, x.a);
   unpack<DT>(b, x.b);
-  turn_pair<DT>(x, it, r, pos);
+  turn_pair<DT>(x, half, g);
   a = pack<DT>(x.a);
   b = pack<DT>(x.b);
 }
 
-// Rows to rows: the queries, and K and V into pages of the element type. Heads run q, k, v.
-template <class DT, int D, bool KV>
-__device__ __forceinline__ void move_rows(const PagedAppendArgs& a, int64_t block) {
+// Rows to rows: the queries, and (KV) K and V into pages of the element type. A workgroup takes a run of tokens of one
+// sequence and a few heads (q, k, then v): a thread has one item of one token, whose angles it reads once, in up to HPT
+// heads.
+struct Moves {
+  int tokens, lanes;  // tokens of a workgroup (a power of two), and heads side by side
+  int chunks, runs;   // head chunks and token runs of a (layer, sequence)
+};
+template <class DT, int D, bool KV, int HPT>
+__device__ __forceinline__ void move_rows(const PagedAppendArgs& a, const Moves& m, unsigned block) {
   constexpr int NI = D / DT::kVec / 2;
   const PagedCache& c = a.c;
   const int heads = a.Hq + (KV ? 2 * c.Hkv : 0);
-  const int64_t r0 = block * (blockDim.x / NI);
-  const int64_t u0 = r0 / c.n_new;
-  const unsigned t0 = (unsigned)(r0 - u0 * c.n_new) + threadIdx.x / NI;
-  const int64_t u = u0 + t0 / (unsigned)c.n_new;
-  const int t = (int)(t0 % (unsigned)c.n_new);
-  if (u >= (int64_t)c.L * c.B * heads) return;
-  const int hh = (int)((unsigned)u % (unsigned)heads), lb = (int)((unsigned)u / (unsigned)heads);
-  const int b = lb % c.B, l = lb / c.B;
-  const int valid = c.valid(b);
+  const int chunk = block % (unsigned)m.chunks, run = block / (unsigned)m.chunks % (unsigned)m.runs;
+  const int lb = block / (unsigned)m.chunks / (unsigned)m.runs, b = lb % c.B, l = lb / c.B;
+  const int tr = threadIdx.x / NI, t = run * m.tokens + (tr & (m.tokens - 1)), lane = tr / m.tokens;
+  const int valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
   if (t >= valid) return;
-  const int j = c.len(b) - valid + t, pos = a.pos0 ? a.pos0[b] + t : j;
-  const bool is_q = hh < a.Hq, is_v = hh >= a.Hq + c.Hkv;
-  const int h = is_q ? hh : is_v ? hh - a.Hq - c.Hkv : hh - a.Hq;
-  const char* src = is_q ? a.q.at(l, b, h, t) : is_v ? a.v.at(l, b, h, t) : a.k.at(l, b, h, t);
-  char* dst;
-  if (is_q) {
-    dst = a.q_out.at(l, b, h, t);
-  } else {
-    if (j < 0) return;
-    const int id = page_id(c, b, j >> c.log_page);
-    if (id < 0) return;
-    dst = (is_v ? c.v : c.k) + (page_unit(c, l, id, h) * c.page + (j & (c.page - 1))) * (size_t)(D * DT::kElt);
+  const int j = min(max(load_uniform(c.lens + b), 0), kMaxRows) - valid + t;
+  const int pos = a.pos0 ? load_uniform(a.pos0 + b) + t : j;
+  const Item it = item_of<DT>(threadIdx.x % NI, a.rope.rot);
+  const bool turned = a.rope.table && it.turn;
+  const int h0 = chunk * HPT * m.lanes + lane;
+  uint4 x[HPT], y[HPT];
+#pragma unroll
+  for (int k = 0; k < HPT; ++k) {
+    const int hh = h0 + k * m.lanes;
+    if (hh >= heads) continue;
+    const char* src = hh < a.Hq ? a.q.at(l, b, hh, t) : hh < a.Hq + c.Hkv ? a.k.at(l, b, hh - a.Hq, t) : a.v.at(l, b, hh - a.Hq - c.Hkv, t);
+    x[k] = ldg16(src + it.va * 16);
+    y[k] = ldg16(src + it.vb * 16);
   }
-  RopeArgs r = a.rope;
-  if (is_v) r.table = nullptr;
-  const Item it = item_of<DT>(threadIdx.x % NI, r.rot);
-  uint4 x, y;
-  load_item<DT>(src, it, r, pos, x, y);
-  *(uint4*)(dst + it.va * 16) = x;
-  *(uint4*)(dst + it.vb * 16) = y;
+  Angles<DT> g;
+  if (turned) g = angles_of<DT>(a.rope, it, pos);
+  const int id = KV && j >= 0 ? page_id_lane(c, b, j >> c.log_page) : -1;
+#pragma unroll
+  for (int k = 0; k < HPT; ++k) {
+    const int hh = h0 + k * m.lanes;
+    if (hh >= heads) continue;
+    if (turned && hh < a.Hq + c.Hkv) turn_item<DT>(x[k], y[k], a.rope.half, g);
+    char* dst;
+    if (hh < a.Hq) {
+      dst = a.q_out.at(l, b, hh, t);
+    } else {
+      if (id < 0) continue;
+      const bool is_v = hh >= a.Hq + c.Hkv;
+      const int h = hh - a.Hq - (is_v ? c.Hkv : 0);
+      dst = (is_v ? c.v : c.k) + (page_unit(c, l, id, h) * c.page + (j & (c.page - 1))) * (size_t)(D * DT::kElt);
+    }
+    *(uint4*)(dst + it.va * 16) = x[k];
+    *(uint4*)(dst + it.vb * 16) = y[k];
+  }
 }
 
 // Largest magnitude of one item's values so far, as float bits, and whether one was not finite.
@@ -172,10 +200,11 @@ __device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned b
   constexpr int NI = D / DT::kVec / 2, V = DT::kVec, RB = D * DT::kElt;
   __shared__ uint32_t s_max[kMaxPageThreads / kWave];
   const PagedCache& c = a.c;
+  // K and V and the heads of one page side by side: they read the same angles
   const bool is_v = block & 1;
-  const unsigned pu = block >> 1;
-  const int i = pu % (unsigned)a.np, u = pu / (unsigned)a.np;
-  const int h = u % c.Hkv, b = u / c.Hkv % c.B, l = u / c.Hkv / c.B;
+  const unsigned ph = (block >> 1) / (unsigned)c.Hkv;
+  const int h = (block >> 1) - ph * c.Hkv, i = ph % (unsigned)a.np, lb = ph / (unsigned)a.np, b = lb % c.B, l = lb / c.B;
+  const int u = lb * c.Hkv + h;
   const int len = min(max(load_uniform(c.lens + b), 0), kMaxRows);
   const int valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
   const int start = len - valid;
@@ -187,8 +216,7 @@ __device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned b
   const char* in = (is_v ? a.v : a.k).at(l, b, h, 0);
   const int64_t step = (is_v ? a.v : a.k).token;
   char* ring = (is_v ? c.v_tail : c.k_tail) + (size_t)u * (2 * c.page) * RB;
-  RopeArgs r = a.rope;
-  if (is_v) r.table = nullptr;
+  const bool turned = a.rope.table && !is_v;
   uint4 x[IPT], y[IPT];
   Item it[IPT];
   // the items of `page` that are wanted: its new rows, and the earlier ones from the ring
@@ -196,16 +224,22 @@ __device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned b
 #pragma unroll
     for (int k = 0; k < IPT; ++k) {
       const int n = threadIdx.x + k * blockDim.x, j = (page << c.log_page) + n / NI;
-      it[k] = item_of<DT>(n % NI, r.rot);
+      it[k] = item_of<DT>(n % NI, a.rope.rot);
       x[k] = y[k] = make_uint4(0, 0, 0, 0);
-      if (j >= start && j < len) {
-        load_item<DT>(in + (j - start) * step, it[k], r, pos0 + (j - start), x[k], y[k]);
-      } else if (j < start && earlier) {
-        const char* row = ring + (size_t)(j & (2 * c.page - 1)) * RB;
+      const bool fresh = j >= start;
+      if (fresh ? j < len : earlier) {
+        const char* row = fresh ? in + (j - start) * step : ring + (size_t)(j & (2 * c.page - 1)) * RB;
         x[k] = ldg16(row + it[k].va * 16);
         y[k] = ldg16(row + it[k].vb * 16);
       }
     }
+    if (turned)
+#pragma unroll
+      for (int k = 0; k < IPT; ++k) {
+        const int j = (page << c.log_page) + (threadIdx.x + k * blockDim.x) / NI;
+        if (it[k].turn && j >= start && j < len)
+          turn_item<DT>(x[k], y[k], a.rope.half, angles_of<DT>(a.rope, it[k], pos0 + (j - start)));
+      }
   };
   auto keep = [&](int page) {
 #pragma unroll
@@ -264,18 +298,18 @@ __device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned b
   }
 }
 
-template <class DT, int D>
-__global__ __launch_bounds__(kThreads) void k_append_rows_paged(PagedAppendArgs a) {
-  move_rows<DT, D, true>(a, blockIdx.x);
+template <class DT, int D, int HPT>
+__global__ __launch_bounds__(kThreads) void k_append_rows_paged(PagedAppendArgs a, Moves m) {
+  move_rows<DT, D, true, HPT>(a, m, blockIdx.x);
 }
 
 // Pages first (they take longest), then the queries.
-template <class DT, int D, int IPT>
-__global__ __launch_bounds__(IPT == 1 ? 2 * kWave : kMaxPageThreads) void k_append_pages(PagedAppendArgs a, unsigned pages) {
+template <class DT, int D, int IPT, int HPT>
+__global__ __launch_bounds__(IPT == 1 ? 2 * kWave : kMaxPageThreads) void k_append_pages(PagedAppendArgs a, Moves m, unsigned pages) {
   if (blockIdx.x < pages)
     append_page<DT, D, IPT>(a, blockIdx.x);
   else
-    move_rows<DT, D, false>(a, blockIdx.x - pages);
+    move_rows<DT, D, false, HPT>(a, m, blockIdx.x - pages);
 }
 
 template <class DT, int D>
@@ -286,17 +320,32 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t st) {
   const bool codes = c.ks != nullptr;
   // a page's items are divided over threads four each, or one each where that would leave less than a wave
   const int items = c.page * NI, ipt = items >= 4 * kWave ? 4 : 1;
-  const int threads = codes ? items / ipt : kThreads, per_block = threads / NI;
-  const int64_t rows = lb * (a.Hq + (codes ? 0 : 2 * c.Hkv)) * c.n_new;
-  const int64_t moves = (rows + per_block - 1) / per_block, pages = codes ? lb * c.Hkv * a.np * 2 : 0;
+  const int threads = codes ? items / ipt : kThreads, slots = threads / NI, heads = a.Hq + (codes ? 0 : 2 * c.Hkv);
+  Moves m{};
+  m.tokens = 1;
+  while (m.tokens < slots && m.tokens < c.n_new) m.tokens *= 2;
+  m.lanes = slots / m.tokens;
+  m.runs = (int)(((int64_t)c.n_new + m.tokens - 1) / m.tokens);
+  // four heads to a thread, where that leaves a few workgroups to a compute unit
+  const int64_t some = lb * m.runs * ((heads + 4 * m.lanes - 1) / (4 * m.lanes));
+  const int hpt = some >= 4 * kNumCU ? 4 : 1;
+  m.chunks = (heads + hpt * m.lanes - 1) / (hpt * m.lanes);
+  const int64_t moves = lb * m.runs * m.chunks, pages = codes ? lb * c.Hkv * a.np * 2 : 0;
   if (moves + pages >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(moves + pages));
-  if (!codes)
-    hipLaunchKernelGGL((k_append_rows_paged<DT, D>), grid, dim3(threads), 0, st, a);
+  const unsigned p = (unsigned)pages;
+  if (!codes && hpt == 4)
+    hipLaunchKernelGGL((k_append_rows_paged<DT, D, 4>), grid, dim3(threads), 0, st, a, m);
+  else if (!codes)
+    hipLaunchKernelGGL((k_append_rows_paged<DT, D, 1>), grid, dim3(threads), 0, st, a, m);
+  else if (ipt == 4 && hpt == 4)
+    hipLaunchKernelGGL((k_append_pages<DT, D, 4, 4>), grid, dim3(threads), 0, st, a, m, p);
   else if (ipt == 4)
-    hipLaunchKernelGGL((k_append_pages<DT, D, 4>), grid, dim3(threads), 0, st, a, (unsigned)pages);
+    hipLaunchKernelGGL((k_append_pages<DT, D, 4, 1>), grid, dim3(threads), 0, st, a, m, p);
+  else if (hpt == 4)
+    hipLaunchKernelGGL((k_append_pages<DT, D, 1, 4>), grid, dim3(threads), 0, st, a, m, p);
   else
-    hipLaunchKernelGGL((k_append_pages<DT, D, 1>), grid, dim3(threads), 0, st, a, (unsigned)pages);
+    hipLaunchKernelGGL((k_append_pages<DT, D, 1, 1>), grid, dim3(threads), 0, st, a, m, p);
   return hipGetLastError();
 }
 

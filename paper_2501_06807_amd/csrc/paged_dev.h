@@ -38,11 +38,12 @@ __device__ __forceinline__ float to_code_range(float x, float inv) {
   return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
 }
 
-// Eight consecutive channels as floats.
-template <class DT>
-__device__ __forceinline__ void load8(const char* p, float* out) {
-  unpack<DT>(ldg16(p), out);
-  if constexpr (DT::kVec == 4) unpack<DT>(ldg16(p + 16), out + 4);
+// Workgroup ids are dealt round-robin over the dies; each die gets one contiguous range of the n items, so that neighbours,
+// which read the same rows, share its L2.
+constexpr unsigned kDies = 8;
+__device__ __forceinline__ unsigned by_die(unsigned id, unsigned n) {
+  const unsigned q = n / kDies, r = n % kDies, x = id % kDies, slot = id / kDies;
+  return x < r ? x * (q + 1) + slot : r * (q + 1) + (x - r) * q + slot;
 }
 
 // A value that the launch does not write, at an address that is the same over the wave: through the scalar cache, so that
@@ -52,19 +53,16 @@ __device__ __forceinline__ T load_uniform(const T* p) {
   return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
 }
 
-// Page id of logical page pg of sequence b, or -1 where the table or the pool has none.
-__device__ __forceinline__ int page_id(const PagedCache& c, int b, int pg) {
-  if (pg < 0 || pg >= c.max_pages) return -1;
-  const int id = c.table[(size_t)b * c.max_pages + pg];
-  return (unsigned)id < (unsigned)c.n_pages ? id : -1;
-}
-// The same in two steps for b and pg (not negative) that are the same over the wave: the table's entry, asked for early, and
-// what it says.
+// Page id of logical page pg (not negative) of sequence b, or -1 where the table or the pool has none, in two steps: the
+// table's entry, asked for early (b and pg the same over the wave, or with a lane to each), and what it says.
 __device__ __forceinline__ int page_entry(const PagedCache& c, int b, int pg) {
   return load_uniform(c.table + (size_t)b * c.max_pages + min(pg, c.max_pages - 1));
 }
 __device__ __forceinline__ int page_of_entry(const PagedCache& c, int entry, int pg) {
   return pg < c.max_pages && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
+}
+__device__ __forceinline__ int page_id_lane(const PagedCache& c, int b, int pg) {
+  return page_of_entry(c, c.table[(size_t)b * c.max_pages + min(pg, c.max_pages - 1)], pg);
 }
 // Index of (layer, page, head) in the pool.
 __device__ __forceinline__ size_t page_unit(const PagedCache& c, int l, int id, int h) {

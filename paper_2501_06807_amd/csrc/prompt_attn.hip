@@ -26,15 +26,7 @@ __device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, f32x16 c
 }
 
 constexpr int kRowsWave = 32, kRowsGroup = 4 * kRowsWave;
-constexpr int kXcds = 8;
 constexpr float kSlack = 8.f;  // log2 of how far a weight may pass 1 before its row's reference moves
-
-// Workgroup ids are dealt round-robin over the dies; each die gets one contiguous range of items, so that the query
-// blocks and heads that read the same keys share its L2.
-__device__ __forceinline__ unsigned by_die(unsigned id, unsigned n) {
-  const unsigned q = n / kXcds, r = n % kXcds, x = id % kXcds, slot = id / kXcds;
-  return x < r ? x * (q + 1) + slot : r * (q + 1) + (x - r) * q + slot;
-}
 
 // The tiles of KT keys that rows at positions lo .. hi may see, as a list: first the `edge` ones, which some row may not see
 // whole (those of the sinks, at the window's start and at the diagonal), then those that every row sees. Keys may be taken in
