@@ -358,28 +358,29 @@ ROPE_STYLE = {"interleaved": 0, "half": 1}
 PAGE_FORMAT = {"same": 0, "e4m3": 1}
 
 
-def _rows(t, what, kv_dtype, heads=None):
-    """A tensor [L][B][H][n][d] (or [L][B][H][d], n = 1): (pointer, strides or None where contiguous, n). The last axis
+def _rows(t, what, dtype, heads=None):
+    """A tensor [L][B][H][n][d] (or [L][B][H][d], n = 1): (pointer, strides or None where contiguous, shape). The last axis
     must have stride 1; the other strides are the caller's."""
     if t.dim() == 4:
         t = t.unsqueeze(3)
-    if t.dim() != 5 or not t.is_cuda or t.dtype != kv_dtype:
-        raise ValueError(f"{what} must be a CUDA tensor [L][B][H][n][d] of type {kv_dtype}")
-    if heads is not None and t.shape[2] != heads:
+    if t.dim() != 5 or not t.is_cuda or t.dtype is not dtype:
+        raise ValueError(f"{what} must be a CUDA tensor [L][B][H][n][d] of type {dtype}")
+    shape = t.shape
+    if heads is not None and shape[2] != heads:
         raise ValueError(f"{what} must have {heads} heads")
     if t.is_contiguous():
-        return ctypes.c_void_p(t.data_ptr()), None, t.shape
+        return t.data_ptr(), None, shape
     if t.stride(4) != 1:
         raise ValueError(f"{what}: the channels of a row must be contiguous")
-    return ctypes.c_void_p(t.data_ptr()), ctypes.byref(MpcStrides(*t.stride()[:4])), t.shape
+    return t.data_ptr(), ctypes.byref(MpcStrides(*t.stride()[:4])), shape
 
 
 def _batch_ints(t, what, B, device):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != device:
+    if t.dtype is not torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{what} must be a contiguous int32 tensor [{B}] on {device}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _on(device, stream, *tensors):
@@ -388,19 +389,21 @@ def _on(device, stream, *tensors):
         if t is not None and t.device != device:
             raise ValueError(f"a tensor on {t.device} in a call on {device}")
     if stream is None:
-        return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(device.index)  # (current_stream() without its object)
     if stream.device != device:
         raise ValueError(f"a stream of {stream.device} in a call on {device}")
-    return ctypes.c_void_p(stream.cuda_stream)
+    return stream.cuda_stream
 
 
-def _call(fn, device, *args):
+def _call(name, fn, device, *args):
     """One library call with `device` as the current one, which its launches go to."""
-    if device.index == torch.cuda.current_device():
-        _check(fn, getattr(lib(), fn)(*args))
+    if device.index == torch._C._cuda_getDevice():
+        status = fn(*args)
     else:
         with torch.cuda.device(device):
-            _check(fn, getattr(lib(), fn)(*args))
+            status = fn(*args)
+    if status != MPC_OK:
+        _check(name, status)
 
 
 class PagedKV:
@@ -441,10 +444,13 @@ class PagedKV:
         self.c = MpcPagedKv(self.page, P, M, PAGE_FORMAT["e4m3" if codes else "same"], p(k_pages), p(v_pages), p(k_scale),
                             p(v_scale), p(k_tail), p(v_tail), p(table), p(lens))
         self.ref = ctypes.byref(self.c)
+        self._dims = {}
 
     def dims(self, n_q_heads):
-        return MpcDims(batch=self.B, layer0=0, n_layers=self.L, n_q_heads=n_q_heads, n_kv_heads=self.Hkv, head_dim=self.d,
-                       dtype=DTYPE_CODE[self.dtype])
+        """The mpc_dims (as an argument) of a call with that many query heads."""
+        if n_q_heads not in self._dims:
+            self._dims[n_q_heads] = ctypes.byref(MpcDims(self.B, 0, self.L, n_q_heads, self.Hkv, self.d, DTYPE_CODE[self.dtype], 0))
+        return self._dims[n_q_heads]
 
 
 def paged_kv(*, n_layers, batch, n_kv_heads, head_dim, dtype, n_pages, max_pages, page_size=64, fp8=False, device="cuda"):
@@ -492,13 +498,13 @@ def mpc_paged_append(k, v, kv, *, q=None, q_out=None, rope=None, rope_style="int
     elif q_out is not None:
         raise ValueError("q_out is given without q")
     st = _on(kv.device, stream, k, v, q, q_out, rope)
-    _call("mpc_paged_append", kv.device, ctypes.byref(kv.dims(Hq)), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
+    _call("mpc_paged_append", lib().mpc_paged_append, kv.device, kv.dims(Hq), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
           r, _batch_ints(pos0, "pos0", kv.B, kv.device), kp, ks, vp, vs, qp, qs, op, os_, st)
 
 
 def paged_attn_workspace_bytes(q, kv):
     """Workspace bytes of mpc_paged_attn for queries shaped like q [L][B][Hq][n][d] (or [L][B][Hq][d])."""
-    return lib().mpc_workspace_bytes(MPC_OP_PAGED_ATTN, ctypes.byref(kv.dims(q.shape[2])), q.shape[3] if q.dim() == 5 else 1,
+    return lib().mpc_workspace_bytes(MPC_OP_PAGED_ATTN, kv.dims(q.shape[2]), q.shape[3] if q.dim() == 5 else 1,
                                      kv.ref)
 
 
@@ -507,7 +513,7 @@ def _lse_of(lse, shape):
         return None
     if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != shape[0] * shape[1] * shape[2] * shape[3]:
         raise ValueError("lse must be contiguous float32 [L][B][Hq][n]")
-    return ctypes.c_void_p(lse.data_ptr())
+    return lse.data_ptr()
 
 
 def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse=None, ws=None, stream=None):
@@ -525,9 +531,9 @@ def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse
     _contig(ws)
     st = _on(kv.device, stream, q, out, lse, ws)
     cfg = MpcAttnCfg(sm_scale, window, sinks)
-    _call("mpc_paged_attn", kv.device, ctypes.byref(kv.dims(shape[2])), kv.ref, n,
+    _call("mpc_paged_attn", lib().mpc_paged_attn, kv.device, kv.dims(shape[2]), kv.ref, n,
           _batch_ints(n_valid, "n_valid", kv.B, kv.device), ctypes.byref(cfg), qp, qs, op, os_, _lse_of(lse, shape),
-          ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(), st)
+          ws.data_ptr(), ws.numel() * ws.element_size(), st)
 
 
 def mpc_prompt_attn(q, k, v, out, *, sm_scale, window=0, sinks=0, q_lens=None, k_lens=None, lse=None, stream=None):
@@ -547,7 +553,7 @@ def mpc_prompt_attn(q, k, v, out, *, sm_scale, window=0, sinks=0, q_lens=None, k
     L, B, Hq, Tq, d = shape
     dev = q.device
     st = _on(dev, stream, k, v, out, lse)
-    dims = MpcDims(batch=B, layer0=0, n_layers=L, n_q_heads=Hq, n_kv_heads=kshape[2], head_dim=d, dtype=DTYPE_CODE[q.dtype])
+    dims = MpcDims(B, 0, L, Hq, kshape[2], d, DTYPE_CODE[q.dtype], 0)
     cfg = MpcAttnCfg(sm_scale, window, sinks)
-    _call("mpc_prompt_attn", dev, ctypes.byref(dims), Tq, kshape[3], _batch_ints(q_lens, "q_lens", B, dev),
+    _call("mpc_prompt_attn", lib().mpc_prompt_attn, dev, ctypes.byref(dims), Tq, kshape[3], _batch_ints(q_lens, "q_lens", B, dev),
           _batch_ints(k_lens, "k_lens", B, dev), ctypes.byref(cfg), qp, qs, kp, ks, vp, vs, op, os_, _lse_of(lse, shape), st)
