@@ -358,6 +358,9 @@ mpc_status mpc_commonality(int32_t L, int32_t units, int32_t k, int32_t m, const
  *   k, v   [L][B][Hkv][n_new][d] (k_strides, v_strides; NULL: contiguous)
  *   q      [L][B][Hq][n_new][d] or NULL; its rotated rows go to q_out (rows from n_valid[b] on are left
  *          as they were), which may be q itself and may not overlap anything otherwise;
+ *   k_out  [L][B][Hkv][n_new][d] or NULL: also receives K's rows as the cache takes them (rotated, in the
+ *          element type), for mpc_prompt_attn; those of rows 0 <= j < M * page_size are written. It may not
+ *          overlap k or anything else;
  *   rope   NULL: no rotation (q must then be NULL too).
  * MPC_PAGE_SAME writes the rows into their pages. MPC_PAGE_E4M3 writes a page when its last row arrives,
  * from its rows in the element type (earlier calls' from the tail): scale = the least 2^e, e in
@@ -370,7 +373,8 @@ mpc_status mpc_commonality(int32_t L, int32_t units, int32_t k, int32_t m, const
 mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                             const mpc_rope* rope, const int32_t* pos0, const void* k, const mpc_strides* k_strides,
                             const void* v, const mpc_strides* v_strides, const void* q, const mpc_strides* q_strides,
-                            void* q_out, const mpc_strides* q_out_strides, void* stream);
+                            void* q_out, const mpc_strides* q_out_strides, void* k_out,
+                            const mpc_strides* k_out_strides, void* stream);
 
 /* Attention of each sequence's newest n_valid[b] tokens (one, some drafted ones, a chunk of a prompt) over
  * a paged cache that holds them already: row t stands at position p = lens[b] - n_valid[b] + t among the

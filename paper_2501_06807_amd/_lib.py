@@ -93,7 +93,7 @@ def lib():
         L.mpc_decode_step_status.argtypes = [V, ctypes.c_size_t, I, P(I)]
         L.mpc_commonality.argtypes = [I, I, I, I, V, V, V]
         KV, S, A = P(MpcPagedKv), P(MpcStrides), P(MpcAttnCfg)
-        L.mpc_paged_append.argtypes = [P(MpcDims), KV, I, V, P(MpcRope), V] + [V, S] * 4 + [V]
+        L.mpc_paged_append.argtypes = [P(MpcDims), KV, I, V, P(MpcRope), V] + [V, S] * 5 + [V]
         L.mpc_paged_attn.argtypes = [P(MpcDims), KV, I, V, A] + [V, S] * 2 + [V, V, ctypes.c_size_t, V]
         L.mpc_prompt_attn.argtypes = [P(MpcDims), I, I, V, V, A] + [V, S] * 4 + [V, V]
         for fn in ("mpc_paged_append", "mpc_paged_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
@@ -473,11 +473,12 @@ def _like(shape, kv, n, what):
         raise ValueError(f"{what} must be [{kv.L}][{kv.B}][H][{n}][{kv.d}]")
 
 
-def mpc_paged_append(k, v, kv, *, q=None, q_out=None, rope=None, rope_style="interleaved", pos0=None, n_valid=None,
-                     stream=None):
+def mpc_paged_append(k, v, kv, *, q=None, q_out=None, k_out=None, rope=None, rope_style="interleaved", pos0=None,
+                     n_valid=None, stream=None):
     """k, v [L][B][Hkv][n][d] (or [L][B][Hkv][d]), any strides, into the cache `kv` at the rows before kv.lens. rope
     [n_pos][rot_dim / 2][2] float32 (cos, sin) rotates K, and q [L][B][Hq][n][d] into q_out (q itself by default), by the
-    positions pos0 [B] + t (the row numbers by default). n_valid [B]: new tokens of each sequence (n by default)."""
+    positions pos0 [B] + t (the row numbers by default); k_out (shaped like k) also receives K's rows as the cache takes
+    them. n_valid [B]: new tokens of each sequence (n by default)."""
     kp, ks, shape = _rows(k, "k", kv.dtype, kv.Hkv)
     n = shape[3]
     _like(shape, kv, n, "k")
@@ -497,9 +498,13 @@ def mpc_paged_append(k, v, kv, *, q=None, q_out=None, rope=None, rope_style="int
         _like(shape, kv, n, "q_out")
     elif q_out is not None:
         raise ValueError("q_out is given without q")
-    st = _on(kv.device, stream, k, v, q, q_out, rope)
+    kop = kos = None
+    if k_out is not None:
+        kop, kos, shape = _rows(k_out, "k_out", kv.dtype, kv.Hkv)
+        _like(shape, kv, n, "k_out")
+    st = _on(kv.device, stream, k, v, q, q_out, k_out, rope)
     _call("mpc_paged_append", lib().mpc_paged_append, kv.device, kv.dims(Hq), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
-          r, _batch_ints(pos0, "pos0", kv.B, kv.device), kp, ks, vp, vs, qp, qs, op, os_, st)
+          r, _batch_ints(pos0, "pos0", kv.B, kv.device), kp, ks, vp, vs, qp, qs, op, os_, kop, kos, st)
 
 
 def paged_attn_workspace_bytes(q, kv):

@@ -845,7 +845,8 @@ mpc_status mpc_append_kv(const mpc_dims* dims, int32_t Ts, int32_t n_tail, const
 mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                             const mpc_rope* rope, const int32_t* pos0, const void* k, const mpc_strides* k_strides,
                             const void* v, const mpc_strides* v_strides, const void* q, const mpc_strides* q_strides,
-                            void* q_out, const mpc_strides* q_out_strides, void* stream) {
+                            void* q_out, const mpc_strides* q_out_strides, void* k_out,
+                            const mpc_strides* k_out_strides, void* stream) {
   mpc_status s = check_dims(dims);
   if (s != MPC_OK) return s;
   mpc::PagedAppendArgs a{};
@@ -868,6 +869,10 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
     a.Hq = dims->n_q_heads;
   } else if (q_out) {
     return fail(MPC_EINVAL, "q_out is given without q");
+  }
+  if (k_out) {
+    if (k_out == k) return fail(MPC_EINVAL, "k_out may not be k");
+    if ((s = rows_of(dims, "k_out", k_out, k_out_strides, dims->n_kv_heads, n_new, true, &a.k_out)) != MPC_OK) return s;
   }
   a.pos0 = pos0;
   a.np = (n_new + kv->page_size - 2) / kv->page_size + 1;

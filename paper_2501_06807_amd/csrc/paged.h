@@ -39,7 +39,7 @@ struct PagedAppendArgs {
   PagedCache c;
   RopeArgs rope;
   const int32_t* pos0;
-  Rows k, v, q, q_out;
+  Rows k, v, q, q_out, k_out;  // k_out.p null: not asked for
   int Hq;        // 0 without queries
   int np;        // pages that the new tokens of one sequence can touch
 };

@@ -147,9 +147,14 @@ __device__ __forceinline__ void move_rows(const PagedAppendArgs& a, const Moves&
     if (hh < a.Hq) {
       dst = a.q_out.at(l, b, hh, t);
     } else {
-      if (id < 0) continue;
       const bool is_v = hh >= a.Hq + c.Hkv;
       const int h = hh - a.Hq - (is_v ? c.Hkv : 0);
+      if (a.k_out.p && !is_v && j >= 0 && j < c.cap()) {
+        char* row = a.k_out.at(l, b, h, t);
+        *(uint4*)(row + it.va * 16) = x[k];
+        *(uint4*)(row + it.vb * 16) = y[k];
+      }
+      if (id < 0) continue;
       dst = (is_v ? c.v : c.k) + (page_unit(c, l, id, h) * c.page + (j & (c.page - 1))) * (size_t)(D * DT::kElt);
     }
     *(uint4*)(dst + it.va * 16) = x[k];
@@ -253,10 +258,20 @@ __device__ __forceinline__ void append_page(const PagedAppendArgs& a, unsigned b
   };
   const int id = page_of_entry(c, entry, pg);
   const bool whole = ((pg + 1) << c.log_page) <= len && id >= 0;
-  const bool kept = i <= 1 && pg >= last - 1;
-  if (!whole && !kept && !(i == 0 && last >= p0 + 2)) return;
+  const bool kept = i <= 1 && pg >= last - 1, plain = a.k_out.p && !is_v;
+  if (!whole && !kept && !plain && !(i == 0 && last >= p0 + 2)) return;
   load(pg, whole);
   if (kept) keep(pg);
+  if (plain) {
+#pragma unroll
+    for (int k = 0; k < IPT; ++k) {
+      const int j = (pg << c.log_page) + (threadIdx.x + k * blockDim.x) / NI;
+      if (j < start || j >= len) continue;
+      char* row = a.k_out.at(l, b, h, j - start);
+      *(uint4*)(row + it[k].va * 16) = x[k];
+      *(uint4*)(row + it[k].vb * 16) = y[k];
+    }
+  }
   if (whole) {
     uint32_t top = 0;
 #pragma unroll

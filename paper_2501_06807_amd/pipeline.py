@@ -1,4 +1,4 @@
-"""Preallocated prefill + decode path over the C-ABI entry points."""
+"""Preallocated prefill + decode paths over the C-ABI entry points: the kept cache of the method, and a paged cache."""
 import ctypes
 import math
 
@@ -152,3 +152,123 @@ class MPCachePath:
         L._check("mpc_decode_step",
                  self._step_fn(*self._step_args, ctypes.c_void_p(q.data_ptr()), *self._step_tail, st))
         return self.out
+
+
+class PagedPath:
+    """Serving from a paged cache over mpc_paged_append, mpc_paged_attn and mpc_prompt_attn: a batch of `batch` sequences of
+    up to `max_rows` rows each, all layers of the block per call, the pages drawn from one pool as the sequences grow.
+
+    prefill() starts every sequence with a prompt, extend() adds tokens to them (one each, drafted ones, or a chunk of a
+    prompt) and attends over the cache, take_back() drops the newest rows again (rejected drafts), and adopt() starts the
+    sequences with the rows that a MPCachePath kept. fp8: pages of e4m3 codes with a scale for each page and head.
+    window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
+    (cos, sin); None where q and k arrive rotated."""
+
+    def __init__(self, *, n_layers, batch, n_q_heads, n_kv_heads, head_dim, dtype, max_rows, page_size=64, n_pages=None,
+                 fp8=True, window=0, sinks=0, rope=None, rope_style="interleaved", sm_scale=None, device="cuda"):
+        self.Hq, self.window, self.sinks, self.rope, self.rope_style = n_q_heads, window, sinks, rope, rope_style
+        self.sm_scale = 1.0 / math.sqrt(head_dim) if sm_scale is None else sm_scale
+        max_pages = -(-max_rows // page_size)
+        n_pages = batch * max_pages if n_pages is None else n_pages
+        self.kv = L.paged_kv(n_layers=n_layers, batch=batch, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype,
+                             n_pages=n_pages, max_pages=max_pages, page_size=page_size, fp8=fp8, device=device)
+        self.pos = torch.zeros(batch, dtype=torch.int32, device=self.kv.device)  # position of each sequence's next token
+        self.rows = [0] * batch  # the lengths again, on the host
+        self._pages = [[] for _ in range(batch)]
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._ws = {}
+
+    def _ints(self, x):
+        return torch.tensor(x, dtype=torch.int32, device=self.kv.device)
+
+    def clear(self):
+        """Empties every sequence; the pages go back to the pool."""
+        for b, pages in enumerate(self._pages):
+            self._free += pages[::-1]
+            self._pages[b] = []
+        self.rows = [0] * self.kv.B
+        self.kv.table.fill_(-1)
+        self.kv.lens.zero_()
+        self.pos.zero_()
+
+    def reserve(self, rows):
+        """Pages for rows[b] rows of each sequence, for steps that are replayed from a graph; extend() does it by itself."""
+        page, M = self.kv.page, self.kv.table.shape[1]
+        want = [max(0, -(-r // page) - len(p)) for r, p in zip(rows, self._pages)]
+        if any(r > M * page for r in rows):
+            raise ValueError(f"a sequence of more than {M * page} rows")
+        if sum(want) > len(self._free):
+            raise ValueError(f"{sum(want)} pages wanted, {len(self._free)} free")
+        if sum(want) == 0:
+            return
+        for b, n in enumerate(want):
+            self._pages[b] += [self._free.pop() for _ in range(n)]
+        self.kv.table.copy_(self._ints([p + [-1] * (M - len(p)) for p in self._pages]))
+
+    def step(self, q, k, v, n_valid=None, out=None, lse=None):
+        """The device's part of extend(), which can be captured as a HIP graph: rotates, appends and attends, for sequences
+        whose pages are reserved. q becomes rotated in place."""
+        n = q.shape[3] if q.dim() == 5 else 1
+        self.kv.lens.add_(n if n_valid is None else n_valid)
+        L.mpc_paged_append(k, v, self.kv, q=q if self.rope is not None else None, rope=self.rope, rope_style=self.rope_style,
+                           pos0=self.pos, n_valid=n_valid)
+        self.pos.add_(n if n_valid is None else n_valid)
+        out = torch.zeros_like(q) if out is None else out
+        key = (n, q.shape[2])
+        if key not in self._ws:
+            self._ws[key] = L.workspace(L.paged_attn_workspace_bytes(q, self.kv), self.kv.device)
+        L.mpc_paged_attn(q, self.kv, out, sm_scale=self.sm_scale, window=self.window, sinks=self.sinks, n_valid=n_valid,
+                         lse=lse, ws=self._ws[key])
+        return out
+
+    def extend(self, q, k, v, new=None, out=None, lse=None):
+        """Adds the tokens q [L][B][Hq][n][d], k, v [L][B][Hkv][n][d] (new[b] of sequence b, n by default) and returns their
+        attention over the cache, shaped like q."""
+        n = q.shape[3] if q.dim() == 5 else 1
+        self.grown([n] * self.kv.B if new is None else new)
+        return self.step(q, k, v, None if new is None else self._ints(new), out, lse)
+
+    def grown(self, new):
+        """Books new[b] rows of each sequence on the host and reserves their pages (before the step, or the replays of one)."""
+        rows = [r + n for r, n in zip(self.rows, new)]
+        self.reserve(rows)
+        self.rows = rows
+
+    def take_back(self, dropped):
+        """Drops the newest dropped[b] rows of each sequence (with 8-bit pages at most a page each: their rows are still in
+        the tail); the pages stay reserved."""
+        if any(d < 0 or d > r or (self.kv.k_scale is not None and d > self.kv.page) for d, r in zip(dropped, self.rows)):
+            raise ValueError("more rows than the sequence has, or than its tail keeps")
+        d = self._ints(dropped)
+        self.rows = [r - x for r, x in zip(self.rows, dropped)]
+        self.kv.lens.sub_(d)
+        self.pos.sub_(d)
+
+    def prefill(self, q, k, v, lens=None, out=None, lse=None):
+        """Starts every sequence with its prompt, q [L][B][Hq][T][d], k, v [L][B][Hkv][T][d] (lens[b] tokens of sequence b, T by
+        default): the rows go into the cache, and the attention of the prompt's rows among themselves is returned. q
+        becomes rotated in place."""
+        self.clear()
+        T = q.shape[3]
+        new = [T] * self.kv.B if lens is None else list(lens)
+        self.grown(new)
+        n = None if lens is None else self._ints(new)
+        self.kv.lens.copy_(self._ints(new))
+        turned = torch.empty_like(k) if self.rope is not None else None
+        L.mpc_paged_append(k, v, self.kv, q=q if self.rope is not None else None, k_out=turned, rope=self.rope,
+                           rope_style=self.rope_style, pos0=self.pos, n_valid=n)
+        self.pos.add_(self.kv.lens)
+        out = torch.zeros_like(q) if out is None else out
+        L.mpc_prompt_attn(q, k if turned is None else turned, v, out, sm_scale=self.sm_scale, window=self.window,
+                          sinks=self.sinks, q_lens=n, k_lens=n, lse=lse)
+        return out
+
+    def adopt(self, path, position):
+        """Starts every sequence with the rows that `path` (a MPCachePath of the same shape) keeps, as they are: its evicted
+        prompt and what was appended to it. `position`: that of the next token."""
+        self.clear()
+        n = path.Ts + path.n_tail
+        self.grown([n] * self.kv.B)
+        self.kv.lens.fill_(n)
+        L.mpc_paged_append(path.k_s[:, :, :, :n], path.v_s[:, :, :, :n], self.kv)
+        self.pos.fill_(position)

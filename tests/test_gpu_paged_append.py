@@ -268,3 +268,28 @@ def test_pool_beyond_four_gib():
         bo, bl = R.bounds(q[0, 0, h].double(), *rows, idx, w, o, ls, d ** -0.5, torch.bfloat16)
         R.check(out[0, 0, h].cpu(), o, bo, f"out {h}")
         R.check(lse[0, 0, h, 0].cpu(), ls, bl, f"lse {h}")
+
+
+@pytest.mark.parametrize("dtype,fp8,page", [("bf16", False, 16), ("bf16", True, 32), ("fp32", True, 16), ("fp16", True, 256)])
+def test_rotated_keys_are_returned_too(dtype, fp8, page):
+    """k_out holds K's rows as the cache takes them, of every token that becomes a row, and nothing else."""
+    import paper_2501_06807_amd as M
+    L, B, H, d, n = 2, 3, 2, 64, 75
+    kv = make(M, L, B, H, d, dtype, page, cap=-(-60 // page), fp8=fp8)
+    cap = kv.table.shape[1] * page
+    lens, new = [min(75, cap), 3, cap + 5], [75, 2, 10]  # ten rows, five of them behind the table's end
+    kv.lens.copy_(torch.tensor(lens))
+    k, v = tokens((L, B, H, n, d), dtype, 1).cuda(), tokens((L, B, H, n, d), dtype, 2).cuda()
+    k_out = torch.full((B, n, L, H, d), 7.0, dtype=DT[dtype], device="cuda").permute(2, 0, 3, 1, 4)
+    rope = R.rope_table(400, d)
+    M.mpc_paged_append(k, v, kv, k_out=k_out, rope=rope.cuda(), rope_style="half",
+                       n_valid=torch.tensor(new, dtype=torch.int32, device="cuda"))
+    got = k_out.cpu()
+    for b in range(B):
+        for t in range(n):
+            j = lens[b] - new[b] + t
+            if t >= new[b] or not 0 <= j < cap:
+                assert bool((got[:, b, :, t] == 7.0).all()), (b, t)
+                continue
+            want, mag = R.rotated(k[:, b, :, t].cpu().double(), rope, "half", j)
+            R.check(got[:, b, :, t], want, R.half_step(DT[dtype]) * want.abs() + 4 * R.U32 * mag + 2.0 ** -25, f"{b} {t}")

@@ -27,10 +27,10 @@ def ref(x):
     return None if x is None else ctypes.byref(x)
 
 
-def append(d=None, kv=None, n=1, r=None, k=FAKE, ks=None, v=FAKE, q=None, q_out=None, os_=None, no_kv=False):
+def append(d=None, kv=None, n=1, r=None, k=FAKE, ks=None, v=FAKE, q=None, q_out=None, os_=None, no_kv=False, k_out=None, ko=None):
     lib = L.lib()
     s = lib.mpc_paged_append(ref(d or dims()), None if no_kv else ref(kv or cache()), n, None, ref(r), None, k, ref(ks), v, None, q,
-                             None, q_out, ref(os_), None)
+                             None, q_out, ref(os_), k_out, ref(ko), None)
     return s, lib.mpc_last_error().decode()
 
 
@@ -80,6 +80,8 @@ def test_caches(call, kv, expect):
     (dict(r=rope(table=(1 << 20) + 8)), L.MPC_EINVAL),
     (dict(ks=L.MpcStrides(-8, 1024, 128, 128)), L.MPC_EINVAL), (dict(ks=L.MpcStrides(4096, 1024, 132, 128)), L.MPC_EINVAL),
     (dict(ks=L.MpcStrides(1 << 60, 1024, 128, 128)), L.MPC_EINVAL),
+    (dict(k_out=FAKE), L.MPC_EINVAL), (dict(k_out=ODD), L.MPC_EINVAL),  # k itself, and off its alignment
+    (dict(k_out=ctypes.c_void_p(1 << 22), ko=L.MpcStrides(4096, 1024, 0, 128)), L.MPC_ESHAPE),
     # rows that are written may not lie on each other: heads a half row apart, sequences on one place
     (dict(q=FAKE, q_out=FAKE, r=rope(), os_=L.MpcStrides(4096, 1024, 64, 128)), L.MPC_ESHAPE),
     (dict(q=FAKE, q_out=FAKE, r=rope(), os_=L.MpcStrides(4096, 0, 128, 128)), L.MPC_ESHAPE),
