@@ -56,7 +56,6 @@ struct AttnArgs {
 // Waves of a workgroup of the paged attention: eight where a wave may take half of a SIMD's registers, four where it takes
 // all of them.
 __host__ __device__ constexpr int paged_waves(int row_tiles) { return row_tiles == 1 ? 8 : 4; }
-constexpr unsigned kMinRun = 4;  // key blocks of a workgroup, at least
 
 struct PagedAttnArgs : AttnArgs {
   PagedCache c;

@@ -381,8 +381,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
   }
   total = __builtin_amdgcn_readfirstlane(total);
   if (total == 0) return;
-  // A run is at least kMinRun blocks: below that, joining parts takes longer than the blocks themselves.
-  const unsigned per = max((total + gridDim.x - 1) / gridDim.x, kMinRun);
+  const unsigned per = (total + gridDim.x - 1) / gridDim.x;
   if ((unsigned long long)blockIdx.x * per >= total) return;
   const unsigned first = blockIdx.x * per, last = min(first + per, total);
   // the sequence of the first block
