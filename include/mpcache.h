@@ -46,7 +46,8 @@
  *   - Apart from mpc_decode_step_status (a blocking read), no call allocates, sets memory, waits on
  *     the host or uses a stream other than `stream`. So calls can be captured into a HIP graph,
  *     whose replays rerun the same kernels on the same pointers and sizes.
- *   - Supported: d in {64, 128}; G in {1, 2, 4, 8}; dtype fp32 / fp16 / bf16.
+ *   - Supported: d in {64, 128}; G in {1, 2, 4, 8}; dtype fp32 / fp16 / bf16. The paged and prompt calls
+ *     read batch, n_layers, n_q_heads, n_kv_heads, head_dim and dtype of dims.
  */
 #ifndef MPCACHE_H
 #define MPCACHE_H
@@ -137,7 +138,8 @@ typedef struct {
   float *k_scale, *v_scale; /* [L][P][Hkv], MPC_PAGE_E4M3 only (else ignored, as the tails)         */
   void *k_tail, *v_tail;    /* [L][B][Hkv][2 * page_size][d], dtype                                 */
   const int32_t* table;     /* [B][M] page ids, the same for every layer                           */
-  const int32_t* lens;      /* [B] rows in the cache, those of the call's new tokens included      */
+  const int32_t* lens;      /* [B] rows in the cache, those of the call's new tokens included
+                             * (values are brought into [0, 2^30])                                 */
 } mpc_paged_kv;
 
 /* Rotary positions: table [n_pos][rot_dim / 2][2] of (cos, sin). HALF pairs channel i with channel
@@ -387,7 +389,10 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
  *   q, out [L][B][Hq][n_new][d] (strides; NULL: contiguous); lse [L][B][Hq][n_new] float or NULL.
  * fp32 scores, sums and accumulation; 16-bit types multiply weights rounded to 16 bits with the values.
  * ws: mpc_workspace_bytes(MPC_OP_PAGED_ATTN, dims, n_new, kv) bytes, zero-filled before its first use;
- * every completed call leaves it ready for the next (calls sharing it must not overlap). */
+ * every completed call leaves it ready for the next (calls sharing it must not overlap). The sizes of the
+ * cache, not the lengths, give the launch, so a captured call follows lengths and tables as they change.
+ * Limits: n_new * G <= 2^30, fewer than 2^31 blocks of 128 keys over all (sequence, layer, kv head)s and
+ * groups of 16 or 32 query rows. */
 mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                           const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, void* out,
                           const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);

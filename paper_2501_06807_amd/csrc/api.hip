@@ -179,6 +179,7 @@ mpc_status check_pages(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new)
   const int G = d->n_q_heads / d->n_kv_heads;
   if (G != 1 && G != 2 && G != 4 && G != 8) return fail(MPC_EUNSUPPORTED, "group size %d not in {1, 2, 4, 8}", G);
   if (n_new <= 0 || n_new > mpc::kMaxRows) return fail(MPC_EINVAL, "n_new %d not in [1, 2^30]", n_new);
+  if ((int64_t)n_new * G > mpc::kMaxRows) return fail(MPC_EUNSUPPORTED, "more than 2^30 query rows to a kv head");
   if (kv->n_pages <= 0 || kv->max_pages <= 0) return fail(MPC_EINVAL, "n_pages and max_pages must be positive");
   if (kv->format != MPC_PAGE_SAME && kv->format != MPC_PAGE_E4M3) return fail(MPC_EINVAL, "unknown page format %d", kv->format);
   const int p = kv->page_size;
@@ -917,7 +918,8 @@ mpc_status mpc_prompt_attn(const mpc_dims* dims, int32_t Tq, int32_t T, const in
   const int G = dims->n_q_heads / dims->n_kv_heads;
   if (G != 1 && G != 2 && G != 4 && G != 8) return fail(MPC_EUNSUPPORTED, "group size %d not in {1, 2, 4, 8}", G);
   if (Tq <= 0 || T <= 0) return fail(MPC_EINVAL, "Tq and T must be positive");
-  if (Tq > mpc::kMaxRows || T > mpc::kMaxRows) return fail(MPC_EUNSUPPORTED, "more than 2^30 rows");
+  if ((int64_t)Tq * G > mpc::kMaxRows || T > mpc::kMaxRows)
+    return fail(MPC_EUNSUPPORTED, "more than 2^30 keys, or query rows to a kv head");
   mpc::PromptAttnArgs a{};
   if ((s = attn_args(dims, cfg, Tq, q, q_strides, out, out_strides, lse, &a)) != MPC_OK) return s;
   if ((s = rows_of(dims, "k", k, k_strides, dims->n_kv_heads, T, false, &a.k)) != MPC_OK) return s;

@@ -20,7 +20,7 @@ PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int
   const int tile = dtype == MPC_FP32 ? 16 : 32;
   const long long nb = cap / (tile * paged_waves(p.row_tiles)) + 2;  // complete pages' tiles and the tail's may each be cut short
   const long long units = (long long)L * B * Hkv * p.groups;
-  p.blocks = units * nb;
+  p.blocks = (double)units * (double)nb >= 2147483648.0 ? 1ll << 31 : units * nb;
   p.grid = (int)std::min<long long>(kNumCU, p.blocks);
   p.cnt_bytes = ((size_t)units * sizeof(int) + 255) & ~(size_t)255;
   p.ws_bytes = p.cnt_bytes + (size_t)p.grid * 2 * p.part_rows * (D + 2) * sizeof(float);

@@ -174,6 +174,7 @@ class PagedPath:
                              n_pages=n_pages, max_pages=max_pages, page_size=page_size, fp8=fp8, device=device)
         self.pos = torch.zeros(batch, dtype=torch.int32, device=self.kv.device)  # position of each sequence's next token
         self.rows = [0] * batch  # the lengths again, on the host
+        self._kept = [0] * batch  # first row of each sequence that its tail still holds
         self._pages = [[] for _ in range(batch)]
         self._free = list(range(n_pages - 1, -1, -1))
         self._ws = {}
@@ -187,6 +188,7 @@ class PagedPath:
             self._free += pages[::-1]
             self._pages[b] = []
         self.rows = [0] * self.kv.B
+        self._kept = [0] * self.kv.B
         self.kv.table.fill_(-1)
         self.kv.lens.zero_()
         self.pos.zero_()
@@ -233,14 +235,19 @@ class PagedPath:
         rows = [r + n for r, n in zip(self.rows, new)]
         self.reserve(rows)
         self.rows = rows
+        page = self.kv.page
+        self._kept = [max(k, ((r - 1) // page - 1) * page) for k, r in zip(self._kept, rows)]
 
     def take_back(self, dropped):
-        """Drops the newest dropped[b] rows of each sequence (with 8-bit pages at most a page each: their rows are still in
-        the tail); the pages stay reserved."""
-        if any(d < 0 or d > r or (self.kv.k_scale is not None and d > self.kv.page) for d, r in zip(dropped, self.rows)):
-            raise ValueError("more rows than the sequence has, or than its tail keeps")
+        """Drops the newest dropped[b] rows of each sequence; the pages stay reserved. With 8-bit pages the page that a
+        sequence then ends in has to be in its tail still, which holds the last two pages that it ever reached: a page's
+        rows at least."""
+        page, rows = self.kv.page, [r - d for r, d in zip(self.rows, dropped)]
+        for r, d, kept in zip(rows, dropped, self._kept):
+            if d < 0 or r < 0 or (self.kv.k_scale is not None and r % page and r // page * page < kept):
+                raise ValueError("more rows than the sequence has, or than its tail keeps")
         d = self._ints(dropped)
-        self.rows = [r - x for r, x in zip(self.rows, dropped)]
+        self.rows = rows
         self.kv.lens.sub_(d)
         self.pos.sub_(d)
 

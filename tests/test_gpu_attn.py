@@ -116,6 +116,43 @@ def test_paged_attention_of_a_long_cache(dtype, fp8):
     check_paged(kv, q, out, lse, lens, [1, 1, 1], 4000, 5, d ** -0.5, dtype + " window", {(0, 0, 0), (1, 2, 1), (1, 1, 0)})
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_paged_attention_of_more_sequences_than_a_wave_has_lanes(fp8):
+    import paper_2501_06807_amd as M
+    B = 150
+    g = torch.Generator().manual_seed(4)
+    lens = torch.randint(0, 90, (B,), generator=g).tolist()
+    new = [min(n, 2) if b % 7 else 0 for b, n in enumerate(lens)]
+    kv = make(M, 2, B, 1, 64, "bf16", 16, cap=6, fp8=fp8)
+    fill(kv, lens, 3, "bf16")
+    q = tokens((2, B, 4, 2, 64), "bf16", 9, spread=False).cuda()
+    out, lse = run_paged(kv, q, new)
+    check_paged(kv, q, out, lse, lens, new, 0, 0, 0.125, "many", {(l, b, 0) for l in range(2) for b in range(0, B, 5)} | {(1, 149, 0), (0, 63, 0), (0, 64, 0)})
+
+
+@pytest.mark.parametrize("sm", [-0.2, 0.0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_scales_of_zero_and_below(sm, dtype):
+    import paper_2501_06807_amd as M
+    lens = [77, 5]
+    kv = make(M, 1, 2, 2, 64, dtype, 16, cap=5, fp8=dtype == "bf16")
+    fill(kv, lens, 3, dtype)
+    q = tokens((1, 2, 4, 3, 64), dtype, 9, spread=False).cuda()
+    out, lse = run_paged(kv, q, [3, 3], 20, 2, sm=sm)
+    check_paged(kv, q, out, lse, lens, [3, 3], 20, 2, sm, "scale")
+    T = 100
+    q, k, v = (tokens((1, 1, 2, T, 64), dtype, s, spread=False) for s in (1, 2, 3))
+    out, lse = torch.empty_like(q).cuda(), torch.empty(1, 1, 2, T, device="cuda")
+    M.mpc_prompt_attn(q.cuda(), k.cuda(), v.cuda(), out, sm_scale=sm, window=30, sinks=2, lse=lse)
+    for h in range(2):
+        for t in (0, 1, 31, 32, 99):
+            x, kd, vd = q[0, 0, h, t].double(), k[0, 0, h].double(), v[0, 0, h].double()
+            o, ls, idx, w = R.attend(x, kd, vd, t, sm, 30, 2)
+            bo, bl = R.bounds(x, kd, vd, idx, w, o, ls, sm, DT[dtype])
+            R.check(out[0, 0, h, t].cpu(), o, bo, f"h{h} t{t}")
+            R.check(lse[0, 0, h, t].cpu(), ls, bl, f"lse h{h} t{t}")
+
+
 def test_paged_scales_far_from_one():
     """Values of 2^-16 and 2^10 times the ordinary size, in 8-bit pages of each type: no range is lost on the way."""
     import paper_2501_06807_amd as M
@@ -252,6 +289,21 @@ def test_a_decode_loop_captured_once_follows_the_lengths():
     lens = [s + 20 for s in start]
     assert twins[0].lens.tolist() == lens
     check_paged(twins[0], qr, out, lse, lens, [1] * B, 0, 0, d ** -0.5, "graph")
+
+
+def test_single_tokens_without_their_axis():
+    """[L][B][H][d] tensors are taken as one token each, as the other decode calls take them."""
+    import paper_2501_06807_amd as M
+    kv = make(M, 2, 3, 2, 64, "bf16", 16, cap=3)
+    fill(kv, [20, 33, 48], 3, "bf16")
+    kv.lens.sub_(1)
+    k, v, q = (tokens((2, 3, h, 64), "bf16", s).cuda() for s, h in ((1, 2), (2, 2), (3, 8)))
+    kv.lens.add_(1)
+    M.mpc_paged_append(k, v, kv)
+    out, lse = torch.empty_like(q), torch.empty(2, 3, 8, device="cuda")
+    M.mpc_paged_attn(q, kv, out, sm_scale=0.125, lse=lse)
+    torch.cuda.synchronize()
+    check_paged(kv, q[:, :, :, None], out[:, :, :, None], lse[..., None], [20, 33, 48], [1] * 3, 0, 0, 0.125, "one")
 
 
 def prompt_case(dtype, L, B, Hq, Hkv, d, Tq, T, q_lens, k_lens, window, sinks, seed=0, rows=None, token_major=False):

@@ -74,8 +74,12 @@ def test_rejected_drafts_leave_the_cache_as_if_they_had_not_been():
         o = [p.extend(x[0].clone(), x[1], x[2]) for p in (a, b)]
         if i > 0:  # (the first of them was rotated in place above by the same step of each)
             assert torch.equal(bits(o[0]), bits(o[1])), i
-    with pytest.raises(ValueError):
-        a.take_back([17, 0, 0])
+    with pytest.raises(ValueError):  # the tail holds the last two pages: rows from 32 on
+        a.take_back([a.rows[0] - 31, 0, 0])
+    a.take_back([a.rows[0] - 33, 0, 0])
+    with pytest.raises(ValueError):  # also for a second time
+        a.take_back([2, 0, 0])
+    a.take_back([1, 0, 0])  # row 32 begins a page: nothing of it is needed
     with pytest.raises(ValueError):
         a.take_back([0, 0, -1])
 

@@ -116,3 +116,17 @@ def test_workspace_of_the_paged_attention():
     size = lambda d, n, kv: lib.mpc_workspace_bytes(L.MPC_OP_PAGED_ATTN, ref(d), n, ref(kv))  # noqa: E731
     assert size(dims(), 1, None) == 0 and size(dims(), 0, cache()) == 0 and size(dims(), 1, cache(page_size=8)) == 0
     assert size(None, 1, cache()) == 0
+    assert size(dims(), 1, cache()) > 0
+    huge = cache(max_pages=1 << 24, page_size=64)
+    assert size(dims(batch=1024), 1, huge) == 0  # more than 2^31 key blocks
+    assert paged(d=dims(batch=1024), kv=huge, ws_bytes=1 << 40)[0] == L.MPC_EUNSUPPORTED
+    need = size(dims(), 1, cache())
+    assert paged(ws_bytes=need - 1)[0] == L.MPC_EWORKSPACE and paged(ws=None, ws_bytes=need)[0] == L.MPC_EWORKSPACE
+    assert paged(ws=ODD, ws_bytes=need)[0] == L.MPC_EINVAL
+
+
+@pytest.mark.parametrize("n", [1 << 29, 1 << 30])
+def test_query_rows_beyond_the_limit(n):
+    assert paged(n=n, ws_bytes=1 << 60)[0] == L.MPC_EUNSUPPORTED  # four heads to a kv head
+    assert append(n=n)[0] == L.MPC_EUNSUPPORTED
+    assert prompt(Tq=n, T=5)[0] == L.MPC_EUNSUPPORTED
