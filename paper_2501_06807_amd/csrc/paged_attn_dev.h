@@ -10,8 +10,10 @@
 // query row and its weights are already the other operand of O^T += V^T P^T: no lane exchange but the row maximum's.
 // The contraction's places are bound to channels and keys so that every load is 8 or 16 bytes of a row; V's rows meet in
 // registers (byte permutes), and nothing passes through LDS until the waves' parts are joined.
-// Running maximum m, sum l and the accumulators are fp32. 16-bit types and codes multiply weights rounded to 16 bits
-// (codes: to bf16, with the page's scale in the weight, whose range they keep); fp32 multiplies in fp32.
+// Running maximum m, sum l and the accumulators are fp32. 16-bit types multiply weights rounded to them, half a step of a
+// weight as the output's own rounding is of it; fp32 multiplies in fp32. Codes widen exactly to either 16-bit type. A page's
+// value scale goes into a bf16 weight, whose range takes it; fp16 weights have no such range: they are lifted by 2^14, so
+// that only weights below 2^-28 of the largest lose bits, and the scale is applied to a tile's product in fp32.
 #pragma once
 #include "attn_mma.h"
 
@@ -35,8 +37,9 @@ struct PagedTile {
   // queries: 16-bit frags of 32 channels, or fp32 words of 4
   static constexpr int QF = F ? D / 4 : D / 32;
   using QFrag = std::conditional_t<F, float, uint4>;
-  // values multiply in this type
-  using PV = std::conditional_t<CODES && !F, BF16, DT>;
+  // fp16: exponents of the weights are lifted by this (also in the sum), and page scales applied to products
+  static constexpr bool H = DT::kCode == MPC_FP16;
+  static constexpr float LIFT = H ? 14.f : 0.f;
 
   // First channel of query fragment i of lane group g (fp32: of word i).
   __device__ static int q_channel(int i, int g) {
@@ -172,7 +175,7 @@ struct PagedWave {
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t) o[rt][t] *= move;
       }
-      const float base = m[rt] == -INFINITY ? 0.f : m[rt];
+      const float base = (m[rt] == -INFINITY ? 0.f : m[rt]) - TL::LIFT;
 #pragma unroll
       for (int j = 0; j < TL::VK; ++j) {
         const float w = fast_exp2(p[rt][j] - base);
@@ -192,10 +195,10 @@ struct PagedWave {
         for (int i = 0; i < TL::VW; ++i) {
           const uint32_t a = v[2 * p][i], b = v[2 * p + 1][i];
           const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05010400u), y = __builtin_amdgcn_perm(b, a, 0x07030602u);
-          w[4 * i][p] = widen2<BF16, false>(x);
-          w[4 * i + 1][p] = widen2<BF16, true>(x);
-          w[4 * i + 2][p] = widen2<BF16, false>(y);
-          w[4 * i + 3][p] = widen2<BF16, true>(y);
+          w[4 * i][p] = widen2<DT, false>(x);
+          w[4 * i + 1][p] = widen2<DT, true>(x);
+          w[4 * i + 2][p] = widen2<DT, false>(y);
+          w[4 * i + 3][p] = widen2<DT, true>(y);
         }
       } else {
 #pragma unroll
@@ -225,9 +228,10 @@ struct PagedWave {
   // o += V^T P^T. With `edge`: value rows that no row of the group sees do not enter (zero times what they hold might not
   // be zero), and values that are not finite in rows that only some see are added apart, to those. lo, hi: the
   // smallest and largest position of the group's rows.
-  template <class PV>
+  // scale: factors of the halves' products, or null.
   __device__ __forceinline__ void add_values(uint32_t (*w)[4], const float (*p)[TL::VK], const AttnArgs& a, bool edge, int k0,
-                                             int rows, const bool* have, int lo, int hi) {
+                                             int rows, const bool* have, int lo, int hi, const float* scale) {
+    using PV = DT;
     const int g = (threadIdx.x % kWave) / 16;
     if (edge) {
       bool bad = false;
@@ -269,8 +273,19 @@ struct PagedWave {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const uint4 x = packed<PV>(p[rt]);
+      if (!scale) {
 #pragma unroll
-      for (int t = 0; t < TL::NT; ++t) o[rt][t] = mma<PV>(words(w[t]), x, o[rt][t]);
+        for (int t = 0; t < TL::NT; ++t) o[rt][t] = mma<PV>(words(w[t]), x, o[rt][t]);
+      } else if (scale[0] == scale[1]) {
+#pragma unroll
+        for (int t = 0; t < TL::NT; ++t) o[rt][t] += mma<PV>(words(w[t]), x, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[0];
+      } else {  // two pages of 16 rows
+        const uint4 x0 = make_uint4(x.x, x.y, 0, 0), x1 = make_uint4(0, 0, x.z, x.w);
+#pragma unroll
+        for (int t = 0; t < TL::NT; ++t)
+          o[rt][t] += mma<PV>(words(w[t]), x0, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[0] +
+                      mma<PV>(words(w[t]), x1, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[1];
+      }
     }
   }
   __device__ static __forceinline__ uint4 words(const uint32_t* w) { return make_uint4(w[0], w[1], w[2], w[3]); }
@@ -280,7 +295,7 @@ struct PagedWave {
   }
   // The same in fp32.
   __device__ __forceinline__ void add_values(float (*x)[TL::NT], const float (*p)[TL::VK], const AttnArgs& a, bool edge, int k0,
-                                             int rows, const bool* have, int lo, int hi) {
+                                             int rows, const bool* have, int lo, int hi, const float*) {
     const int g = (threadIdx.x % kWave) / 16;
     if (edge) {
       bool bad = false;
@@ -532,16 +547,13 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         load_k(i1, next, k, ks);
         entries_of(after(i1), entry);
         float p[RT][TL::VK];
-        w.weights(sr, sc, CODES ? vf : nullptr, a, edge, k0, s.full, have, p);
+        w.weights(sr, sc, CODES && !TL::H ? vf : nullptr, a, edge, k0, s.full, have, p);
         Operand x;
         w.template operands<false>(v, x);
         load_v(i1, next, v, vs);
 #pragma unroll
         for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
-        if constexpr (TL::F)
-          w.add_values(x, p, a, edge, k0, s.full, have, lo, hi);
-        else
-          w.template add_values<typename TL::PV>(x, p, a, edge, k0, s.full, have, lo, hi);
+        w.add_values(x, p, a, edge, k0, s.full, have, lo, hi, CODES && TL::H ? vf : nullptr);
         if (i1 == i) break;
         i = i1;
       }
@@ -577,10 +589,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         w.weights(sr, sc, nullptr, a, true, k0, s.rows, have, p);
         Operand x;
         w.template operands<true>(vr, x);
-        if constexpr (TL::F)
-          w.add_values(x, p, a, true, k0, s.rows, have, lo, hi);
-        else
-          w.template add_values<DT>(x, p, a, true, k0, s.rows, have, lo, hi);
+        w.add_values(x, p, a, true, k0, s.rows, have, lo, hi, nullptr);
       }
     }
 
@@ -660,7 +669,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
           if (alone) {
             if (a.lse)
               a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
-                  Lsum[rt] == 0.f ? -INFINITY : (M[rt] + __log2f(Lsum[rt])) * 0.69314718055994531f;
+                  Lsum[rt] == 0.f ? -INFINITY : (M[rt] - TL::LIFT + __log2f(Lsum[rt])) * 0.69314718055994531f;
           } else {
             st_coherent2(part + r * (D + 2) + D, M[rt], Lsum[rt]);
           }
@@ -763,7 +772,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
             *(uint32_t*)out = pack2<DT>(x0, x1);
           if (e == 0 && a.lse)
             a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
-                sum == 0.f ? -INFINITY : (b0 + __log2f(sum)) * 0.69314718055994531f;
+                sum == 0.f ? -INFINITY : (b0 - TL::LIFT + __log2f(sum)) * 0.69314718055994531f;
         }
       }
     }

@@ -6,7 +6,8 @@
 // half of the row's lying 32 lanes on, and its weights, packed to 16 bits, are the operand of O^T += V^T P^T as they
 // stand; V comes from LDS through the transposing reads of gfx950 (four keys of one channel to a lane).
 // The row's reference (what its exponents are taken against) moves only when a score passes it by 2^8, so that the
-// accumulators are seldom rescaled; weights are at most 2^8, their sum and the accumulators fp32.
+// accumulators are seldom rescaled; weights are at most 2^8 (fp16: 2^15, lifted so that only those below 2^-21 of the
+// reference lose bits), their sum and the accumulators fp32.
 #include "attn_mma.h"
 
 namespace mpc {
@@ -78,6 +79,7 @@ template <class DT, int D, int NS>
 __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   constexpr int KT = 32, KB = KT / 32;  // keys of a tile, and its 32-key blocks
   constexpr int CH = D / 8, KSTEPS = D / 16, DB = D / 32, THREADS = 256;
+  constexpr float LIFT = DT::kCode == MPC_FP16 ? 7.f : 0.f;  // of the weights' exponents, also in their sum
   constexpr int PER = KT * CH / THREADS;  // chunks of K (and of V) that a thread stages
   __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
   __shared__ int s_bad[NS][2];  // the last round whose values, staged for an edge, were not all finite
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= move;
     }
-    const float base = ref == -INFINITY ? 0.f : ref;
+    const float base = (ref == -INFINITY ? 0.f : ref) - LIFT;
     uint32_t p[KB][8];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     }
   if (a.lse && hl == 0)
     a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
-        sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * 0.69314718055994531f;
+        sum == 0.f ? -INFINITY : (ref - LIFT + __log2f(sum)) * 0.69314718055994531f;
 }
 
 template <class DT, int D>

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kFp32Waves* kWave, RT == 1 ? 2 : 1) void k_prompt_f
       w.weights(s, sc, nullptr, a, edge, k0, rows, have, p);
       float x[TL::VK][NT];
       w.template operands<false>(v, x);
-      w.add_values(x, p, a, edge, k0, rows, have, lo, hi);
+      w.add_values(x, p, a, edge, k0, rows, have, lo, hi, nullptr);
       load_v(i1, v);
       if (i1 == i) break;
       i = i1;

@@ -71,7 +71,7 @@ def attend(q, k, v, pos, sm, window, sinks, has=None):
 def bounds(q, k, v, idx, w, out, lse, sm, dtype):
     """Largest errors of out [d] and lse that the kernels' roundings allow. Scores: fp32 products and sums of d terms in
     any order, the scale and the exponent's own rounding; weights: exp2 of one step, their sum over the keys in fp32, and
-    for 16-bit types one rounding of each weight to at most bf16 (2^-8); out: one rounding to its type."""
+    for 16-bit types one rounding of each weight to the type; out: one rounding to its type."""
     if w is None or idx.numel() == 0:
         return torch.zeros_like(out), 0.0
     d = q.numel()
@@ -79,7 +79,7 @@ def bounds(q, k, v, idx, w, out, lse, sm, dtype):
     ds = (d + 8) * U32 * top + 4 * U32
     n = idx.numel()
     rel = 2 * ds + (n + 16) * U32
-    weight = half_step(torch.bfloat16) if dtype != torch.float32 else 0.0
+    weight = half_step(dtype) if dtype != torch.float32 else 0.0
     spread = w @ v[idx].abs()
     tiny = 2.0 ** -24 if dtype == torch.float16 else 0.0  # fp16 below its normal range
     return (2 * rel + weight) * spread + half_step(dtype) * out.abs() + tiny, 2 * ds + (n + 16) * U32 + 4 * U32 * abs(lse)

@@ -116,6 +116,36 @@ def test_paged_attention_of_a_long_cache(dtype, fp8):
     check_paged(kv, q, out, lse, lens, [1, 1, 1], 4000, 5, d ** -0.5, dtype + " window", {(0, 0, 0), (1, 2, 1), (1, 1, 0)})
 
 
+@pytest.mark.parametrize("dtype,fp8", [("fp16", False), ("fp16", True), ("bf16", False), ("bf16", True)])
+def test_small_weights_of_large_values(dtype, fp8):
+    """One key in a page of its own has a weight of 2^-14 to 2^-22 of the largest and a value 2^15 times theirs."""
+    import paper_2501_06807_amd as M
+    d, page, T = 64, 16, 64
+    k = torch.zeros(1, 1, 1, T, d)
+    k[..., 0] = 4 + 0.001 * torch.arange(T)
+    v = tokens((1, 1, 1, T, d), dtype, 2, spread=False).float()
+    q = torch.zeros(1, 1, 2, 1, d)
+    q[..., 0] = torch.tensor([1.0, 1.5])[None, None, :, None]
+    k[0, 0, 0, 20, 0] = -6.0
+    v[0, 0, 0, 16:32] = 0
+    v[0, 0, 0, 20] = 30000.0
+    k, v, q = (x.to(DT[dtype]) for x in (k, v, q))
+    kv = make(M, 1, 1, 1, d, dtype, page, cap=5, fp8=fp8)
+    kv.lens.fill_(T)
+    M.mpc_paged_append(k.cuda(), v.cuda(), kv)
+    out, lse = run_paged(kv, q.cuda(), [1], sm=1.0)
+    check_paged(kv, q.cuda(), out, lse, [T], [1], 0, 0, 1.0, f"{dtype} {fp8}")
+    po, pl = torch.empty_like(q).cuda(), torch.empty(1, 1, 2, 1, device="cuda")
+    M.mpc_prompt_attn(q.cuda(), k.cuda(), v.cuda(), po, sm_scale=1.0, lse=pl)
+    for h in range(2):
+        x, kd, vd = q[0, 0, h, 0].double(), k[0, 0, 0].double(), v[0, 0, 0].double()
+        o, ls, idx, w = R.attend(x, kd, vd, T - 1, 1.0, 0, 0)
+        assert 2.0 ** -22 < float(w[20] / w.max()) < 2.0 ** -14
+        bo, bl = R.bounds(x, kd, vd, idx, w, o, ls, 1.0, DT[dtype])
+        R.check(po[0, 0, h, 0].cpu(), o, bo, f"prompt h{h}")
+        R.check(pl[0, 0, h, 0].cpu(), ls, bl, f"prompt lse h{h}")
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_paged_attention_of_more_sequences_than_a_wave_has_lanes(fp8):
     import paper_2501_06807_amd as M
