@@ -1,9 +1,17 @@
 // Append of new tokens to a paged cache with the rotation of their positions.
 //
-// A row's channels are handled in pairs of 16-byte vectors, so that a thread holds both partners of every channel
-// pair it rotates (vectors i and i + half the rotated ones), reads and writes each once, and may write in place.
-// Every product and sum of the rotation is rounded on its own (no fused multiply-add), so that the rows, and with
-// them the codes of a page, do not depend on how the compiler groups them.
+// y0 = x0 c - x1 s, y1 = x0 s + x1 c for each channel pair; then rows to rows (queries, pages of the element type) or a page's
+// rows to its scale 2^e (the least with amax <= 448 2^e) and codes. A row's channels are handled in pairs of 16-byte
+// vectors, so that a thread holds both partners of every channel pair it rotates (vectors i and i + half the rotated ones),
+// reads and writes each once, and may write in place. Every product and sum of the rotation is rounded on its own (no
+// fused multiply-add), so that the rows, and with them the codes of a page, do not depend on how the compiler groups them.
+//
+// Memory bounds it: 32K tokens of 2 layers (32 query heads, 8 kv heads, d 128, fp16) into 8-bit pages 310 us, 4.8 TB/s of the
+// bytes it has to move; four prompts of up to 8K tokens (32 heads, bf16) into 16-bit pages 218 us, 5.2 TB/s (a plain copy of
+// the queries alone: 5.4). The angles are the second stream: a row of the rotary table is as large as a row of both
+// types, so a thread reads it once for four heads, and the heads of a token run side by side (each head by itself: 719 us
+// of the first case). One token of one layer takes 5.6 us, a chain of memory round trips (lengths, angles, rows).
+// Work items in contiguous ranges per die cost 15% of the second case, and were not kept.
 #include "attn_mma.h"
 
 namespace mpc {
