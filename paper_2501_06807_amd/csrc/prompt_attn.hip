@@ -96,12 +96,13 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int G = a.Hq / a.Hkv;
 
-  // item: (layer, sequence, kv head), then the blocks of rows from the last one on, then the heads of the group
+  // item: (kv head, layer, sequence), then the blocks of rows from the last one on, then the heads of the group; so the dies
+  // divide the heads, and sequences of different lengths fall to all of them
   const unsigned id = by_die(blockIdx.x, gridDim.x);
   const unsigned nqb = (a.n + kRowsGroup - 1) / kRowsGroup;
   const int gq = id % G, qb = nqb - 1 - id / G % nqb;
   const unsigned u = id / G / nqb;
-  const int h = u % a.Hkv, b = u / a.Hkv % a.B, l = u / a.Hkv / a.B, hq = h * G + gq;
+  const int b = u % a.B, l = u / a.B % a.L, h = u / a.B / a.L, hq = h * G + gq;
   const int q_len = a.q_lens ? min(max(load_uniform(a.q_lens + b), 0), a.n) : a.n;
   const int rows = a.k_lens ? min(max(load_uniform(a.k_lens + b), 0), a.T) : a.T;
   if (qb * kRowsGroup >= q_len) return;
