@@ -9,13 +9,14 @@
 // accumulators are seldom rescaled; weights are at most 2^8 (fp16: 2^15, lifted so that only those below 2^-21 of the
 // reference lose bits), their sum and the accumulators fp32.
 //
-// 8K rows and keys of 32 heads of 128 in bf16: 628 us, 875 TFLOP/s of the products that the rows need (a large bf16 product
+// 8K rows and keys of 32 heads of 128 in bf16: 638 us, 862 TFLOP/s of the products that the rows need (a large bf16 product
 // of the library: 1229). The matrix unit is busy 41% of the cycles, the vector unit as much (a quarter of it exponentials),
-// at 1.7 to 2 GHz; both units side by side, in a written-out pipeline that took the next tile's scores beside this one's
-// weights, saved 5% of the cycles and no time, the clock falling with them. 32-key tiles instead of 64 (which spill):
-// 1072 -> 730 us; whole tiles apart from edge tiles, and the values asked for before the scores: 640. A window of 1024 over
-// four prompts of up to 16K: 1376 us; a block of 128 rows visits 37 tiles for 32 full ones' worth of keys, 11 of them
-// with masks (one check of the staged values instead of one of every fragment took it from 2130).
+// at 1.7 to 2 GHz. Both units side by side, in a written-out pipeline that takes the next tile's scores beside this one's
+// weights, gave 2% there and cost 4% behind a window: the clock falls as the units fill. 32-key tiles instead of 64 (which
+// spill): 1072 -> 730 us; whole tiles apart from edge tiles, and the values asked for before the scores: 640. A window of
+// 1024 over four prompts of up to 16K: 1045 us; a block of 128 rows visits 37 tiles for 32 full ones' worth of keys, 11 of
+// them with masks (one check of the staged values instead of one of every fragment, 2130 -> 1383; the dies dividing the heads
+// instead of the sequences, 1376 -> 1078).
 #include "attn_mma.h"
 
 namespace mpc {
@@ -174,8 +175,8 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     for (int n = 0; n < PER; ++n) top = max_magnitude(max_magnitude(max_magnitude(max_magnitude(top, vr[n].x), vr[n].y), vr[n].z), vr[n].w);
     return not_finite<DT>(top);
   };
-  // One tile; EDGE: some row of the wave may not see some key of it, and `bad` says that its values are not all finite.
-  auto tile = [&](auto edge, int k0, int buf, bool bad) {
+  // The tile of round n; EDGE: some row of the wave may not see some key of it.
+  auto tile = [&](auto edge, int k0, int buf, int n) {
     constexpr bool EDGE = decltype(edge)::value;
     const uint4* sk = s_k[grp][buf];
     const char* sv = (const char*)s_v[grp][buf];
@@ -195,6 +196,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
           v[d][2 * e + 1] = y.y;
         }
     };
+    const int bad = EDGE ? s_bad[grp][buf] : 0;
     uint4 kf[KB][KSTEPS];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -228,13 +230,21 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
       }
       if (a.window && k0 <= hi - a.window && k0 + KT > a.sinks) {
         const int gone = pos - a.window - j0, sinks = a.sinks - j0;
+        if (k0 < a.sinks) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
-            if (j <= gone && j >= sinks) s[kb][r] = -INFINITY;
-          }
+            for (int r = 0; r < 16; ++r) {
+              const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+              if (j <= gone && j >= sinks) s[kb][r] = -INFINITY;
+            }
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (32 * kb + 8 * (r >> 2) + (r & 3) <= gone) s[kb][r] = -INFINITY;
+        }
       }
     }
     float top = -INFINITY;
@@ -274,7 +284,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
         if constexpr (EDGE) {
           // Values that are not finite, in keys that some row does not see, must not meet that row's weight of zero: they
           // are added apart, to the rows that see them
-          if (bad) {
+          if (__builtin_amdgcn_readfirstlane(bad) == n) {
             const int j0 = k0 + 32 * kb + 16 * st + 4 * hl;
             float one[8];
 #pragma unroll
@@ -319,7 +329,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
     if (i >= tl.n || hi < lo) return;
     const int k0 = tl.id(i) * KT;
     if (EDGE && !seen_by(a, k0, k0 + KT - 1, lo, hi, rows)) return;
-    tile(edge, k0, buf, EDGE && __builtin_amdgcn_readfirstlane(s_bad[grp][buf]) == n);
+    tile(edge, k0, buf, n);
   };
   for (int n = 0; n < edges; ++n) round(std::true_type{}, n);
   for (int n = edges; n < rounds; ++n) round(std::false_type{}, n);
