@@ -106,6 +106,12 @@ struct PagedWave {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) s[rt][h] = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (F) {
+        // four chains of products, one for each word of a row's piece: a chain's sum is rounded at every step of it
+        f32x4 y[RT][4];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < (TAIL ? TL::KLT : TL::KL); ++i) {
           const uint32_t w[4] = {k[h][i].x, k[h][i].y, k[h][i].z, k[h][i].w};
@@ -117,13 +123,15 @@ struct PagedWave {
 #pragma unroll
               for (int n = 0; n < 4; ++n)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][h] = mma(x[n], q[rt][16 * i + 4 * e + n], s[rt][h]);
+                for (int rt = 0; rt < RT; ++rt) y[rt][e] = mma(x[n], q[rt][16 * i + 4 * e + n], y[rt][e]);
             } else {
 #pragma unroll
-              for (int rt = 0; rt < RT; ++rt) s[rt][h] = mma(__uint_as_float(w[e]), q[rt][4 * i + e], s[rt][h]);
+              for (int rt = 0; rt < RT; ++rt) y[rt][e] = mma(__uint_as_float(w[e]), q[rt][4 * i + e], y[rt][e]);
             }
           }
         }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][h] = (y[rt][0] + y[rt][1]) + (y[rt][2] + y[rt][3]);
       } else if constexpr (CODES && !TAIL) {
 #pragma unroll
         for (int i = 0; i < TL::KL; ++i) {
