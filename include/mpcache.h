@@ -387,7 +387,8 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
  * NaN or +infinity among the scores that a row sees makes its out and lse NaN. Nothing that a row does not
  * see reaches it, whatever it holds. Rows from n_valid[b] on are left as they were.
  *   q, out [L][B][Hq][n_new][d] (strides; NULL: contiguous); lse [L][B][Hq][n_new] float or NULL.
- * fp32 scores, sums and accumulation; 16-bit types multiply weights rounded to 16 bits with the values.
+ * fp32 scores, sums and accumulation; 16-bit types multiply each weight with the values in two parts of
+ * their type (its rounding and that of the rest).
  * ws: mpc_workspace_bytes(MPC_OP_PAGED_ATTN, dims, n_new, kv) bytes, zero-filled before its first use;
  * every completed call leaves it ready for the next (calls sharing it must not overlap). The sizes of the
  * cache, not the lengths, give the launch, so a captured call follows lengths and tables as they change.
@@ -400,7 +401,8 @@ mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
 /* The same attention of a prompt's rows over its keys, in plain tensors: row t of sequence b stands at
  * position k_lens[b] - q_lens[b] + t and sees keys 0 <= j < k_lens[b] as cfg names them; q_lens / k_lens
  * [B] int32 (NULL: Tq / T each; values are brought into [0, Tq] / [0, T]). Rows from q_lens[b] on are left as
- * they were. Weights, empty rows and NaN as in mpc_paged_attn.
+ * they were. Scores, empty rows and NaN as in mpc_paged_attn; 16-bit types multiply weights rounded once to
+ * their type.
  *   q, out [L][B][Hq][Tq][d], k, v [L][B][Hkv][T][d] (strides; NULL: contiguous);
  *   lse [L][B][Hq][Tq] float or NULL. No workspace. */
 mpc_status mpc_prompt_attn(const mpc_dims* dims, int32_t Tq, int32_t T, const int32_t* q_lens, const int32_t* k_lens,

@@ -10,17 +10,20 @@
 // query row and its weights are already the other operand of O^T += V^T P^T: no lane exchange but the row maximum's.
 // The contraction's places are bound to channels and keys so that every load is 8 or 16 bytes of a row; V's rows meet in
 // registers (byte permutes), and nothing passes through LDS until the waves' parts are joined.
-// Running maximum m, sum l and the accumulators are fp32. 16-bit types multiply weights rounded to them, half a step of a
-// weight as the output's own rounding is of it; fp32 multiplies in fp32. Codes widen exactly to either 16-bit type. A page's
-// value scale goes into a bf16 weight, whose range takes it; fp16 weights have no such range: they are lifted by 2^14, so
-// that only weights below 2^-28 of the largest lose bits, and the scale is applied to a tile's product in fp32.
+// Running maximum m, sum l and the accumulators are fp32. 16-bit types multiply a weight in two parts of the type, its rounding
+// and that of the rest, which holds it to half a step of half a step; fp32 multiplies in fp32. The second product of each value
+// costs no time (the first case below 371 us with one part and with two, the second 61.6 and 61.0, the drafts 37.7 and 31.4: their kernel no
+// longer spills), and takes the outputs' error from 0.0018 to 0.0017 of their size, what rounding them to bf16 costs. Codes
+// widen exactly to either 16-bit type. A page's value scale goes into a bf16 weight, whose range takes it; fp16 weights have no
+// such range: they are lifted by 2^14, so that only weights below 2^-28 of the largest lose bits of their first part, and the
+// scale is applied to a tile's product in fp32.
 //
 // Reading K and V bounds it: 4 x 32K rows, 2 layers of 32 heads of 128 over 8-bit pages, 2.1 GB in 371 us (5.8 TB/s); one
 // sequence of 128K rows and 8 kv heads, 268 MB in 61 us, of which about 12 are not reading: the launch, the chain of
 // lengths, table entry and first rows (4), and the joins (4 to 8). In between the dies differ: their workgroups read at rates
 // 35% apart, so that the even division ends with the slowest (41 us on average, 48 on the last). Keys two tiles ahead instead
 // of one changed nothing (373 and 63 us), nor did runs of at least four blocks where there is enough work. 32 sequences of
-// four drafted tokens behind a window of 1024 (16-bit pages of 16 rows) take 37 us, 136 MB. A table entry or a
+// four drafted tokens behind a window of 1024 (16-bit pages of 16 rows) take 31 us, 136 MB. A table entry or a
 // scale read through the vector cache waits for every row in flight: the scalar cache took the first case from 426 to 365.
 #pragma once
 #include "attn_mma.h"
@@ -251,15 +254,15 @@ struct PagedWave {
   }
 
   // o += V^T P^T. With `edge`: value rows that no row of the group sees do not enter (zero times what they hold might not
-  // be zero), and values that are not finite in rows that only some see are added apart, to those. lo, hi: the
-  // smallest and largest position of the group's rows.
+  // be zero). Values that are not finite are added apart, to the rows that see them: a weight's second part may be zero, or
+  // below zero, and with `edge` some rows do not see them at all. (Codes hold no infinities, and a NaN needs no sign: those of
+  // tiles that every row sees stay where they are.) lo, hi: the smallest and largest position of the group's rows.
   // scale: factors of the halves' products, or null.
   __device__ __forceinline__ void add_values(uint32_t (*w)[4], const float (*p)[TL::VK], const AttnArgs& a, bool edge, int k0,
                                              int rows, const bool* have, int lo, int hi, const float* scale) {
     using PV = DT;
     const int g = (threadIdx.x % kWave) / 16;
     if (edge) {
-      bool bad = false;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         uint32_t keep = 0;
@@ -270,12 +273,16 @@ struct PagedWave {
           keep |= any ? 0xFFFFu << 16 * i : 0u;
         }
 #pragma unroll
-        for (int t = 0; t < TL::NT; ++t) {
-          w[t][n] &= keep;
-          bad |= not_finite<PV>(w[t][n]);
-        }
+        for (int t = 0; t < TL::NT; ++t) w[t][n] &= keep;
       }
-      if (lo != hi && __any(bad)) {
+    }
+    if (edge || !CODES) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int t = 0; t < TL::NT; ++t) top = max_magnitude(top, w[t][n]);
+      if (__any(not_finite<PV>(top))) {
         float one[RT][TL::VK];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -295,21 +302,28 @@ struct PagedWave {
         }
       }
     }
+    // A weight is multiplied in two parts of the type, itself rounded and the rest of that, rounded: it loses half a step of
+    // half a step (2^-16 in bf16), not the half step that the output's own rounding would have beside it.
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const uint4 x = packed<PV>(p[rt]);
+      float rest[TL::VK];
+      unpack<PV>(x, rest);
+#pragma unroll
+      for (int j = 0; j < TL::VK; ++j) rest[j] = p[rt][j] - rest[j];
+      const uint4 y = packed<PV>(rest);
       if (!scale) {
 #pragma unroll
-        for (int t = 0; t < TL::NT; ++t) o[rt][t] = mma<PV>(words(w[t]), x, o[rt][t]);
+        for (int t = 0; t < TL::NT; ++t) o[rt][t] = mma<PV>(words(w[t]), x, mma<PV>(words(w[t]), y, o[rt][t]));
       } else if (scale[0] == scale[1]) {
 #pragma unroll
-        for (int t = 0; t < TL::NT; ++t) o[rt][t] += mma<PV>(words(w[t]), x, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[0];
+        for (int t = 0; t < TL::NT; ++t) o[rt][t] += mma<PV>(words(w[t]), x, mma<PV>(words(w[t]), y, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[0];
       } else {  // two pages of 16 rows
-        const uint4 x0 = make_uint4(x.x, x.y, 0, 0), x1 = make_uint4(0, 0, x.z, x.w);
+        const uint4 x0 = make_uint4(x.x, x.y, 0, 0), x1 = make_uint4(0, 0, x.z, x.w), y0 = make_uint4(y.x, y.y, 0, 0), y1 = make_uint4(0, 0, y.z, y.w);
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t)
-          o[rt][t] += mma<PV>(words(w[t]), x0, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[0] +
-                      mma<PV>(words(w[t]), x1, f32x4{0.f, 0.f, 0.f, 0.f}) * scale[1];
+          o[rt][t] += mma<PV>(words(w[t]), x0, mma<PV>(words(w[t]), y0, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[0] +
+                      mma<PV>(words(w[t]), x1, mma<PV>(words(w[t]), y1, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[1];
       }
     }
   }

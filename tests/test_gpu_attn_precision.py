@@ -1,5 +1,5 @@
 """What the attentions' roundings cost, where it would show: scores far from zero that lie close together, and products of a
-score that are small beside others."""
+score that are small beside others, and weights of 16-bit types over values that cancel."""
 import math
 
 import pytest
@@ -102,3 +102,30 @@ def test_small_products_beside_a_large_one(form, d):
     bound = (0.12 * (d / 4 - 1) + 2) * step / 4
     assert bound < 0.7 * (want - 0.5)
     R.check(out.cpu(), torch.full_like(out.cpu(), want), bound, form)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("fp8,page", [(False, 16), (True, 16), (True, 64)])
+@pytest.mark.parametrize("n,window,sinks", [(1, 0, 0), (3, 0, 0), (5, 90, 3)])
+def test_weights_of_16_bit_caches_keep_twice_their_bits(dtype, fp8, page, n, window, sinks):
+    """Weights enter the product with the values in two parts of the type, what the first part leaves being rounded once
+    more: half a step of half a step each, beside the fp32 roundings (R.bounds without a 16-bit weight) and the output's
+    one rounding to the type. fp16 weights are lifted by 2^14, below which their second part keeps 2^-25 at least."""
+    import paper_2501_06807_amd as M
+    d, Hq, Hkv, lens = 128, 8, 2, [300, 77, 512]
+    kv = make(M, 1, 3, Hkv, d, dtype, page, cap=-(-512 // page), fp8=fp8)
+    fill(kv, lens, 21, dtype)
+    q = tokens((1, 3, Hq, n, d), dtype, 3, spread=False).cuda()
+    out, lse = run_paged(kv, q, [n] * 3, window, sinks)
+    sm, half = d ** -0.5, R.half_step(DT[dtype])
+    for b in range(3):
+        for h in range(Hkv):
+            k, v, _ = rows_of(kv, 0, b, h, lens[b])
+            for hq in range(4 * h, 4 * h + 4):
+                for t in range(n):
+                    x = q[0, b, hq, t].cpu().double()
+                    o, ls, idx, w = R.attend(x, k, v, lens[b] - n + t, sm, window, sinks)
+                    bo, _ = R.bounds(x, k, v, idx, w, o, ls, sm, torch.float32)
+                    spread = w @ v[idx].abs()
+                    tiny = 2.0 ** -24 + 2.0 ** -39 * v[idx].abs().sum(0) if dtype == "fp16" else 0.0
+                    R.check(out[0, b, hq, t].cpu(), o, bo + half * half * spread + half * o.abs() + tiny, f"b{b} h{hq} t{t}")
