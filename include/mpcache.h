@@ -390,7 +390,9 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
  * fp32 scores, sums and accumulation; 16-bit types multiply each weight with the values in two parts of
  * their type (its rounding and that of the rest).
  * ws: mpc_workspace_bytes(MPC_OP_PAGED_ATTN, dims, n_new, kv) bytes, zero-filled before its first use;
- * every completed call leaves it ready for the next (calls sharing it must not overlap). The sizes of the
+ * every completed call leaves it ready for the next, of this or any other dims, cache and n_new whose
+ * bytes it has (calls sharing it must not overlap). The bytes follow head_dim and n_new * G up to 32 only
+ * and never fall with either. The sizes of the
  * cache, not the lengths, give the launch, so a captured call follows lengths and tables as they change.
  * Limits: n_new * G <= 2^30, fewer than 2^31 blocks of 128 keys over all (sequence, layer, kv head)s and
  * groups of 16 or 32 query rows. */

@@ -525,7 +525,7 @@ def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse
     """Attention of the newest tokens' queries q [L][B][Hq][n][d] (or [L][B][Hq][d]) over the cache `kv`, which holds their
     keys and values already -> out (shaped like q), lse [L][B][Hq][n] float32. window, sinks: a row at position p sees
     the rows j <= p with j > p - window (0: all) or j < sinks. ws: from workspace(paged_attn_workspace_bytes(q, kv)),
-    reused by later calls of the same shape (made for the call by default)."""
+    reused by later calls of any shape that needs no more bytes (made for the call by default)."""
     qp, qs, shape = _rows(q, "q", kv.dtype)
     n = shape[3]
     _like(shape, kv, n, "q")

@@ -897,10 +897,9 @@ mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
     return fail(MPC_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, p.ws_bytes);
   if (!aligned16(ws)) return fail(MPC_EINVAL, "ws must be 16-byte aligned");
   a.cnt = (int*)ws;
-  a.part = (float*)((char*)ws + p.cnt_bytes);
+  a.part = (float*)((char*)ws + mpc::kPagedCntBytes);
   a.row_tiles = p.row_tiles;
   a.log_g = __builtin_ctz((unsigned)(dims->n_q_heads / dims->n_kv_heads));
-  a.groups = p.groups;
   a.part_rows = p.part_rows;
   a.grid = p.grid;
   clear_stale_error();

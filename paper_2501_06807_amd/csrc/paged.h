@@ -59,18 +59,20 @@ __host__ __device__ constexpr int paged_waves(int row_tiles) { return row_tiles 
 
 struct PagedAttnArgs : AttnArgs {
   PagedCache c;
-  int* cnt;       // arrivals of each unit, zero between launches
+  int* cnt;       // arrivals at a shared unit, by its first workgroup; zero between launches
   float* part;    // [grid][2][part_rows][D + 2]: accumulator, maximum and sum of a unit's part
   int row_tiles;  // 16-row tiles of a unit
   int log_g;      // G = 2^log_g
-  int groups;     // units of a kv head: its query rows over those of a unit
   int part_rows, grid;
 };
 struct PagedPlan {
-  int row_tiles, groups, part_rows, grid;
+  int row_tiles, part_rows, grid;
   long long blocks;  // at most, for sequences as long as the table
-  size_t cnt_bytes, ws_bytes;
+  size_t ws_bytes;   // counters, then parts
 };
+// Bytes of the arrival counters: a workgroup is the first one of at most one unit that others share (one that goes on behind
+// its run), so there is a counter to each, at the same place in every call.
+constexpr size_t kPagedCntBytes = kNumCU * sizeof(int);
 PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap);
 hipError_t launch_paged_attn_fp32(const PagedAttnArgs& a, int D, hipStream_t st);
 hipError_t launch_paged_attn_fp16(const PagedAttnArgs& a, int D, hipStream_t st);

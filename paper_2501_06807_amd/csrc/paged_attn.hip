@@ -15,15 +15,15 @@ PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int
   const long long rows = (long long)(Hq / Hkv) * n;
   p.row_tiles = rows > 16 ? 2 : 1;
   const int unit_rows = 16 * p.row_tiles;
-  p.groups = (int)((rows + unit_rows - 1) / unit_rows);
+  const long long groups = (rows + unit_rows - 1) / unit_rows;
   p.part_rows = (int)std::min<long long>(rows, unit_rows);
   const int tile = dtype == MPC_FP32 ? 16 : 32;
   const long long nb = cap / (tile * paged_waves(p.row_tiles)) + 2;  // complete pages' tiles and the tail's may each be cut short
-  const long long units = (long long)L * B * Hkv * p.groups;
+  const long long units = (long long)L * B * Hkv * groups;
   p.blocks = (double)units * (double)nb >= 2147483648.0 ? 1ll << 31 : units * nb;
   p.grid = (int)std::min<long long>(kNumCU, p.blocks);
-  p.cnt_bytes = ((size_t)units * sizeof(int) + 255) & ~(size_t)255;
-  p.ws_bytes = p.cnt_bytes + (size_t)p.grid * 2 * p.part_rows * (D + 2) * sizeof(float);
+  // for the largest grid, so that a workspace made for the most rows serves calls of fewer, and every cache
+  p.ws_bytes = kPagedCntBytes + (size_t)kNumCU * 2 * p.part_rows * (D + 2) * sizeof(float);
   return p;
 }
 

@@ -721,7 +721,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       const int share = __builtin_amdgcn_readfirstlane((int)(w1 - w0) + 1);
-      int* cnt = a.cnt + ((size_t)b * per_group + lh) * a.groups + rg;
+      int* cnt = a.cnt + w0;  // (no other shared unit starts in that workgroup's run)
       if (threadIdx.x == 0) {
         const int n = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = n == share - 1;
