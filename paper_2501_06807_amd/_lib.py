@@ -153,6 +153,15 @@ def workspace(nbytes, device="cuda"):
     return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _call_ws(nbytes, device, stream):
+    """The workspace of one call that was given none, made and cleared on the stream that the call runs on: the zeros come
+    before its kernels, and the memory goes back to the allocator in that stream's order."""
+    if stream is None:
+        return workspace(nbytes, device)
+    with torch.cuda.stream(stream):
+        return workspace(nbytes, device)
+
+
 def mpc_static_evict(q_win, k, v, kept_idx, k_out, v_out, *, keep, local_keep, sm_scale, causal=True,
                      layer0=0, share_period=1, share_start=2, token_score=None, row_lse=None, ws=None,
                      stream=None):
@@ -164,7 +173,7 @@ def mpc_static_evict(q_win, k, v, kept_idx, k_out, v_out, *, keep, local_keep, s
     cfg = MpcEvictCfg(window=W, keep=keep, local_keep=local_keep, sm_scale=sm_scale, causal=int(causal),
                       share_period=share_period, share_start=share_start)
     if ws is None:
-        ws = workspace(workspace_bytes(MPC_OP_STATIC_EVICT, dims, T, cfg), k.device)
+        ws = _call_ws(workspace_bytes(MPC_OP_STATIC_EVICT, dims, T, cfg), k.device, stream)
     _check("mpc_static_evict", lib().mpc_static_evict(
         ctypes.byref(dims), T, ctypes.byref(cfg), _ptr(q_win), _ptr(k), _ptr(v), _ptr(kept_idx), _ptr(k_out),
         _ptr(v_out), _ptr(token_score), _ptr(row_lse), _ptr(ws), ws.numel(), _stream(stream)))
@@ -254,7 +263,7 @@ def mpc_prefill(q_win, k, v, kept_idx, k_out, v_out, cent, scent, cfg, *, keep, 
     ecfg = MpcEvictCfg(window=W, keep=keep, local_keep=local_keep, sm_scale=sm_scale, causal=int(causal),
                        share_period=share_period, share_start=share_start)
     if ws is None:
-        ws = workspace(workspace_bytes(MPC_OP_STATIC_EVICT, dims, T, ecfg), k.device)
+        ws = _call_ws(workspace_bytes(MPC_OP_STATIC_EVICT, dims, T, ecfg), k.device, stream)
     _check("mpc_prefill", lib().mpc_prefill(
         ctypes.byref(dims), T, ctypes.byref(ecfg), ctypes.byref(cfg), _ptr(q_win), _ptr(k), _ptr(v), _ptr(kept_idx),
         _ptr(k_out), _ptr(v_out), _ptr(cent), _ptr(scent), _ptr(token_score), _ptr(row_lse), _ptr(ws), ws.numel(),
@@ -287,7 +296,7 @@ def mpc_sparse_decode_attn(q, k_cache, v_cache, sel, out, *, cluster_size, sm_sc
     dims = dims_of(q, k_cache, layer0)
     Ts = k_cache.shape[3] - n_tail if Ts is None else Ts
     if ws is None:
-        ws = workspace(workspace_bytes(MPC_OP_DECODE_ATTN, dims, Ts), q.device)
+        ws = _call_ws(workspace_bytes(MPC_OP_DECODE_ATTN, dims, Ts), q.device, stream)
     _check("mpc_sparse_decode_attn", lib().mpc_sparse_decode_attn(
         ctypes.byref(dims), Ts, n_tail, cluster_size, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(sel), sel.shape[2],
         sel.shape[-1], sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream)))
@@ -305,7 +314,7 @@ def mpc_decode_step(q, cent, scent, k_cache, v_cache, sel, out, cfg, *, sm_scale
     dims = dims_of(q, k_cache, layer0)
     Ts = k_cache.shape[3] - n_tail if Ts is None else Ts
     if ws is None:
-        ws = workspace(workspace_bytes(MPC_OP_DECODE_STEP, dims, Ts, cfg), q.device)
+        ws = _call_ws(workspace_bytes(MPC_OP_DECODE_STEP, dims, Ts, cfg), q.device, stream)
     _check("mpc_decode_step", lib().mpc_decode_step(
         ctypes.byref(dims), Ts, n_tail, ctypes.byref(cfg), _ptr(q), _ptr(cent), _ptr(scent), _ptr(k_cache), _ptr(v_cache),
         sm_scale, _ptr(sel), _ptr(sel_score), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream)))
@@ -532,7 +541,7 @@ def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse
     op, os_, oshape = _rows(out, "out", kv.dtype, shape[2])
     _like(oshape, kv, n, "out")
     if ws is None:
-        ws = workspace(paged_attn_workspace_bytes(q, kv), kv.device)
+        ws = _call_ws(paged_attn_workspace_bytes(q, kv), kv.device, stream)
     _contig(ws)
     st = _on(kv.device, stream, q, out, lse, ws)
     cfg = MpcAttnCfg(sm_scale, window, sinks)

@@ -1,4 +1,5 @@
-"""One workspace of the paged attention for calls of different shapes."""
+"""One workspace of the paged attention for calls of different shapes, and the one that a call makes for itself on another
+stream."""
 import pytest
 import torch
 
@@ -24,3 +25,23 @@ def test_one_workspace_for_calls_of_different_shapes():
         kv, q, new, want = calls[i]
         got = run_paged(kv, q, new, ws=ws)
         assert torch.equal(bits(got[0]), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1])), i
+
+
+def test_workspace_of_a_call_on_another_stream():
+    """A call without ws, on a stream that is not the current one: its workspace is made and cleared there."""
+    import paper_2501_06807_amd as M
+    kv = make(M, 1, 2, 2, 128, "bf16", 32, cap=100)
+    fill(kv, [3200, 2000], 3, "bf16")
+    q = tokens((1, 2, 8, 1, 128), "bf16", 5, spread=False).cuda()
+    want = run_paged(kv, q, [1, 1])
+    side = torch.cuda.Stream()
+    new = torch.tensor([1, 1], dtype=torch.int32, device="cuda")
+    outs = [torch.full_like(q, 7.0) for _ in range(8)]
+    torch.cuda.synchronize()
+    busy = torch.randn(4096, 4096, device="cuda")
+    for out in outs:
+        busy = busy @ busy * 1e-4  # what the current stream has before the zeros, if they were put there
+        M.mpc_paged_attn(q, kv, out, sm_scale=128 ** -0.5, n_valid=new, stream=side)
+    side.synchronize()
+    for out in outs:
+        assert torch.equal(bits(out), bits(want[0]))
