@@ -177,7 +177,10 @@ class PagedPath:
         self._kept = [0] * batch  # first row of each sequence that its tail still holds
         self._pages = [[] for _ in range(batch)]
         self._free = list(range(n_pages - 1, -1, -1))
-        self._ws = {}
+        # for steps of any number of tokens (the bytes do not grow beyond 32 query rows to a kv head), and cleared here, so
+        # that a step may be captured before one has run
+        size = lambda n: L.lib().mpc_workspace_bytes(L.MPC_OP_PAGED_ATTN, self.kv.dims(n_q_heads), n, self.kv.ref)  # noqa: E731
+        self.ws = L.workspace(max(size(1), size(32)), self.kv.device)
 
     def _ints(self, x):
         return torch.tensor(x, dtype=torch.int32, device=self.kv.device)
@@ -216,11 +219,8 @@ class PagedPath:
                            pos0=self.pos, n_valid=n_valid)
         self.pos.add_(n if n_valid is None else n_valid)
         out = torch.zeros_like(q) if out is None else out
-        key = (n, q.shape[2])
-        if key not in self._ws:
-            self._ws[key] = L.workspace(L.paged_attn_workspace_bytes(q, self.kv), self.kv.device)
         L.mpc_paged_attn(q, self.kv, out, sm_scale=self.sm_scale, window=self.window, sinks=self.sinks, n_valid=n_valid,
-                         lse=lse, ws=self._ws[key])
+                         lse=lse, ws=self.ws)
         return out
 
     def extend(self, q, k, v, new=None, out=None, lse=None):

@@ -1,10 +1,12 @@
-"""One workspace of the paged attention for calls of different shapes, and the one that a call makes for itself on another
-stream."""
+"""One workspace of the paged attention for calls of different shapes, the one that a call makes for itself on another stream,
+and a step of PagedPath whose first use is its capture."""
 import pytest
 import torch
 
 from test_gpu_attn import fill, run_paged
 from test_gpu_paged_append import bits, make, tokens
+from test_gpu_paged_path import inputs
+from test_gpu_paged_path import make as make_path
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +47,35 @@ def test_workspace_of_a_call_on_another_stream():
     side.synchronize()
     for out in outs:
         assert torch.equal(bits(out), bits(want[0]))
+
+
+def test_a_step_whose_first_use_is_its_capture():
+    """The capture makes nothing that later steps use (its clearing would wait for the first replay): eager steps of the same
+    shape run right after it, before the first replay, and between the replays."""
+    import paper_2501_06807_amd as M
+    a, b = make_path(page=16), make_path(page=16)
+    q, k, v = inputs(a, 100, "bf16", 0)
+    for p in (a, b):
+        p.prefill(q.clone(), k, v)
+        p.reserve([150] * 3)
+    q, k, v = inputs(a, 1, "bf16", 5)
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    g = M.MPCachePath.capture(a, a.step, q, k, v, None, out)
+    # (a graph keeps two words of its own; a workspace of two query rows has 270 KB)
+    assert torch.cuda.memory_allocated() - held <= 4096
+    for i in range(12):
+        x = inputs(a, 1, "bf16", 100 + 10 * i)
+        if i % 3 == 0:
+            got = a.extend(x[0].clone(), x[1], x[2])
+        else:
+            for dst, src in zip((q, k, v), x):
+                dst.copy_(src)
+            a.grown([1] * 3)
+            g.replay()
+            got = out
+        want = b.extend(x[0].clone(), x[1], x[2])
+        torch.cuda.synchronize()
+        assert torch.equal(bits(got), bits(want)), i
+    assert a.kv.lens.tolist() == b.kv.lens.tolist() == a.rows
