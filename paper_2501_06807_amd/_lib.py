@@ -384,6 +384,30 @@ def _rows(t, what, dtype, heads=None):
     return t.data_ptr(), ctypes.byref(MpcStrides(*t.stride()[:4])), shape
 
 
+def _placed(t, what, written=False):
+    """Refuses the address and strides that the library would refuse: off 16 bytes, or of rows that are written and overlap."""
+    size = t.element_size()
+    if t.data_ptr() % 16:
+        raise ValueError(f"{what} must be 16-byte aligned")
+    if t.is_contiguous():
+        return
+    axes = sorted((s, n) for s, n in zip(t.stride()[:-1], t.shape[:-1]) if n > 1)
+    if any(s * size % 16 for s, _ in axes):
+        raise ValueError(f"{what}: strides must be whole numbers of 16 bytes")
+    span = t.shape[-1]  # elements from the first to behind the last of the axes so far
+    for s, n in axes if written else ():
+        if s < span:
+            raise ValueError(f"{what}: rows that are written overlap")
+        span += (n - 1) * s
+
+
+def _rope_of(rope):
+    """(pointer, positions, rotated channels) of a rotary table."""
+    if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous():
+        raise ValueError("rope must be contiguous float32 [n_pos][rot_dim / 2][2]")
+    return rope.data_ptr(), rope.shape[0], 2 * rope.shape[1]
+
+
 def _batch_ints(t, what, B, device):
     if t is None:
         return None
@@ -495,9 +519,7 @@ def mpc_paged_append(k, v, kv, *, q=None, q_out=None, k_out=None, rope=None, rop
     _like(shape, kv, n, "v")
     Hq, qp, qs, op, os_, r = kv.Hkv, None, None, None, None, None
     if rope is not None:
-        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous():
-            raise ValueError("rope must be contiguous float32 [n_pos][rot_dim / 2][2]")
-        r = ctypes.byref(MpcRope(rope.data_ptr(), rope.shape[0], 2 * rope.shape[1], ROPE_STYLE[rope_style]))
+        r = ctypes.byref(MpcRope(*_rope_of(rope), ROPE_STYLE[rope_style]))
     if q is not None:
         q_out = q if q_out is None else q_out
         qp, qs, shape = _rows(q, "q", kv.dtype)

@@ -1,6 +1,7 @@
 """Preallocated prefill + decode paths over the C-ABI entry points: the kept cache of the method, and a paged cache."""
 import ctypes
 import math
+import operator
 
 import torch
 
@@ -160,18 +161,26 @@ class PagedPath:
 
     prefill() starts every sequence with a prompt, extend() adds tokens to them (one each, drafted ones, or a chunk of a
     prompt) and attends over the cache, take_back() drops the newest rows again (rejected drafts), and adopt() starts the
-    sequences with the rows that a MPCachePath kept. fp8: pages of e4m3 codes with a scale for each page and head.
-    window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
+    sequences with the rows that a MPCachePath kept. A call that is refused has changed nothing. fp8: pages of e4m3 codes
+    with a scale for each page and head. window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
     (cos, sin); None where q and k arrive rotated."""
 
     def __init__(self, *, n_layers, batch, n_q_heads, n_kv_heads, head_dim, dtype, max_rows, page_size=64, n_pages=None,
                  fp8=True, window=0, sinks=0, rope=None, rope_style="interleaved", sm_scale=None, device="cuda"):
         self.Hq, self.window, self.sinks, self.rope, self.rope_style = n_q_heads, window, sinks, rope, rope_style
         self.sm_scale = 1.0 / math.sqrt(head_dim) if sm_scale is None else sm_scale
+        if not 0 <= window < 2 ** 31 or not 0 <= sinks < 2 ** 31 or not math.isfinite(self.sm_scale):
+            raise ValueError("window and sinks must be from 0 on, and sm_scale finite")
+        if rope_style not in L.ROPE_STYLE:
+            raise ValueError(f"rope_style must be one of {list(L.ROPE_STYLE)}")
         max_pages = -(-max_rows // page_size)
         n_pages = batch * max_pages if n_pages is None else n_pages
         self.kv = L.paged_kv(n_layers=n_layers, batch=batch, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype,
                              n_pages=n_pages, max_pages=max_pages, page_size=page_size, fp8=fp8, device=device)
+        if rope is not None:
+            p, n_pos, rot = L._rope_of(rope)
+            if rope.device != self.kv.device or p % 16 or n_pos == 0 or rot == 0 or rot % 16 or rot > head_dim:
+                raise ValueError(f"rope must turn a multiple of 16 channels up to {head_dim} and lie 16-byte aligned on {self.kv.device}")
         self.pos = torch.zeros(batch, dtype=torch.int32, device=self.kv.device)  # position of each sequence's next token
         self.rows = [0] * batch  # the lengths again, on the host
         self._kept = [0] * batch  # first row of each sequence that its tail still holds
@@ -180,10 +189,49 @@ class PagedPath:
         # for steps of any number of tokens (the bytes do not grow beyond 32 query rows to a kv head), and cleared here, so
         # that a step may be captured before one has run
         size = lambda n: L.lib().mpc_workspace_bytes(L.MPC_OP_PAGED_ATTN, self.kv.dims(n_q_heads), n, self.kv.ref)  # noqa: E731
+        if size(1) == 0:
+            raise ValueError(f"sizes that the library does not take ({L.lib().mpc_last_error().decode()})")
         self.ws = L.workspace(max(size(1), size(32)), self.kv.device)
 
     def _ints(self, x):
         return torch.tensor(x, dtype=torch.int32, device=self.kv.device)
+
+    def _counts(self, x, what, most=math.inf):
+        """One whole number from 0 to `most` for each sequence."""
+        x = [operator.index(n) for n in x]
+        if len(x) != self.kv.B or any(not 0 <= n <= most for n in x):
+            raise ValueError(f"{what}: {self.kv.B} numbers from 0 to {most} are wanted")
+        return x
+
+    def _check(self, n, q, k, v, out, lse):
+        """Refuses the tensors that the calls of a step or a prompt would refuse, before any of them has run."""
+        kv, turned = self.kv, self.rope is not None
+        if n < 1:
+            raise ValueError("no tokens")
+        for what, t, heads, written in (("q", q, self.Hq, turned), ("k", k, kv.Hkv, False), ("v", v, kv.Hkv, False),
+                                        ("out", out, self.Hq, True)):
+            if t is None:
+                continue
+            L._like(L._rows(t, what, kv.dtype, heads)[2], kv, n, what)
+            L._placed(t, what, written)
+        L._lse_of(lse, (kv.L, kv.B, self.Hq, n))
+        L._on(kv.device, None, q, k, v, out, lse)
+
+    def _lacking(self, rows, held, free):
+        """The pages that rows[b] rows of each sequence want beyond the held[b] that it has, of `free` ones."""
+        page, M = self.kv.page, self.kv.table.shape[1]
+        if any(r > M * page for r in rows):
+            raise ValueError(f"a sequence of more than {M * page} rows")
+        want = [max(0, -(-r // page) - n) for r, n in zip(rows, held)]
+        if sum(want) > free:
+            raise ValueError(f"{sum(want)} pages wanted, {free} free")
+        return want
+
+    def _start(self, rows):
+        """Empties every sequence and books rows[b] rows for each, if the whole pool has pages for them."""
+        self._lacking(rows, [0] * self.kv.B, len(self._free) + sum(len(p) for p in self._pages))
+        self.clear()
+        self.grown(rows)
 
     def clear(self):
         """Empties every sequence; the pages go back to the pool."""
@@ -198,12 +246,7 @@ class PagedPath:
 
     def reserve(self, rows):
         """Pages for rows[b] rows of each sequence, for steps that are replayed from a graph; extend() does it by itself."""
-        page, M = self.kv.page, self.kv.table.shape[1]
-        want = [max(0, -(-r // page) - len(p)) for r, p in zip(rows, self._pages)]
-        if any(r > M * page for r in rows):
-            raise ValueError(f"a sequence of more than {M * page} rows")
-        if sum(want) > len(self._free):
-            raise ValueError(f"{sum(want)} pages wanted, {len(self._free)} free")
+        want, M = self._lacking(self._counts(rows, "rows"), [len(p) for p in self._pages], len(self._free)), self.kv.table.shape[1]
         if sum(want) == 0:
             return
         for b, n in enumerate(want):
@@ -212,8 +255,13 @@ class PagedPath:
 
     def step(self, q, k, v, n_valid=None, out=None, lse=None):
         """The device's part of extend(), which can be captured as a HIP graph: rotates, appends and attends, for sequences
-        whose pages are reserved. q becomes rotated in place."""
+        whose pages are reserved. n_valid[b] (int32 on the device) is from 0 to n. q becomes rotated in place."""
         n = q.shape[3] if q.dim() == 5 else 1
+        self._check(n, q, k, v, out, lse)
+        L._batch_ints(n_valid, "n_valid", self.kv.B, self.kv.device)
+        return self._step(n, q, k, v, n_valid, out, lse)
+
+    def _step(self, n, q, k, v, n_valid, out, lse):
         self.kv.lens.add_(n if n_valid is None else n_valid)
         L.mpc_paged_append(k, v, self.kv, q=q if self.rope is not None else None, rope=self.rope, rope_style=self.rope_style,
                            pos0=self.pos, n_valid=n_valid)
@@ -224,15 +272,17 @@ class PagedPath:
         return out
 
     def extend(self, q, k, v, new=None, out=None, lse=None):
-        """Adds the tokens q [L][B][Hq][n][d], k, v [L][B][Hkv][n][d] (new[b] of sequence b, n by default) and returns their
+        """Adds the tokens q [L][B][Hq][n][d], k, v [L][B][Hkv][n][d] (new[b] <= n of sequence b, n by default) and returns their
         attention over the cache, shaped like q."""
         n = q.shape[3] if q.dim() == 5 else 1
+        new = None if new is None else self._counts(new, "new", n)
+        self._check(n, q, k, v, out, lse)
         self.grown([n] * self.kv.B if new is None else new)
-        return self.step(q, k, v, None if new is None else self._ints(new), out, lse)
+        return self._step(n, q, k, v, None if new is None else self._ints(new), out, lse)
 
     def grown(self, new):
         """Books new[b] rows of each sequence on the host and reserves their pages (before the step, or the replays of one)."""
-        rows = [r + n for r, n in zip(self.rows, new)]
+        rows = [r + n for r, n in zip(self.rows, self._counts(new, "new"))]
         self.reserve(rows)
         self.rows = rows
         page = self.kv.page
@@ -242,9 +292,10 @@ class PagedPath:
         """Drops the newest dropped[b] rows of each sequence; the pages stay reserved. With 8-bit pages the page that a
         sequence then ends in has to be in its tail still, which holds the last two pages that it ever reached: a page's
         rows at least."""
+        dropped = self._counts(dropped, "dropped")
         page, rows = self.kv.page, [r - d for r, d in zip(self.rows, dropped)]
         for r, d, kept in zip(rows, dropped, self._kept):
-            if d < 0 or r < 0 or (self.kv.k_scale is not None and r % page and r // page * page < kept):
+            if r < 0 or (self.kv.k_scale is not None and r % page and r // page * page < kept):
                 raise ValueError("more rows than the sequence has, or than its tail keeps")
         d = self._ints(dropped)
         self.rows = rows
@@ -253,12 +304,14 @@ class PagedPath:
 
     def prefill(self, q, k, v, lens=None, out=None, lse=None):
         """Starts every sequence with its prompt, q [L][B][Hq][T][d], k, v [L][B][Hkv][T][d] (lens[b] tokens of sequence b, T by
-        default): the rows go into the cache, and the attention of the prompt's rows among themselves is returned. q
+        default, lens[b] <= T): the rows go into the cache, and the attention of the prompt's rows among themselves is returned. q
         becomes rotated in place."""
-        self.clear()
+        if q.dim() != 5 or k.dim() != 5 or v.dim() != 5:
+            raise ValueError("q, k and v must be [L][B][H][T][d]")
         T = q.shape[3]
-        new = [T] * self.kv.B if lens is None else list(lens)
-        self.grown(new)
+        new = [T] * self.kv.B if lens is None else self._counts(lens, "lens", T)
+        self._check(T, q, k, v, out, lse)
+        self._start(new)
         n = None if lens is None else self._ints(new)
         self.kv.lens.copy_(self._ints(new))
         turned = torch.empty_like(k) if self.rope is not None else None
@@ -273,9 +326,14 @@ class PagedPath:
     def adopt(self, path, position):
         """Starts every sequence with the rows that `path` (a MPCachePath of the same shape) keeps, as they are: its evicted
         prompt and what was appended to it. `position`: that of the next token."""
-        self.clear()
-        n = path.Ts + path.n_tail
-        self.grown([n] * self.kv.B)
+        kv, n = self.kv, path.Ts + path.n_tail
+        for what, t in (("path.k_s", path.k_s), ("path.v_s", path.v_s)):
+            L._like(L._rows(t[:, :, :, :n], what, kv.dtype, kv.Hkv)[2], kv, n, what)
+        L._on(kv.device, None, path.k_s, path.v_s)
+        position = operator.index(position)
+        if not 0 <= position < 2 ** 31:
+            raise ValueError("position must be from 0 on")
+        self._start([n] * kv.B)
         self.kv.lens.fill_(n)
         L.mpc_paged_append(path.k_s[:, :, :, :n], path.v_s[:, :, :, :n], self.kv)
         self.pos.fill_(position)
