@@ -295,10 +295,12 @@ class PagedPath:
         dropped = self._counts(dropped, "dropped")
         page, rows = self.kv.page, [r - d for r, d in zip(self.rows, dropped)]
         for r, d, kept in zip(rows, dropped, self._kept):
-            if r < 0 or (self.kv.k_scale is not None and r % page and r // page * page < kept):
+            if r < 0 or (d and self.kv.k_scale is not None and r % page and r // page * page < kept):
                 raise ValueError("more rows than the sequence has, or than its tail keeps")
         d = self._ints(dropped)
         self.rows = rows
+        # where a page begins nothing of the tail is needed, and what follows is written into it again
+        self._kept = [min(k, r) if r % page == 0 else k for k, r in zip(self._kept, rows)]
         self.kv.lens.sub_(d)
         self.pos.sub_(d)
 

@@ -1,4 +1,4 @@
-"""PagedPath: a call that is refused leaves the path as it was, on the host and on the device."""
+"""PagedPath: a call that is refused leaves the path as it was, on the host and on the device; rows taken back far."""
 import math
 
 import pytest
@@ -138,3 +138,24 @@ def test_an_evicted_cache_of_another_shape_is_refused():
                   dict(T=512, keep=256)):
         refused(path, path.adopt, M.MPCachePath(**dict(kw, **other)), 64)
     refused(path, path.adopt, M.MPCachePath(**kw), -1)
+
+
+def test_rows_taken_back_to_a_page_far_behind():
+    """From row 161 to row 32, where a page begins, and on from there: drafts are taken back again as on a path that never
+    went further, and the other sequences' too."""
+    a, b = make(page=16), make(page=16)
+    q, k, v = inputs(a, 161, "bf16", 0)
+    a.prefill(q.clone(), k, v, [161, 30, 161])
+    a.take_back([161 - 32, 0, 161 - 32])
+    b.prefill(q[:, :, :, :32].contiguous(), k[:, :, :, :32], v[:, :, :, :32], [32, 30, 32])
+    for i, (new, back) in enumerate([([5, 5, 1], [2, 1, 0]), ([4, 0, 5], [0, 2, 3]), ([5, 5, 5], [5, 1, 0]), ([5, 5, 5], [0, 5, 5]),
+                                     ([5, 3, 5], [1, 3, 5])]):
+        x = inputs(a, 5, "bf16", 10 + 10 * i)
+        got, want = (p.extend(x[0].clone(), x[1], x[2], new) for p in (a, b))
+        assert torch.equal(bits(got), bits(want)), i
+        for p in (a, b):
+            p.take_back(back)
+        assert a.rows == b.rows and a.kv.lens.tolist() == b.kv.lens.tolist() == a.rows
+    for p in (a, b):
+        with pytest.raises(ValueError):  # row 20 lies in a page that neither tail holds now
+            p.take_back([p.rows[0] - 20, 0, 0])
