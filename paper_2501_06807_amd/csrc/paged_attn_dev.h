@@ -161,6 +161,11 @@ struct PagedWave {
     return j <= p && (!a.window || j > p - a.window || j < a.sinks);
   }
 
+  // Whether the row at position p sees any of the 16 keys from j0 on (of those that exist).
+  __device__ static __forceinline__ bool sees_half(const AttnArgs& a, int p, int j0) {
+    return j0 <= p && (!a.window || j0 + 15 > p - a.window || j0 < a.sinks);
+  }
+
   // Scores to weights (by value place): scale c and weight factor f of each half; maximum and sum follow. With `edge`
   // some row may not see some key; have: halves that exist, rows: rows that do.
   __device__ __forceinline__ void weights(const f32x4 (*s)[TL::HALVES], const float* c, const float* f, const AttnArgs& a,
@@ -206,9 +211,17 @@ struct PagedWave {
       }
 #pragma unroll
       for (int j = 0; j < TL::VK; ++j) {
-        const float w = fast_exp2(e[j]);
-        l[rt] += w;
-        p[rt][j] = f ? w * f[j / 4] : w;
+        p[rt][j] = fast_exp2(e[j]);
+        l[rt] += p[rt][j];
+      }
+      if (f) {
+#pragma unroll
+        for (int h = 0; h < TL::HALVES; ++h) {
+          // a page that the row sees nothing of does not reach it, whatever its scale is
+          const float fh = !edge || sees_half(a, pos[rt], k0 + 16 * h) ? f[h] : 0.f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[rt][4 * h + r] *= fh;
+        }
       }
     }
   }
@@ -315,15 +328,16 @@ struct PagedWave {
       if (!scale) {
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t) o[rt][t] = mma<PV>(words(w[t]), x, mma<PV>(words(w[t]), y, o[rt][t]));
-      } else if (scale[0] == scale[1]) {
+      } else if (!edge && scale[0] == scale[1]) {
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t) o[rt][t] += mma<PV>(words(w[t]), x, mma<PV>(words(w[t]), y, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[0];
-      } else {  // two pages of 16 rows
+      } else {  // two pages of 16 rows, or rows that see nothing of one half (its scale does not reach them)
+        const float s0 = !edge || sees_half(a, pos[rt], k0) ? scale[0] : 0.f, s1 = !edge || sees_half(a, pos[rt], k0 + 16) ? scale[1] : 0.f;
         const uint4 x0 = make_uint4(x.x, x.y, 0, 0), x1 = make_uint4(0, 0, x.z, x.w), y0 = make_uint4(y.x, y.y, 0, 0), y1 = make_uint4(0, 0, y.z, y.w);
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t)
-          o[rt][t] += mma<PV>(words(w[t]), x0, mma<PV>(words(w[t]), y0, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[0] +
-                      mma<PV>(words(w[t]), x1, mma<PV>(words(w[t]), y1, f32x4{0.f, 0.f, 0.f, 0.f})) * scale[1];
+          o[rt][t] += mma<PV>(words(w[t]), x0, mma<PV>(words(w[t]), y0, f32x4{0.f, 0.f, 0.f, 0.f})) * s0 +
+                      mma<PV>(words(w[t]), x1, mma<PV>(words(w[t]), y1, f32x4{0.f, 0.f, 0.f, 0.f})) * s1;
       }
     }
   }
