@@ -117,7 +117,8 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
   const int pos = start + t;
 
   // a negative scale is taken into the queries
-  const float c = fmaxf(fabsf(a.qscale), 1e-30f);  // (zero times a masked score would be NaN)
+  // zero times a masked score would be NaN: the smallest number that is not zero instead, 5e-7 times the largest score
+  const float c = fmaxf(fabsf(a.qscale), 0x1p-149f);
   const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
   uint4 q[KSTEPS];
   {

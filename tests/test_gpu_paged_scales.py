@@ -1,4 +1,4 @@
-"""Page scales that a caller wrote, or nobody did, in pages that a row does not see."""
+"""Page scales that a caller wrote, or nobody did, in pages that a row does not see; score scales far below one."""
 import math
 
 import pytest
@@ -44,3 +44,30 @@ def test_scales_of_pages_that_a_row_does_not_see(dtype, side, bad, n, lens, page
                 bo, bl = R.bounds(x, k, v, idx, w, o, ls, d ** -0.5, DT[dtype])
                 R.check(out[0, b, hq, t].cpu(), o, bo, f"b{b} h{hq} t{t}")
                 R.check(lse[0, b, hq, t].cpu(), ls, bl, f"lse b{b} h{hq} t{t}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_score_scales_far_below_one(dtype):
+    """Products of 2^116 to 2^117 with a scale of 2^-116 are scores of 1 to 2: the scale is taken as it is."""
+    import paper_2501_06807_amd as M
+    d, T, sm = 64, 70, 2.0 ** -116
+    k, q = torch.zeros(1, 1, 1, T, d), torch.zeros(1, 1, 2, T, d)
+    k[..., 0] = (1 + torch.arange(T) % 8 / 8.0) * 2.0 ** 58
+    q[..., 0] = 2.0 ** 58
+    q[0, 0, 1] *= -1
+    v = tokens((1, 1, 1, T, d), dtype, 2, spread=False)
+    k, q = k.to(DT[dtype]), q.to(DT[dtype])
+    out, lse = torch.empty_like(q).cuda(), torch.empty(1, 1, 2, T, device="cuda")
+    M.mpc_prompt_attn(q.cuda(), k.cuda(), v.cuda(), out, sm_scale=sm, window=20, sinks=2, lse=lse)
+    kv = make(M, 1, 1, 1, d, dtype, 16, cap=5, fp8=False)
+    kv.lens.fill_(T)
+    M.mpc_paged_append(k.cuda(), v.cuda(), kv)
+    po, pl = run_paged(kv, q.cuda(), [T], 20, 2, sm=sm)
+    for h in range(2):
+        for t in (0, 5, 40, 69):
+            x, kd, vd = q[0, 0, h, t].double(), k[0, 0, 0].double(), v[0, 0, 0].double()
+            o, ls, idx, w = R.attend(x, kd, vd, t, sm, 20, 2)
+            bo, bl = R.bounds(x, kd, vd, idx, w, o, ls, sm, DT[dtype])
+            for got, gl, what in ((out, lse, "prompt"), (po, pl, "pages")):
+                R.check(got[0, 0, h, t].cpu(), o, bo, f"{what} h{h} t{t}")
+                R.check(gl[0, 0, h, t].cpu(), ls, bl, f"{what} lse h{h} t{t}")
