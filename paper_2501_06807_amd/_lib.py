@@ -544,6 +544,13 @@ def paged_attn_workspace_bytes(q, kv):
                                      kv.ref)
 
 
+def _attn_cfg(sm_scale, window, sinks):
+    for what, x in (("window", window), ("sinks", sinks)):
+        if not -2 ** 31 <= x < 2 ** 31:  # (a field would keep the lower 32 bits)
+            raise ValueError(f"{what} {x} does not fit 32 bits")
+    return MpcAttnCfg(sm_scale, window, sinks)
+
+
 def _lse_of(lse, shape):
     if lse is None:
         return None
@@ -566,7 +573,7 @@ def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse
         ws = _call_ws(paged_attn_workspace_bytes(q, kv), kv.device, stream)
     _contig(ws)
     st = _on(kv.device, stream, q, out, lse, ws)
-    cfg = MpcAttnCfg(sm_scale, window, sinks)
+    cfg = _attn_cfg(sm_scale, window, sinks)
     _call("mpc_paged_attn", lib().mpc_paged_attn, kv.device, kv.dims(shape[2]), kv.ref, n,
           _batch_ints(n_valid, "n_valid", kv.B, kv.device), ctypes.byref(cfg), qp, qs, op, os_, _lse_of(lse, shape),
           ws.data_ptr(), ws.numel() * ws.element_size(), st)
@@ -590,6 +597,6 @@ def mpc_prompt_attn(q, k, v, out, *, sm_scale, window=0, sinks=0, q_lens=None, k
     dev = q.device
     st = _on(dev, stream, k, v, out, lse)
     dims = MpcDims(B, 0, L, Hq, kshape[2], d, DTYPE_CODE[q.dtype], 0)
-    cfg = MpcAttnCfg(sm_scale, window, sinks)
+    cfg = _attn_cfg(sm_scale, window, sinks)
     _call("mpc_prompt_attn", lib().mpc_prompt_attn, dev, ctypes.byref(dims), Tq, kshape[3], _batch_ints(q_lens, "q_lens", B, dev),
           _batch_ints(k_lens, "k_lens", B, dev), ctypes.byref(cfg), qp, qs, kp, ks, vp, vs, op, os_, _lse_of(lse, shape), st)
