@@ -359,7 +359,7 @@ mpc_status mpc_commonality(int32_t L, int32_t units, int32_t k, int32_t m, const
  *   result rounded once to the element type; a position outside the rotary table gives NaN.
  *   k, v   [L][B][Hkv][n_new][d] (k_strides, v_strides; NULL: contiguous)
  *   q      [L][B][Hq][n_new][d] or NULL; its rotated rows go to q_out (rows from n_valid[b] on are left
- *          as they were), which may be q itself and may not overlap anything otherwise;
+ *          as they were), which may be q itself (strides and all) and may not overlap anything otherwise;
  *   k_out  [L][B][Hkv][n_new][d] or NULL: also receives K's rows as the cache takes them (rotated, in the
  *          element type), for mpc_prompt_attn; those of rows 0 <= j < M * page_size are written. It may not
  *          overlap k or anything else;

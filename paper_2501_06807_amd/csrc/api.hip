@@ -867,6 +867,8 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
     if (!rope) return fail(MPC_EINVAL, "q is given without a rotation");
     if ((s = rows_of(dims, "q", q, q_strides, dims->n_q_heads, n_new, false, &a.q)) != MPC_OK) return s;
     if ((s = rows_of(dims, "q_out", q_out, q_out_strides, dims->n_q_heads, n_new, true, &a.q_out)) != MPC_OK) return s;
+    if (q_out == q && (a.q.layer != a.q_out.layer || a.q.batch != a.q_out.batch || a.q.head != a.q_out.head || a.q.token != a.q_out.token))
+      return fail(MPC_EINVAL, "q_out may be q itself, but not q's memory in another order");
     a.Hq = dims->n_q_heads;
   } else if (q_out) {
     return fail(MPC_EINVAL, "q_out is given without q");
