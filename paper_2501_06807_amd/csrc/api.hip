@@ -867,7 +867,9 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
     if (!rope) return fail(MPC_EINVAL, "q is given without a rotation");
     if ((s = rows_of(dims, "q", q, q_strides, dims->n_q_heads, n_new, false, &a.q)) != MPC_OK) return s;
     if ((s = rows_of(dims, "q_out", q_out, q_out_strides, dims->n_q_heads, n_new, true, &a.q_out)) != MPC_OK) return s;
-    if (q_out == q && (a.q.layer != a.q_out.layer || a.q.batch != a.q_out.batch || a.q.head != a.q_out.head || a.q.token != a.q_out.token))
+    const auto differ = [](int64_t x, int64_t y, int size) { return size > 1 && x != y; };
+    if (q_out == q && (differ(a.q.layer, a.q_out.layer, dims->n_layers) || differ(a.q.batch, a.q_out.batch, dims->batch) ||
+                       differ(a.q.head, a.q_out.head, dims->n_q_heads) || differ(a.q.token, a.q_out.token, n_new)))
       return fail(MPC_EINVAL, "q_out may be q itself, but not q's memory in another order");
     a.Hq = dims->n_q_heads;
   } else if (q_out) {

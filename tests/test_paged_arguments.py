@@ -32,3 +32,9 @@ def test_queries_in_place_are_rotated_where_they_lie(qs, os_, same):
     s = L.lib().mpc_paged_append(ref(dims()), ref(cache()), 4, None, ref(rope()), None, FAKE, None, FAKE, None, FAKE, ref(qs), FAKE,
                                  ref(os_), FAKE, None, None)
     assert s == L.MPC_EINVAL and ("k_out" if same else "q_out") in L.lib().mpc_last_error().decode()
+
+
+def test_strides_of_axes_of_one_entry_are_not_compared():
+    s = L.lib().mpc_paged_append(ref(dims(batch=1, n_layers=1)), ref(cache()), 1, None, ref(rope()), None, FAKE, None, FAKE, None, FAKE,
+                                 None, FAKE, ref(L.MpcStrides(7, 0, 128, 1)), FAKE, None, None)
+    assert s == L.MPC_EINVAL and "k_out" in L.lib().mpc_last_error().decode()
