@@ -128,3 +128,19 @@ def test_appended_prompts(dtype, fp8, page, d, Hq, Hkv, n, style, rot):
                 at = j % (2 * page)
                 assert torch.equal(bits(kv.k_tail[0, b, :, at]), bits(k_out[0, b, :, j - base])), (b, j)
                 assert torch.equal(bits(kv.v_tail[0, b, :, at]), bits(v[0, b, :, j - base])), (b, j)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 4)])
+def test_chunks_over_a_paged_cache(dtype, fp8, d, window, sinks):
+    """48 query rows to a kv head: two units of two 16-row tiles each, their keys divided over workgroups and joined."""
+    import paper_2501_06807_amd as M
+    from test_gpu_attn import check_paged, fill, run_paged
+    lens, new, n = [3000, 12, 701], [12, 12, 5], 12
+    kv = make(M, 1, 3, 2, d, dtype, 32, cap=94, fp8=fp8)
+    fill(kv, lens, 5, dtype)
+    q = tokens((1, 3, 8, n, d), dtype, 3, spread=False).cuda()
+    out, lse = run_paged(kv, q, new, window, sinks)
+    check_paged(kv, q, out, lse, lens, new, window, sinks, d ** -0.5, f"{dtype} {fp8} {d}")
