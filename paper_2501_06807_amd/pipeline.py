@@ -210,11 +210,13 @@ class PagedPath:
             raise ValueError("no tokens")
         for what, t, heads, written in (("q", q, self.Hq, turned), ("k", k, kv.Hkv, False), ("v", v, kv.Hkv, False),
                                         ("out", out, self.Hq, True)):
-            if t is None:
+            if t is None or (t.dtype is kv.dtype and t.shape == (kv.L, kv.B, heads, n, kv.d) and t.device == kv.device and
+                             t.is_contiguous() and t.data_ptr() % 16 == 0):  # (a step's host time: nothing else can be wrong)
                 continue
             L._like(L._rows(t, what, kv.dtype, heads)[2], kv, n, what)
             L._placed(t, what, written)
-        L._lse_of(lse, (kv.L, kv.B, self.Hq, n))
+        if lse is not None:
+            L._lse_of(lse, (kv.L, kv.B, self.Hq, n))
         L._on(kv.device, None, q, k, v, out, lse)
 
     def _lacking(self, rows, held, free):
