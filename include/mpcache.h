@@ -394,8 +394,9 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
  * bytes it has (calls sharing it must not overlap). The bytes follow head_dim and n_new * G up to 32 only
  * and never fall with either. The sizes of the
  * cache, not the lengths, give the launch, so a captured call follows lengths and tables as they change.
- * Limits: n_new * G <= 2^30, fewer than 2^31 blocks of 128 keys over all (sequence, layer, kv head)s and
- * groups of 16 or 32 query rows. */
+ * Limits: n_new * G <= 2^30, fewer than 2^31 blocks of keys over all (sequence, layer, kv head)s and groups
+ * of query rows. For n_new * G <= 16 a group has 16 rows and a block 256 keys (fp32: 128), beyond that 32 rows
+ * and 128 keys (fp32: 64). */
 mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                           const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, void* out,
                           const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -7,9 +7,9 @@ namespace mpc {
 
 // Units of one 16-row tile where the rows fit, else of two. The grid is one workgroup to a compute unit (eight waves, what
 // the registers allow), or fewer where even the longest sequences have fewer blocks. Runs of a single block are taken too: a
-// wave's second tile costs as much as joining the parts (one sequence of 500 rows, 12 heads of 64: 11.6 us, with runs of at
-// least four blocks 12.0; 32 heads over 8 behind a window of 1024: 13.7 and 23.1; four sequences of drafts behind it: 21.1
-// and 34.2).
+// wave's second tile costs as much as joining the parts (one sequence of 500 rows, 12 heads of 64: 11.5 us, with runs of at
+// least four blocks 12.0; 32 heads over 8 behind a window of 1024: 13.5 and 22.8; four sequences of drafts behind it: 20.2
+// and 33.0).
 PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap) {
   PagedPlan p{};
   const long long rows = (long long)(Hq / Hkv) * n;

@@ -12,8 +12,10 @@
 // registers (byte permutes), and nothing passes through LDS until the waves' parts are joined.
 // Running maximum m, sum l and the accumulators are fp32. 16-bit types multiply a weight in two parts of the type, its rounding
 // and that of the rest, which holds it to half a step of half a step; fp32 multiplies in fp32. The second product of each value
-// costs no time (the first case below 371 us with one part and with two, the second 61.6 and 61.0, the drafts 37.7 and 31.4: their kernel no
-// longer spills), and takes the outputs' error from 0.0018 to 0.0017 of their size, what rounding them to bf16 costs. Codes
+// costs single and drafted tokens no time (one part and two: 371 us and 371 in the first case below, 61.6 and 61.0 in the
+// second, 37.7 and 31.4 for the drafts, whose kernel no longer spills); chunks of more than 16 query rows to a unit over codes
+// take 1.05 to 1.2 times as long (1000 rows of 32 heads over 20K rows of 8: 1076 us and 1272; over 16-bit pages 1460 and 1446).
+// The outputs' error falls from 0.0018 to 0.0017 of their size, what rounding them to bf16 costs. Codes
 // widen exactly to either 16-bit type. A page's value scale goes into a bf16 weight, whose range takes it; fp16 weights have no
 // such range: they are lifted by 2^14, so that only weights below 2^-28 of the largest lose bits of their first part, and the
 // scale is applied to a tile's product in fp32.
@@ -23,7 +25,8 @@
 // lengths, table entry and first rows (4), and the joins (4 to 8). In between the dies differ: their workgroups read at rates
 // 35% apart, so that the even division ends with the slowest (41 us on average, 48 on the last). Keys two tiles ahead instead
 // of one changed nothing (373 and 63 us), nor did runs of at least four blocks where there is enough work. 32 sequences of
-// four drafted tokens behind a window of 1024 (16-bit pages of 16 rows) take 31 us, 136 MB. A table entry or a
+// four drafted tokens behind a window of 1024 (16-bit pages of 16 rows) take 32 us, 136 MB (147 fetched): each workgroup has
+// one unit of 34 tiles, five rounds of its waves, and nothing beside the start, the last round and the end. A table entry or a
 // scale read through the vector cache waits for every row in flight: the scalar cache took the first case from 426 to 365.
 #pragma once
 #include "attn_mma.h"
@@ -646,7 +649,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       }
     }
 
-    // join the four waves: maxima and sums, then the accumulators in two steps
+    // join the waves: maxima and sums, then the accumulators in two steps
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       s_ml[wave][rt][0][lane] = w.m[rt];

@@ -11,9 +11,9 @@
 // the rounding leaves takes 818 us instead of 640 in the first case below, and 1306 instead of 1050 behind the window, for
 // outputs that are off by 0.0017 of their size instead of 0.0022 (their own rounding: 0.0017).
 //
-// 8K rows and keys of 32 heads of 128 in bf16: 638 us, 862 TFLOP/s of the products that the rows need (a large bf16 product
-// of the library: 1229). The matrix unit is busy 41% of the cycles, the vector unit as much (a quarter of it exponentials),
-// at 1.7 to 2 GHz. Both units side by side, in a written-out pipeline that takes the next tile's scores beside this one's
+// 8K rows and keys of 32 heads of 128 in bf16: 631 to 640 us, 862 TFLOP/s of the products that the rows need (a large bf16
+// product of the library: 1229). The matrix unit is busy 40% of the cycles, the vector unit as much (a quarter of it
+// exponentials), at 2.07 GHz. Both units side by side, in a written-out pipeline that takes the next tile's scores beside this one's
 // weights, gave 2% there and cost 4% behind a window: the clock falls as the units fill. 32-key tiles instead of 64 (which
 // spill): 1072 -> 730 us; whole tiles apart from edge tiles, and the values asked for before the scores: 640. A window of
 // 1024 over four prompts of up to 16K: 1045 us; a block of 128 rows visits 37 tiles for 32 full ones' worth of keys, 11 of

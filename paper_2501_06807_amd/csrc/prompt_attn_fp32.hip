@@ -4,8 +4,8 @@
 // tiles of 16 keys, which come straight from memory into registers: fp32 products (16x16x4, a sixteenth of the 16-bit
 // rate) leave the caches time to bring the rows, and short prompts have many workgroups this way. The waves' parts meet in
 // LDS. The scores, weights and products of a tile are those of the paged attention. 512 rows and keys of 12 heads of 64: 16 us
-// (the products alone 2.6 at the rate of a large fp32 product, 153 TFLOP/s): up to eight tiles one after the other, each a
-// chain of 16 dependent products and a memory round trip.
+// (the products alone 2.6 at the rate of a large fp32 product, 153 TFLOP/s): up to eight tiles one after the other, each with
+// four chains of four dependent products for its scores and a memory round trip (one chain of 16: 16 us too).
 #include "paged_attn_dev.h"
 
 namespace mpc {
