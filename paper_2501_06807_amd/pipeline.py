@@ -161,7 +161,8 @@ class PagedPath:
 
     prefill() starts every sequence with a prompt, extend() adds tokens to them (one each, drafted ones, or a chunk of a
     prompt) and attends over the cache, take_back() drops the newest rows again (rejected drafts), and adopt() starts the
-    sequences with the rows that a MPCachePath kept. A call that is refused has changed nothing. fp8: pages of e4m3 codes
+    sequences with the rows that a MPCachePath kept. A call that is refused has changed nothing. All calls of a path, and the
+    replays of its captured steps, share its cache and workspace, so they run in one stream's order. fp8: pages of e4m3 codes
     with a scale for each page and head. window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
     (cos, sin); None where q and k arrive rotated."""
 
