@@ -204,7 +204,7 @@ struct PagedWave {
       }
       const float base = (m[rt] == -INFINITY ? 0.f : m[rt]) - TL::LIFT;
       // The exponent s c - base in one rounding: what the product alone would lose, half a step of the score's size, is as
-      // large as that step in the weight (scores of 4000 in fp32: outputs off by 6e-6 before, 1e-6 now).
+      // large as that step in the weight (scores of 4000 in fp32: outputs off by 6e-6).
       float e[TL::VK];
 #pragma unroll
       for (int j = 0; j < TL::VK; ++j) e[j] = fmaf(s[rt][j / 4][j % 4], c[j / 4], -base);
