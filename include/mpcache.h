@@ -11,7 +11,8 @@
  *   - the commonality score of adjacent layers' top-k sets (Sec. 3, Observation 3).
  * Beside them stand the operators of serving from a paged cache, for the same models:
  *   - appending new tokens' keys and values to a paged cache, rotated by their positions, in the
- *     element type or in 8 bits with a scale for each page and head (mpc_paged_append);
+ *     element type, in 8 bits with a scale for each page and head, or in 4 bits with a scale for each 32
+ *     channels of a row (mpc_paged_append), and reading rows back (mpc_paged_read);
  *   - attention of one or more new tokens over such a cache (mpc_paged_attn);
  *   - attention of a prompt's rows over its keys (mpc_prompt_attn);
  *   both with an optional sliding window and first tokens that stay visible.
@@ -123,8 +124,10 @@ typedef struct {
 
 /* Page formats. SAME: rows of the element type. E4M3: 8-bit floating point codes (4 exponent bits, 3
  * mantissa bits, largest value 448, no infinities) with one fp32 scale for each (page, kv head), for K
- * and V apart: a row's value is code * scale. */
-typedef enum { MPC_PAGE_SAME = 0, MPC_PAGE_E4M3 = 1 } mpc_page_format;
+ * and V apart: a row's value is code * scale. MX4: 4-bit floating point codes (sign, 2 exponent bits, 1 mantissa
+ * bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte, the even channel in the low half, with one scale 2^(x - 127) for
+ * each 32 channels of a row, kept as the byte x (0 to 252; 255: all 32 values are NaN). */
+typedef enum { MPC_PAGE_SAME = 0, MPC_PAGE_E4M3 = 1, MPC_PAGE_MX4 = 4 } mpc_page_format;
 
 /* A paged cache. Row j of sequence b lies in page table[b][j / page_size], at row j % page_size.
  * With MPC_PAGE_E4M3 the pages hold complete pages only: the tail, a ring in the element type, has row
@@ -134,9 +137,10 @@ typedef struct {
   int32_t n_pages;          /* P: pages of a layer's pool                                          */
   int32_t max_pages;        /* M: table entries of a sequence; M * page_size rows at most (2^30)   */
   int32_t format;           /* mpc_page_format                                                     */
-  void *k_pages, *v_pages;  /* [L][P][Hkv][page_size][d], dtype or codes                            */
-  float *k_scale, *v_scale; /* [L][P][Hkv], MPC_PAGE_E4M3 only (else ignored, as the tails)         */
-  void *k_tail, *v_tail;    /* [L][B][Hkv][2 * page_size][d], dtype                                 */
+  void *k_pages, *v_pages;  /* [L][P][Hkv][page_size][d], dtype or codes (MPC_PAGE_MX4: d / 2 bytes to a row) */
+  void *k_scale, *v_scale;  /* MPC_PAGE_E4M3: float [L][P][Hkv]; MPC_PAGE_MX4: bytes [L][P][Hkv][d / 32][page_size],
+                             * 16-byte aligned; else ignored                                         */
+  void *k_tail, *v_tail;    /* [L][B][Hkv][2 * page_size][d], dtype, MPC_PAGE_E4M3 only (else ignored)  */
   const int32_t* table;     /* [B][M] page ids, the same for every layer                           */
   const int32_t* lens;      /* [B] rows in the cache, those of the call's new tokens included
                              * (values are brought into [0, 2^30])                                 */
@@ -371,12 +375,27 @@ mpc_status mpc_commonality(int32_t L, int32_t units, int32_t k, int32_t m, const
  * sign. New rows of the page of the last row and of the page before it also go to the tail, so the
  * cache is the same however its tokens are divided over calls, and up to page_size of the newest rows can
  * be taken back by lowering lens[b].
+ * MPC_PAGE_MX4 writes each row as it arrives: for each 32 channels of the row in the element type, scale = the least
+ * 2^e, e in [-126, 125], with amax <= 6 * 2^e over the finite values (2^0 where all are zero), code = value / scale to
+ * nearest (halves to the even code); what is beyond 6, infinities among it, becomes 6 of its sign, and a NaN makes the 32
+ * values NaN. Any number of the newest rows can be taken back.
  * No two table entries that a call writes to may name one page. No workspace. */
 mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                             const mpc_rope* rope, const int32_t* pos0, const void* k, const mpc_strides* k_strides,
                             const void* v, const mpc_strides* v_strides, const void* q, const mpc_strides* q_strides,
                             void* q_out, const mpc_strides* q_out_strides, void* k_out,
                             const mpc_strides* k_out_strides, void* stream);
+
+/* Rows of a paged cache of any format, in the element type: row t < n_valid[b] (NULL: n; values are brought into [0, n]) of
+ * sequence b is row first[b] + t of the cache (NULL: lens[b] - n_valid[b] + t, the newest ones), for the prompt
+ * attention over what the cache keeps, for eviction from it, or to move it. A value is code * scale, rounded once to the
+ * element type. Rows from n_valid[b] on, and rows that the cache does not have (outside [0, lens[b]) or
+ * [0, M * page_size), or in a page whose table entry lies outside [0, P)), are left as they were.
+ *   k_out, v_out [L][B][Hkv][n][d] (strides; NULL: contiguous), either of which may be NULL. They may overlap neither
+ *   each other nor the cache. No workspace. */
+mpc_status mpc_paged_read(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n, const int32_t* n_valid,
+                          const int32_t* first, void* k_out, const mpc_strides* k_strides, void* v_out,
+                          const mpc_strides* v_strides, void* stream);
 
 /* Attention of each sequence's newest n_valid[b] tokens (one, some drafted ones, a chunk of a prompt) over
  * a paged cache that holds them already: row t stands at position p = lens[b] - n_valid[b] + t among the
@@ -388,7 +407,8 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
  * see reaches it, whatever it holds. Rows from n_valid[b] on are left as they were.
  *   q, out [L][B][Hq][n_new][d] (strides; NULL: contiguous); lse [L][B][Hq][n_new] float or NULL.
  * fp32 scores, sums and accumulation; 16-bit types multiply each weight with the values in two parts of
- * their type (its rounding and that of the rest).
+ * their type (its rounding and that of the rest). 4-bit codes are multiplied as bf16 values, which hold code * scale
+ * exactly: fp16 queries and the weights enter as two bf16 parts (the queries' exactly).
  * ws: mpc_workspace_bytes(MPC_OP_PAGED_ATTN, dims, n_new, kv) bytes, zero-filled before its first use;
  * every completed call leaves it ready for the next, of this or any other dims, cache and n_new whose
  * bytes it has (calls sharing it must not overlap). The bytes follow head_dim and n_new * G up to 32 only

@@ -64,7 +64,7 @@ _LIB = None
 EXPORTS = ("mpc_workspace_bytes", "mpc_static_evict", "mpc_static_evict_noalloc", "mpc_static_evict_noalloc_limit",
            "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters",
            "mpc_sparse_decode_attn", "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality",
-           "mpc_paged_append", "mpc_paged_attn", "mpc_prompt_attn", "mpc_owner_layer",
+           "mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_prompt_attn", "mpc_owner_layer",
            "mpc_status_string", "mpc_last_error")
 
 
@@ -94,9 +94,10 @@ def lib():
         L.mpc_commonality.argtypes = [I, I, I, I, V, V, V]
         KV, S, A = P(MpcPagedKv), P(MpcStrides), P(MpcAttnCfg)
         L.mpc_paged_append.argtypes = [P(MpcDims), KV, I, V, P(MpcRope), V] + [V, S] * 5 + [V]
+        L.mpc_paged_read.argtypes = [P(MpcDims), KV, I, V, V] + [V, S] * 2 + [V]
         L.mpc_paged_attn.argtypes = [P(MpcDims), KV, I, V, A] + [V, S] * 2 + [V, V, ctypes.c_size_t, V]
         L.mpc_prompt_attn.argtypes = [P(MpcDims), I, I, V, V, A] + [V, S] * 4 + [V, V]
-        for fn in ("mpc_paged_append", "mpc_paged_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
+        for fn in ("mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
                    "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality"):
             getattr(L, fn).restype = ctypes.c_int
         L.mpc_owner_layer.argtypes = [I, I, I]
@@ -364,7 +365,8 @@ def mpc_decode_step_status(ws, clear=False):
 
 
 ROPE_STYLE = {"interleaved": 0, "half": 1}
-PAGE_FORMAT = {"same": 0, "e4m3": 1}
+PAGE_FORMAT = {"same": 0, "e4m3": 1, "mx4": 4}
+MX4_BLOCK = 32  # channels to a scale of 4-bit codes
 
 
 def _rows(t, what, dtype, heads=None):
@@ -443,22 +445,33 @@ class PagedKV:
     """A paged cache over the caller's tensors, as mpc_paged_append and mpc_paged_attn take it.
 
     k_pages, v_pages [L][P][Hkv][page][d] of the element type, or torch.float8_e4m3fn codes with k_scale, v_scale
-    [L][P][Hkv] float32 and the rings k_tail, v_tail [L][B][Hkv][2 page][d] of the element type; table [B][M] int32 page
-    ids; lens [B] int32, rows of each sequence with those of the next call's new tokens. The tables and lengths live on the
-    device: a caller writes them there, and a captured graph reads what they hold at its replay."""
+    [L][P][Hkv] float32 and the rings k_tail, v_tail [L][B][Hkv][2 page][d] of the element type, or torch.uint8 [L][P][Hkv]
+    [page][d / 2], two 4-bit codes to a byte, with k_scale, v_scale torch.uint8 [L][P][Hkv][d / 32][page]; table [B][M] int32
+    page ids; lens [B] int32, rows of each sequence with those of the next call's new tokens. dtype: the element type, which
+    4-bit pages do not tell. The tables and lengths live on the device: a caller writes them there, and a captured graph reads
+    what they hold at its replay."""
 
-    def __init__(self, k_pages, v_pages, table, lens, *, k_scale=None, v_scale=None, k_tail=None, v_tail=None):
-        codes = k_pages.dtype == torch.float8_e4m3fn
+    def __init__(self, k_pages, v_pages, table, lens, *, k_scale=None, v_scale=None, k_tail=None, v_tail=None, dtype=None):
+        codes, codes4 = k_pages.dtype == torch.float8_e4m3fn, k_pages.dtype == torch.uint8
         extra = (k_scale, v_scale, k_tail, v_tail)
-        if codes != all(t is not None for t in extra) or (not codes and any(t is not None for t in extra)):
+        if codes4:
+            if k_scale is None or v_scale is None or k_tail is not None or v_tail is not None:
+                raise ValueError("4-bit pages have scales and no tails")
+        elif codes != all(t is not None for t in extra) or (not codes and any(t is not None for t in extra)):
             raise ValueError("scales and tails belong to float8_e4m3fn pages, all four of them")
         _contig(k_pages, v_pages, table, lens, *extra)
         if k_pages.dim() != 5 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
             raise ValueError("k_pages and v_pages must be alike, [L][P][Hkv][page][d]")
         self.L, P, self.Hkv, self.page, self.d = k_pages.shape
-        self.dtype = k_tail.dtype if codes else k_pages.dtype
+        self.dtype = dtype if codes4 else k_tail.dtype if codes else k_pages.dtype
         if self.dtype not in DTYPE_CODE:
             raise TypeError(f"unsupported dtype {self.dtype}")
+        if dtype is not None and dtype != self.dtype:
+            raise TypeError(f"the cache's element type is {self.dtype}")
+        if codes4:
+            self.d *= 2
+            if any(t.dtype != torch.uint8 or t.shape != (self.L, P, self.Hkv, self.d // MX4_BLOCK, self.page) for t in (k_scale, v_scale)):
+                raise ValueError("k_scale and v_scale must be uint8 [L][P][Hkv][d / 32][page]")
         if table.dtype != torch.int32 or table.dim() != 2 or lens.dtype != torch.int32 or lens.shape != table.shape[:1]:
             raise ValueError("table must be int32 [B][M] and lens int32 [B]")
         self.B, M = table.shape
@@ -474,7 +487,7 @@ class PagedKV:
         self.k_pages, self.v_pages, self.table, self.lens = k_pages, v_pages, table, lens
         self.k_scale, self.v_scale, self.k_tail, self.v_tail = extra
         p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self.c = MpcPagedKv(self.page, P, M, PAGE_FORMAT["e4m3" if codes else "same"], p(k_pages), p(v_pages), p(k_scale),
+        self.c = MpcPagedKv(self.page, P, M, PAGE_FORMAT["mx4" if codes4 else "e4m3" if codes else "same"], p(k_pages), p(v_pages), p(k_scale),
                             p(v_scale), p(k_tail), p(v_tail), p(table), p(lens))
         self.ref = ctypes.byref(self.c)
         self._dims = {}
@@ -486,18 +499,32 @@ class PagedKV:
         return self._dims[n_q_heads]
 
 
-def paged_kv(*, n_layers, batch, n_kv_heads, head_dim, dtype, n_pages, max_pages, page_size=64, fp8=False, device="cuda"):
-    """An empty PagedKV: table entries -1 (no page), lengths 0."""
+def _page_format(fmt, fp8):
+    if fmt is None:
+        return "e4m3" if fp8 else "same"
+    if fmt not in PAGE_FORMAT or (fp8 and fmt != "e4m3"):
+        raise ValueError(f"the page format must be one of {list(PAGE_FORMAT)}, and \"e4m3\" with fp8")
+    return fmt
+
+
+def paged_kv(*, n_layers, batch, n_kv_heads, head_dim, dtype, n_pages, max_pages, page_size=64, fp8=False, fmt=None, device="cuda"):
+    """An empty PagedKV: table entries -1 (no page), lengths 0. fmt: the pages' format, "same" (as the element type), "e4m3" or
+    "mx4"; fp8 is another way to say "e4m3"."""
+    fmt = _page_format(fmt, fp8)
     dev = torch.device(device)
     new = lambda t, *shape: torch.zeros(shape, dtype=t, device=dev)  # noqa: E731
     pool = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
     ring = (n_layers, batch, n_kv_heads, 2 * page_size, head_dim)
+    table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=dev)
+    if fmt == "mx4":
+        pool, scales = pool[:4] + (head_dim // 2,), pool[:3] + (head_dim // MX4_BLOCK, page_size)
+        return PagedKV(new(torch.uint8, *pool), new(torch.uint8, *pool), table, new(torch.int32, batch),
+                       k_scale=new(torch.uint8, *scales), v_scale=new(torch.uint8, *scales), dtype=dtype)
     extra = {}
-    if fp8:
+    if fmt == "e4m3":
         extra = dict(k_scale=new(torch.float32, *pool[:3]), v_scale=new(torch.float32, *pool[:3]), k_tail=new(dtype, *ring),
                      v_tail=new(dtype, *ring))
-    t = torch.float8_e4m3fn if fp8 else dtype
-    table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=dev)
+    t = torch.float8_e4m3fn if fmt == "e4m3" else dtype
     return PagedKV(new(t, *pool), new(t, *pool), table, new(torch.int32, batch), **extra)
 
 
@@ -536,6 +563,22 @@ def mpc_paged_append(k, v, kv, *, q=None, q_out=None, k_out=None, rope=None, rop
     st = _on(kv.device, stream, k, v, q, q_out, k_out, rope)
     _call("mpc_paged_append", lib().mpc_paged_append, kv.device, kv.dims(Hq), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
           r, _batch_ints(pos0, "pos0", kv.B, kv.device), kp, ks, vp, vs, qp, qs, op, os_, kop, kos, st)
+
+
+def mpc_paged_read(kv, k_out=None, v_out=None, *, first=None, n_valid=None, stream=None):
+    """Rows of the cache `kv`, in the element type, into k_out, v_out [L][B][Hkv][n][d] (or [L][B][Hkv][d], any strides; either may be
+    None): row t < n_valid[b] (n by default) of sequence b is row first[b] + t of the cache (the newest n_valid[b] rows by
+    default). Rows that the cache does not have are left as they were."""
+    out = [(t, what, _rows(t, what, kv.dtype, kv.Hkv)) for t, what in ((k_out, "k_out"), (v_out, "v_out")) if t is not None]
+    if not out:
+        raise ValueError("neither k_out nor v_out is given")
+    n = out[0][2][2][3]
+    for _, what, (_, _, shape) in out:
+        _like(shape, kv, n, what)
+    args = [x for t in (k_out, v_out) for x in ((None, None) if t is None else next(r[:2] for u, _, r in out if u is t))]
+    st = _on(kv.device, stream, k_out, v_out)
+    _call("mpc_paged_read", lib().mpc_paged_read, kv.device, kv.dims(kv.Hkv), kv.ref, n, _batch_ints(n_valid, "n_valid", kv.B, kv.device),
+          _batch_ints(first, "first", kv.B, kv.device), *args, st)
 
 
 def paged_attn_workspace_bytes(q, kv):

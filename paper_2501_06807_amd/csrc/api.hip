@@ -181,7 +181,7 @@ mpc_status check_pages(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new)
   if (n_new <= 0 || n_new > mpc::kMaxRows) return fail(MPC_EINVAL, "n_new %d not in [1, 2^30]", n_new);
   if ((int64_t)n_new * G > mpc::kMaxRows) return fail(MPC_EUNSUPPORTED, "more than 2^30 query rows to a kv head");
   if (kv->n_pages <= 0 || kv->max_pages <= 0) return fail(MPC_EINVAL, "n_pages and max_pages must be positive");
-  if (kv->format != MPC_PAGE_SAME && kv->format != MPC_PAGE_E4M3) return fail(MPC_EINVAL, "unknown page format %d", kv->format);
+  if (kv->format != MPC_PAGE_SAME && kv->format != MPC_PAGE_E4M3 && kv->format != MPC_PAGE_MX4) return fail(MPC_EINVAL, "unknown page format %d", kv->format);
   const int p = kv->page_size;
   if (p != 16 && p != 32 && p != 64 && p != 128 && p != 256)
     return fail(MPC_EUNSUPPORTED, "page_size %d not in {16, 32, 64, 128, 256}", p);
@@ -197,17 +197,23 @@ mpc::PagedPlan plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n) {
 mpc_status paged_cache(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid, mpc::PagedCache* c) {
   mpc_status s = check_pages(d, kv, n_new);
   if (s != MPC_OK) return s;
-  const bool codes = kv->format == MPC_PAGE_E4M3;
+  const bool codes = kv->format == MPC_PAGE_E4M3, codes4 = kv->format == MPC_PAGE_MX4;
   if (!kv->k_pages || !kv->v_pages || !kv->table || !kv->lens)
     return fail(MPC_EINVAL, "a required pointer of the paged cache is NULL");
   if (codes && (!kv->k_scale || !kv->v_scale || !kv->k_tail || !kv->v_tail))
     return fail(MPC_EINVAL, "8-bit pages need scales and tails");
+  if (codes4 && (!kv->k_scale || !kv->v_scale)) return fail(MPC_EINVAL, "4-bit pages need scales");
   if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages) || (codes && (!aligned16(kv->k_tail) || !aligned16(kv->v_tail))))
     return fail(MPC_EINVAL, "the paged cache's pages and tails must be 16-byte aligned");
+  if (codes4 && (!aligned16(kv->k_scale) || !aligned16(kv->v_scale)))
+    return fail(MPC_EINVAL, "the scales of 4-bit pages must be 16-byte aligned");
   c->k = (char*)kv->k_pages;
   c->v = (char*)kv->v_pages;
-  c->ks = codes ? kv->k_scale : nullptr;
-  c->vs = codes ? kv->v_scale : nullptr;
+  c->ks = codes ? (float*)kv->k_scale : nullptr;
+  c->vs = codes ? (float*)kv->v_scale : nullptr;
+  c->kx = codes4 ? (uint8_t*)kv->k_scale : nullptr;
+  c->vx = codes4 ? (uint8_t*)kv->v_scale : nullptr;
+  c->format = kv->format;
   c->k_tail = codes ? (char*)kv->k_tail : nullptr;
   c->v_tail = codes ? (char*)kv->v_tail : nullptr;
   c->table = kv->table;
@@ -883,6 +889,23 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
   a.np = (n_new + kv->page_size - 2) / kv->page_size + 1;
   clear_stale_error();
   if ((s = launched(mpc::launch_paged_append(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged append")) != MPC_OK)
+    return s;
+  return ok();
+}
+
+mpc_status mpc_paged_read(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n, const int32_t* n_valid,
+                          const int32_t* first, void* k_out, const mpc_strides* k_strides, void* v_out,
+                          const mpc_strides* v_strides, void* stream) {
+  mpc_status s = check_dims(dims);
+  if (s != MPC_OK) return s;
+  mpc::PagedReadArgs a{};
+  if ((s = paged_cache(dims, kv, n, n_valid, &a.c)) != MPC_OK) return s;
+  if (!k_out && !v_out) return fail(MPC_EINVAL, "k_out and v_out are both NULL");
+  if (k_out && (s = rows_of(dims, "k_out", k_out, k_strides, dims->n_kv_heads, n, true, &a.k)) != MPC_OK) return s;
+  if (v_out && (s = rows_of(dims, "v_out", v_out, v_strides, dims->n_kv_heads, n, true, &a.v)) != MPC_OK) return s;
+  a.first = first;
+  clear_stale_error();
+  if ((s = launched(mpc::launch_paged_read(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged read")) != MPC_OK)
     return s;
   return ok();
 }

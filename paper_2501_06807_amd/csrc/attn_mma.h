@@ -35,6 +35,17 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2_t));
 }
 
+// fp16 values as the sum of two bf16 ones, 8 places and the 3 that they leave (exact; what is not finite is in the first).
+__device__ __forceinline__ void split_bf16(uint4& x, uint4& rest) {
+  float f[8], hi[8];
+  unpack<F16>(x, f);
+  x = make_uint4(pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7]));
+  unpack<BF16>(x, hi);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = fabsf(hi[i]) < INFINITY ? f[i] - hi[i] : 0.f;
+  rest = make_uint4(pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7]));
+}
+
 // Codes HI, HI + 1 of a word as a pair of the 16-bit type (exact: both hold every e4m3 value).
 template <class DT, bool HI>
 __device__ __forceinline__ uint32_t widen2(uint32_t w) {

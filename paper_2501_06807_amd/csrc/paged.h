@@ -5,6 +5,7 @@
 namespace mpc {
 
 constexpr int kMaxRows = 1 << 30;  // rows of a sequence, and new tokens of a call
+constexpr int kMx4Block = 32;      // channels to a scale of 4-bit codes
 
 // A tensor [L][B][H][n][d]: byte strides of the first four axes.
 struct Rows {
@@ -18,10 +19,11 @@ struct Rows {
 // The cache of a call, with the sequence lengths and the new tokens of each sequence.
 struct PagedCache {
   char *k, *v;            // pages
-  float *ks, *vs;         // page scales, or null
+  float *ks, *vs;         // page scales (8-bit codes), or null
+  uint8_t *kx, *vx;       // exponents of a row's scales (4-bit codes), or null
   char *k_tail, *v_tail;  // rings, or null
   const int32_t *table, *lens, *n_valid;
-  int page, log_page, n_pages, max_pages;
+  int page, log_page, n_pages, max_pages, format;
   int L, B, Hkv, n_new;
 
   __device__ int cap() const { return max_pages * page; }
@@ -44,6 +46,14 @@ struct PagedAppendArgs {
   int np;        // pages that the new tokens of one sequence can touch
 };
 hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int D, hipStream_t st);
+
+// Rows first[b] + t (null: the newest ones) of the cache, as rows of the element type.
+struct PagedReadArgs {
+  PagedCache c;
+  const int32_t* first;
+  Rows k, v;  // p null: not asked for
+};
+hipError_t launch_paged_read(const PagedReadArgs& a, int dtype, int D, hipStream_t st);
 
 struct AttnArgs {
   Rows q, out;
@@ -77,6 +87,7 @@ PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int
 hipError_t launch_paged_attn_fp32(const PagedAttnArgs& a, int D, hipStream_t st);
 hipError_t launch_paged_attn_fp16(const PagedAttnArgs& a, int D, hipStream_t st);
 hipError_t launch_paged_attn_bf16(const PagedAttnArgs& a, int D, hipStream_t st);
+hipError_t launch_paged_attn_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 
 struct PromptAttnArgs : AttnArgs {

@@ -28,6 +28,7 @@ PagedPlan paged_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st) {
+  if (a.c.format == MPC_PAGE_MX4) return launch_paged_attn_mx4(a, dtype, D, st);
   if (dtype == MPC_FP32) return launch_paged_attn_fp32(a, D, st);
   return dtype == MPC_FP16 ? launch_paged_attn_fp16(a, D, st) : launch_paged_attn_bf16(a, D, st);
 }

@@ -4,7 +4,7 @@
 namespace mpc {
 
 hipError_t launch_paged_attn_bf16(const PagedAttnArgs& a, int D, hipStream_t st) {
-  return dev::launch_paged_dtype<BF16>(a, D, st);
+  return a.c.format == MPC_PAGE_E4M3 ? dev::launch_paged_format<BF16, MPC_PAGE_E4M3>(a, D, st) : dev::launch_paged_format<BF16, MPC_PAGE_SAME>(a, D, st);
 }
 
 }  // namespace mpc

@@ -35,30 +35,37 @@ namespace mpc {
 namespace dev {
 
 
-template <class DT, int D, bool CODES, int RT>
+template <class DT, int D, int FMT, int RT>
 struct PagedTile {
   static constexpr bool F = DT::kElt == 4;
+  static constexpr bool C8 = FMT == MPC_PAGE_E4M3, C4 = FMT == MPC_PAGE_MX4;  // codes of 8 bits, or of 4
   static constexpr int TK = F ? 16 : 32;       // keys of a tile
   static constexpr int HALVES = TK / 16;       // 16-key halves, each inside one page
   static constexpr int NT = D / 16;            // 16-channel tiles of the output; channel (4 g + r) * NT + t in tile t
   static constexpr int KB = F ? 4 : 2;         // element bytes
-  static constexpr int RB = D * (CODES ? 1 : KB);          // bytes of a page's row
-  static constexpr int KL = RB / 64;           // 16-byte loads of a lane's key row (four lanes to a row)
+  static constexpr int RB = C4 ? D / 2 : D * (C8 ? 1 : KB);  // bytes of a page's row
+  static constexpr int KL = RB < 64 ? 1 : RB / 64;  // 16-byte loads of a lane's key row (four lanes to a row; 8 bytes where a row has 32)
   static constexpr int KLT = D * KB / 64;      // the same of a tail row
   static constexpr int VK = F ? 4 : 8;         // keys of a lane's value rows
   static constexpr int VWT = NT * KB / 4;      // words of a lane's piece of a tail row
-  static constexpr int VW = NT * (CODES ? 1 : KB) / 4;     // and of a page's row
+  static constexpr int VW = C4 ? 1 : NT * (C8 ? 1 : KB) / 4;  // and of a page's row (4 bits, d 64: half a word)
+  static constexpr int SB = D / kMx4Block;     // 4 bits: scales of a row
+  // Type of the values' product, and of the scores' with 4-bit codes: what holds every code times its scale. fp16 does not,
+  // so its queries are multiplied in two bf16 parts (exact: 8 + 3 places), the second part's frags behind the first's.
+  using PV = std::conditional_t<C4 && !F, BF16, DT>;
+  static constexpr bool SPLIT = C4 && DT::kCode == MPC_FP16;
   // queries: 16-bit frags of 32 channels, or fp32 words of 4
-  static constexpr int QF = F ? D / 4 : D / 32;
+  static constexpr int QF = F ? D / 4 : D / 32, QN = SPLIT ? 2 * QF : QF;
   using QFrag = std::conditional_t<F, float, uint4>;
   // fp16: exponents of the weights are lifted by this (also in the sum), and page scales applied to products
-  static constexpr bool H = DT::kCode == MPC_FP16;
+  static constexpr bool H = PV::kCode == MPC_FP16;
   static constexpr float LIFT = H ? 14.f : 0.f;
 
   // First channel of query fragment i of lane group g (fp32: of word i).
   __device__ static int q_channel(int i, int g) {
-    if constexpr (F) return CODES ? i / 16 * 64 + g * 16 + i % 16 : i / 4 * 16 + g * 4 + i % 4;
-    return CODES ? i / 2 * 64 + g * 16 + i % 2 * 8 : i * 32 + g * 8;
+    if constexpr (C4) return g * (D / 4) + i * (F ? 1 : 8);
+    if constexpr (F) return C8 ? i / 16 * 64 + g * 16 + i % 16 : i / 4 * 16 + g * 4 + i % 4;
+    return C8 ? i / 2 * 64 + g * 16 + i % 2 * 8 : i * 32 + g * 8;
   }
   // Key (of the tile) of value place j of lane group g.
   __device__ static int v_key(int j, int g) { return j < 4 ? 4 * g + j : 16 + 4 * g + j - 4; }
@@ -85,11 +92,11 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 }
 
 // The state of a wave's rows: column c of each 16-row tile is a query row.
-template <class DT, int D, bool CODES, int RT>
+template <class DT, int D, int FMT, int RT>
 struct PagedWave {
-  using TL = PagedTile<DT, D, CODES, RT>;
-  static constexpr bool F = TL::F;
-  typename TL::QFrag q[RT][TL::QF];
+  using TL = PagedTile<DT, D, FMT, RT>;
+  static constexpr bool F = TL::F, C8 = TL::C8, C4 = TL::C4, CODES = C8 || C4;
+  typename TL::QFrag q[RT][TL::QN];
   f32x4 o[RT][TL::NT];
   float m[RT], l[RT];  // running maximum of the column; sum over this lane's keys
   int pos[RT];         // position of the column's row, or one that sees nothing
@@ -104,9 +111,9 @@ struct PagedWave {
     }
   }
 
-  // s += K Q^T of one tile: keys in the rows, query rows in the columns.
+  // s += K Q^T of one tile: keys in the rows, query rows in the columns. kx: scale bytes of this lane's codes (4 bits).
   template <bool TAIL>
-  __device__ __forceinline__ void scores(const uint4 (*k)[TAIL ? TL::KLT : TL::KL], f32x4 (*s)[TL::HALVES]) const {
+  __device__ __forceinline__ void scores(const uint4 (*k)[TAIL ? TL::KLT : TL::KL], f32x4 (*s)[TL::HALVES], const uint32_t* kx = nullptr) const {
 #pragma unroll
     for (int h = 0; h < TL::HALVES; ++h) {
 #pragma unroll
@@ -123,7 +130,15 @@ struct PagedWave {
           const uint32_t w[4] = {k[h][i].x, k[h][i].y, k[h][i].z, k[h][i].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if constexpr (CODES && !TAIL) {
+            if constexpr (C4) {
+              if (e >= D / 32) continue;  // (d 64: two words)
+              float x[8];
+              decode8(w[e], mx4_scale(kx[h]), x);
+#pragma unroll
+              for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) y[rt][(8 * e + n) / (D / 16)] = mma(x[n], q[rt][8 * e + n], y[rt][(8 * e + n) / (D / 16)]);
+            } else if constexpr (C8 && !TAIL) {
               float x[4];
               decode4(w[e], x);
 #pragma unroll
@@ -138,7 +153,19 @@ struct PagedWave {
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][h] = (y[rt][0] + y[rt][1]) + (y[rt][2] + y[rt][3]);
-      } else if constexpr (CODES && !TAIL) {
+      } else if constexpr (C4) {
+        const uint32_t w[4] = {k[h][0].x, k[h][0].y, k[h][0].z, k[h][0].w};
+        const float scale = mx4_scale(kx[h]);
+#pragma unroll
+        for (int i = 0; i < TL::QF; ++i) {
+          const uint4 x = widen8(w[i], scale);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            if constexpr (TL::SPLIT) s[rt][h] = mma<BF16>(x, q[rt][TL::QF + i], s[rt][h]);
+            s[rt][h] = mma<BF16>(x, q[rt][i], s[rt][h]);
+          }
+        }
+      } else if constexpr (C8 && !TAIL) {
 #pragma unroll
         for (int i = 0; i < TL::KL; ++i) {
           const uint4& x = k[h][i];
@@ -229,12 +256,22 @@ struct PagedWave {
     }
   }
 
-  // Value rows as 16-bit operands, one for each channel tile: the places of a channel side by side.
+  // Value rows as 16-bit operands, one for each channel tile: the places of a channel side by side. vx: the scale bytes of
+  // four keys of each half (4 bits).
   template <bool TAIL>
-  __device__ static __forceinline__ void operands(const uint32_t (*v)[TAIL ? TL::VWT : TL::VW], uint32_t (*w)[4]) {
+  __device__ static __forceinline__ void operands(const uint32_t (*v)[TAIL ? TL::VWT : TL::VW], uint32_t (*w)[4], const uint32_t* vx = nullptr) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      if constexpr (CODES && !TAIL) {
+      if constexpr (C4) {
+        const float sa = mx4_scale(vx[p / 2] >> 16 * (p % 2)), sb = mx4_scale(vx[p / 2] >> (16 * (p % 2) + 8));
+        const uint4 a = widen8(v[2 * p][0], sa), b = widen8(v[2 * p + 1][0], sb);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int n = 0; n < TL::NT / 2; ++n) {
+          w[2 * n][p] = __builtin_amdgcn_perm(y[n], x[n], 0x05040100u);
+          w[2 * n + 1][p] = __builtin_amdgcn_perm(y[n], x[n], 0x07060302u);
+        }
+      } else if constexpr (C8 && !TAIL) {
 #pragma unroll
         for (int i = 0; i < TL::VW; ++i) {
           const uint32_t a = v[2 * p][i], b = v[2 * p + 1][i];
@@ -256,10 +293,15 @@ struct PagedWave {
   }
   // Value rows as fp32 operands.
   template <bool TAIL>
-  __device__ static __forceinline__ void operands(const uint32_t (*v)[TAIL ? TL::VWT : TL::VW], float (*x)[TL::NT]) {
+  __device__ static __forceinline__ void operands(const uint32_t (*v)[TAIL ? TL::VWT : TL::VW], float (*x)[TL::NT], const uint32_t* vx = nullptr) {
 #pragma unroll
     for (int j = 0; j < TL::VK; ++j) {
-      if constexpr (CODES && !TAIL) {
+      if constexpr (C4) {
+        float y[8];
+        decode8(v[j][0], mx4_scale(vx[j / 4] >> 8 * (j % 4)), y);
+#pragma unroll
+        for (int i = 0; i < TL::NT; ++i) x[j][i] = y[i];
+      } else if constexpr (C8 && !TAIL) {
 #pragma unroll
         for (int i = 0; i < TL::VW; ++i) decode4(v[j][i], x[j] + 4 * i);
       } else {
@@ -276,7 +318,7 @@ struct PagedWave {
   // scale: factors of the halves' products, or null.
   __device__ __forceinline__ void add_values(uint32_t (*w)[4], const float (*p)[TL::VK], const AttnArgs& a, bool edge, int k0,
                                              int rows, const bool* have, int lo, int hi, const float* scale) {
-    using PV = DT;
+    using PV = typename TL::PV;
     const int g = (threadIdx.x % kWave) / 16;
     if (edge) {
 #pragma unroll
@@ -400,9 +442,10 @@ struct PagedWave {
   }
 };
 
-template <class DT, int D, bool CODES, int RT>
+template <class DT, int D, int FMT, int RT>
 __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAttnArgs a) {
-  using TL = PagedTile<DT, D, CODES, RT>;
+  using TL = PagedTile<DT, D, FMT, RT>;
+  constexpr bool C8 = TL::C8, C4 = TL::C4;
   constexpr int NT = TL::NT, RW = 16 * RT, NW = paged_waves(RT), THREADS = NW * kWave;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
@@ -424,7 +467,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     s.rows = min(s.len, c.cap());
     s.start = s.len - s.valid;
     s.groups = ((s.valid << a.log_g) + RW - 1) / RW;
-    s.full = CODES ? s.rows & ~(c.page - 1) : s.rows;
+    s.full = C8 ? s.rows & ~(c.page - 1) : s.rows;
     const int all = (s.full + TL::TK - 1) / TL::TK;
     s.skip = all;
     s.at = all;
@@ -483,7 +526,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     base += __builtin_amdgcn_readlane(sum, kWave - 1);
   }
 
-  PagedWave<DT, D, CODES, RT> w;
+  PagedWave<DT, D, FMT, RT> w;
   unsigned x = first;
   while (x < last) {
     while (x >= base + blocks_of(s)) {
@@ -517,24 +560,40 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     auto place = [&](int i, int hf, int id) {
       return page_unit(c, l, max(id, 0), h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
     };
-    auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks) {
+    // scale byte of block `blk` of a half's first row (4 bits)
+    auto mx4_at = [&](const uint8_t* x, size_t row, int blk) {
+      return x + (row >> c.log_page) * (size_t)(TL::SB * c.page) + blk * c.page + (row & (c.page - 1));
+    };
+    auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks, uint32_t* kx) {
 #pragma unroll
       for (int hf = 0; hf < TL::HALVES; ++hf) {
         const size_t row = place(i, hf, id[hf]);
-        const char* p = c.k + row * TL::RB + col * TL::RB + g * 16;
+        const char* p = c.k + row * TL::RB + col * TL::RB + g * (TL::RB < 64 ? 8 : 16);
+        if constexpr (TL::RB < 64) {
+          const uint2 x = *(const uint2*)p;
+          k[hf][0] = make_uint4(x.x, x.y, 0, 0);
+        } else {
 #pragma unroll
-        for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
-        if constexpr (CODES) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
+          for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
+        }
+        if constexpr (C8) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
+        if constexpr (C4) kx[hf] = mx4_at(c.kx, row, g * TL::SB / 4)[col];
       }
     };
-    auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs) {
+    auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs, uint32_t* vx) {
 #pragma unroll
       for (int hf = 0; hf < TL::HALVES; ++hf) {
         const size_t row = place(i, hf, id[hf]);
-        const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::VW * 4);
+        const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::RB / 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
-        if constexpr (CODES) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (TL::RB < 64)
+            v[4 * hf + j][0] = *(const uint16_t*)(p + j * TL::RB);
+          else
+            load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
+        }
+        if constexpr (C8) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
+        if constexpr (C4) vx[hf] = *(const uint32_t*)(mx4_at(c.vx, row, col * TL::SB / 16) + 4 * g);
       }
     };
     using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
@@ -560,6 +619,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
           for (int i = 0; i < TL::QF; ++i) {
             const uint4 y = ldg16(row + TL::q_channel(i, g) * 2);
             w.q[rt][i] = ok ? y : make_uint4(0, 0, 0, 0);
+            if constexpr (TL::SPLIT) split_bf16(w.q[rt][i], w.q[rt][TL::QF + i]);
           }
         }
       }
@@ -572,11 +632,12 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       uint4 k[TL::HALVES][TL::KL];
       uint32_t v[TL::VK][TL::VW];
       float ks[TL::HALVES], vs[TL::HALVES];
+      uint32_t kx[TL::HALVES], vx[TL::HALVES];
       int id[TL::HALVES], next[TL::HALVES], entry[TL::HALVES];
       entries_of(i, entry);
       ids_of(i, entry, id);
-      load_k(i, id, k, ks);
-      load_v(i, id, v, vs);
+      load_k(i, id, k, ks, kx);
+      load_v(i, id, v, vs, vx);
       load_queries();
       auto after = [&](int n) { return n + NW < i_end ? n + NW : n; };
       entries_of(after(i), entry);
@@ -593,23 +654,23 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         }
         const bool edge = !(all && k1 < s.full && k1 <= lo && (!a.window || k0 > hi - a.window || k1 < a.sinks));
         f32x4 sr[RT][TL::HALVES];
-        w.template scores<false>(k, sr);
+        w.template scores<false>(k, sr, kx);
 #pragma unroll
         for (int hf = 0; hf < TL::HALVES; ++hf) {
-          sc[hf] = CODES ? (have[hf] ? a.qscale * ks[hf] : 0.f) : a.qscale;
-          vf[hf] = CODES ? (have[hf] ? vs[hf] : 0.f) : 1.f;
+          sc[hf] = C8 ? (have[hf] ? a.qscale * ks[hf] : 0.f) : a.qscale;
+          vf[hf] = C8 ? (have[hf] ? vs[hf] : 0.f) : 1.f;
         }
         ids_of(i1, entry, next);
-        load_k(i1, next, k, ks);
+        load_k(i1, next, k, ks, kx);
         entries_of(after(i1), entry);
         float p[RT][TL::VK];
-        w.weights(sr, sc, CODES && !TL::H ? vf : nullptr, a, edge, k0, s.full, have, p);
+        w.weights(sr, sc, C8 && !TL::H ? vf : nullptr, a, edge, k0, s.full, have, p);
         Operand x;
-        w.template operands<false>(v, x);
-        load_v(i1, next, v, vs);
+        w.template operands<false>(v, x, vx);
+        load_v(i1, next, v, vs, vx);
 #pragma unroll
         for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
-        w.add_values(x, p, a, edge, k0, s.full, have, lo, hi, CODES && TL::H ? vf : nullptr);
+        w.add_values(x, p, a, edge, k0, s.full, have, lo, hi, C8 && TL::H ? vf : nullptr);
         if (i1 == i) break;
         i = i1;
       }
@@ -617,7 +678,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     else {
       load_queries();
     }
-    if constexpr (CODES) {
+    if constexpr (C8) {
       // rows of the page that is not complete, from the ring
       const int t_end = blk_end * NW;
       int n = blk * NW + wave;
@@ -837,21 +898,16 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
   }
 }
 
-template <class DT, int D, bool CODES, int RT>
+template <class DT, int D, int FMT, int RT>
 hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_attn<DT, D, CODES, RT>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
   return hipGetLastError();
 }
 
-template <class DT>
-hipError_t launch_paged_dtype(const PagedAttnArgs& a, int D, hipStream_t st) {
-  const bool codes = a.c.ks != nullptr;
-  if (a.row_tiles == 1) {
-    if (D == 64) return codes ? launch_paged<DT, 64, true, 1>(a, st) : launch_paged<DT, 64, false, 1>(a, st);
-    return codes ? launch_paged<DT, 128, true, 1>(a, st) : launch_paged<DT, 128, false, 1>(a, st);
-  }
-  if (D == 64) return codes ? launch_paged<DT, 64, true, 2>(a, st) : launch_paged<DT, 64, false, 2>(a, st);
-  return codes ? launch_paged<DT, 128, true, 2>(a, st) : launch_paged<DT, 128, false, 2>(a, st);
+template <class DT, int FMT>
+hipError_t launch_paged_format(const PagedAttnArgs& a, int D, hipStream_t st) {
+  if (a.row_tiles == 1) return D == 64 ? launch_paged<DT, 64, FMT, 1>(a, st) : launch_paged<DT, 128, FMT, 1>(a, st);
+  return D == 64 ? launch_paged<DT, 64, FMT, 2>(a, st) : launch_paged<DT, 128, FMT, 2>(a, st);
 }
 
 }  // namespace dev

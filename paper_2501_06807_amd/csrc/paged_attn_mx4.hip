@@ -1,0 +1,12 @@
+// Paged attention kernels of caches of 4-bit codes.
+#include "paged_attn_dev.h"
+
+namespace mpc {
+
+hipError_t launch_paged_attn_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st) {
+  if (dtype == MPC_FP32) return dev::launch_paged_format<F32, MPC_PAGE_MX4>(a, D, st);
+  if (dtype == MPC_FP16) return dev::launch_paged_format<F16, MPC_PAGE_MX4>(a, D, st);
+  return dev::launch_paged_format<BF16, MPC_PAGE_MX4>(a, D, st);
+}
+
+}  // namespace mpc

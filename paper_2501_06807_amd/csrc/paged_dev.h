@@ -19,6 +19,44 @@ __device__ __forceinline__ void decode4(uint32_t w, float* out) {
   out[3] = hi[1];
 }
 
+// Codes of 4 bits (e2m1), eight channels to a word, the even one of a byte low; scale: 2^e, of which the conversions take the
+// exponent (all ones: NaN, as the scale byte 255 says).
+__device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_float((byte & 255u) << 23); }
+__device__ __forceinline__ void decode8(uint32_t w, float scale, float* out) {
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+  const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+  out[0] = a[0];
+  out[1] = a[1];
+  out[2] = b[0];
+  out[3] = b[1];
+  out[4] = c[0];
+  out[5] = c[1];
+  out[6] = d[0];
+  out[7] = d[1];
+}
+// The same as bf16 pairs (exact: bf16 holds every code at every scale).
+__device__ __forceinline__ uint4 widen8(uint32_t w, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+}
+
+// Codes of eight values in units of their scale: to nearest, halves to even codes, what is beyond 6 to 6.
+__device__ __forceinline__ uint32_t encode8(const float* x) {
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0], x[1], 1.f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], 1.f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], 1.f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], 1.f, 3);
+}
+// Exponent s of a block's scale 2^s: the least with amax <= 6 * 2^s = 1.5 * 2^(s + 2), off the bits of amax, up to 125 (6 * 2^126
+// is no fp32 value).
+__device__ __forceinline__ int mx4_exponent(uint32_t amax_bits) {
+  if (amax_bits == 0) return 0;
+  const int s = (int)(amax_bits >> 23) - 127 - 2 + ((amax_bits & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  return min(max(s, -126), 125);
+}
+
 // Exponent s of a page's scale 2^s: the least with amax <= 448 * 2^s = 1.75 * 2^(s + 8), read off the bits of amax.
 __device__ __forceinline__ int scale_exponent(uint32_t amax_bits) {
   if (amax_bits == 0) return 0;
