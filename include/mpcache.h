@@ -13,7 +13,8 @@
  *   - appending new tokens' keys and values to a paged cache, rotated by their positions, in the
  *     element type, in 8 bits with a scale for each page and head, or in 4 bits with a scale for each 32
  *     channels of a row (mpc_paged_append), and reading rows back (mpc_paged_read);
- *   - attention of one or more new tokens over such a cache (mpc_paged_attn);
+ *   - attention of one or more new tokens over such a cache (mpc_paged_attn), for sequences that share
+ *     their first rows with these read once for all of them (mpc_shared_attn);
  *   - attention of a prompt's rows over its keys (mpc_prompt_attn);
  *   both with an optional sliding window and first tokens that stay visible.
  * mpc_prefill runs the first two steps as one call; mpc_decode_step runs selection and attention
@@ -168,13 +169,15 @@ enum {
   MPC_OP_SELECT = 1,
   MPC_OP_DECODE_ATTN = 2,
   MPC_OP_DECODE_STEP = 3,
-  MPC_OP_PAGED_ATTN = 4
+  MPC_OP_PAGED_ATTN = 4,
+  MPC_OP_SHARED_ATTN = 5
 };
 
 /* Workspace bytes needed by `op` (MPC_OP_*) for these dims. `T_or_Ts` is T for static eviction, n_new
  * for the paged attention and Ts otherwise; `cfg` points to the op's config struct (mpc_evict_cfg for
  * static eviction, mpc_select_cfg for selection and the decode step, mpc_paged_kv, of which only the
- * sizes are read, for the paged attention) or is NULL for MPC_OP_DECODE_ATTN. Returns 0
+ * sizes are read, for the paged attention, mpc_shared_sizes for the attention behind shared rows) or is NULL for
+ * MPC_OP_DECODE_ATTN. `T_or_Ts` is n_new there too. Returns 0
  * when the op needs no workspace or the arguments are invalid. The size for static eviction never falls
  * with a dimension, T or the window, so one made for the longest prompt serves the shorter ones. */
 size_t mpc_workspace_bytes(int32_t op, const mpc_dims* dims, int32_t T_or_Ts, const void* cfg);
@@ -420,6 +423,33 @@ mpc_status mpc_paged_read(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
 mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                           const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides, void* out,
                           const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Sequences whose first rows are the same (a batch behind one prompt), as groups of neighbours in the batch: group g is the
+ * sequences first[g] <= b < first[g + 1], and rows[g], rounded down to whole pages, is the number of rows that they share. The
+ * arrays lie on the device. Values of `first` are brought into [0, B] and in order (each at least the one before it);
+ * a sequence outside all groups shares nothing. */
+typedef struct {
+  int32_t n_groups;      /* 1 to min(B, 1024) */
+  const int32_t* first;  /* [n_groups + 1]    */
+  const int32_t* rows;   /* [n_groups]        */
+} mpc_shared;
+typedef struct {
+  const mpc_paged_kv* kv; /* only the sizes are read */
+  int32_t n_groups;
+} mpc_shared_sizes;
+
+/* mpc_paged_attn, with the shared rows of a group read once for all its sequences, through the table of the group's first
+ * sequence and from its pages (with MPC_PAGE_E4M3 these have to be complete; the others' tables are not read for
+ * them). What a row sees, its weights, empty rows, NaN and lse are as there; so are the outputs, up to the
+ * roundings of another order of summation.
+ * ws: mpc_workspace_bytes(MPC_OP_SHARED_ATTN, dims, n_new, &sizes) bytes, zero-filled before its first use; every completed
+ * call leaves it ready for the next, of this or any other sizes whose bytes it has, and for mpc_paged_attn (calls sharing
+ * it must not overlap). The sizes, not the lengths or the groups' contents, give the launches, so a captured call follows
+ * lengths, tables and groups as they change.
+ * Limits: those of mpc_paged_attn, B * n_new * G <= 2^30. */
+mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                           const mpc_shared* shared, const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides,
+                           void* out, const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* The same attention of a prompt's rows over its keys, in plain tensors: row t of sequence b stands at
  * position k_lens[b] - q_lens[b] + t and sees keys 0 <= j < k_lens[b] as cfg names them; q_lens / k_lens

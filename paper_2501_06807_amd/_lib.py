@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmpcache.so")
 
 MPC_OK, MPC_EINVAL, MPC_ESHAPE, MPC_EUNSUPPORTED, MPC_EWORKSPACE, MPC_EHIP = range(6)
-MPC_OP_STATIC_EVICT, MPC_OP_SELECT, MPC_OP_DECODE_ATTN, MPC_OP_DECODE_STEP, MPC_OP_PAGED_ATTN = range(5)
+MPC_OP_STATIC_EVICT, MPC_OP_SELECT, MPC_OP_DECODE_ATTN, MPC_OP_DECODE_STEP, MPC_OP_PAGED_ATTN, MPC_OP_SHARED_ATTN = range(6)
 DTYPE_CODE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -54,6 +54,14 @@ class MpcAttnCfg(ctypes.Structure):
     _fields_ = [("sm_scale", ctypes.c_float), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
+class MpcShared(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("first", ctypes.c_void_p), ("rows", ctypes.c_void_p)]
+
+
+class MpcSharedSizes(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(MpcPagedKv)), ("n_groups", ctypes.c_int32)]
+
+
 class MpcError(RuntimeError):
     def __init__(self, fn, status, msg):
         super().__init__(f"{fn}: status {status} ({msg})")
@@ -64,7 +72,7 @@ _LIB = None
 EXPORTS = ("mpc_workspace_bytes", "mpc_static_evict", "mpc_static_evict_noalloc", "mpc_static_evict_noalloc_limit",
            "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters",
            "mpc_sparse_decode_attn", "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality",
-           "mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_prompt_attn", "mpc_owner_layer",
+           "mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_shared_attn", "mpc_prompt_attn", "mpc_owner_layer",
            "mpc_status_string", "mpc_last_error")
 
 
@@ -96,8 +104,9 @@ def lib():
         L.mpc_paged_append.argtypes = [P(MpcDims), KV, I, V, P(MpcRope), V] + [V, S] * 5 + [V]
         L.mpc_paged_read.argtypes = [P(MpcDims), KV, I, V, V] + [V, S] * 2 + [V]
         L.mpc_paged_attn.argtypes = [P(MpcDims), KV, I, V, A] + [V, S] * 2 + [V, V, ctypes.c_size_t, V]
+        L.mpc_shared_attn.argtypes = [P(MpcDims), KV, I, V, P(MpcShared), A] + [V, S] * 2 + [V, V, ctypes.c_size_t, V]
         L.mpc_prompt_attn.argtypes = [P(MpcDims), I, I, V, V, A] + [V, S] * 4 + [V, V]
-        for fn in ("mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
+        for fn in ("mpc_paged_append", "mpc_paged_read", "mpc_paged_attn", "mpc_shared_attn", "mpc_prompt_attn", "mpc_static_evict", "mpc_build_clusters", "mpc_prefill", "mpc_select_clusters", "mpc_sparse_decode_attn",
                    "mpc_decode_step", "mpc_decode_step_status", "mpc_append_kv", "mpc_commonality"):
             getattr(L, fn).restype = ctypes.c_int
         L.mpc_owner_layer.argtypes = [I, I, I]
@@ -620,6 +629,36 @@ def mpc_paged_attn(q, kv, out, *, sm_scale, window=0, sinks=0, n_valid=None, lse
     _call("mpc_paged_attn", lib().mpc_paged_attn, kv.device, kv.dims(shape[2]), kv.ref, n,
           _batch_ints(n_valid, "n_valid", kv.B, kv.device), ctypes.byref(cfg), qp, qs, op, os_, _lse_of(lse, shape),
           ws.data_ptr(), ws.numel() * ws.element_size(), st)
+
+
+def shared_attn_workspace_bytes(q, kv, n_groups):
+    """Workspace bytes of mpc_shared_attn for queries shaped like q [L][B][Hq][n][d] (or [L][B][Hq][d]) and that many groups."""
+    sizes = MpcSharedSizes(ctypes.pointer(kv.c), n_groups)
+    return lib().mpc_workspace_bytes(MPC_OP_SHARED_ATTN, kv.dims(q.shape[2]), q.shape[3] if q.dim() == 5 else 1, ctypes.byref(sizes))
+
+
+def mpc_shared_attn(q, kv, out, *, first, shared_rows, sm_scale, window=0, sinks=0, n_valid=None, lse=None, ws=None, stream=None):
+    """mpc_paged_attn for sequences that share their first rows, in groups of neighbours: group g is the sequences first[g] <= b <
+    first[g + 1] (int32 [n_groups + 1] on the device), and their first shared_rows[g] rows (int32 [n_groups]; whole pages of them)
+    are read once for all of them, from the pages of the group's first sequence. ws: from
+    workspace(shared_attn_workspace_bytes(q, kv, n_groups)); it serves mpc_paged_attn too."""
+    qp, qs, shape = _rows(q, "q", kv.dtype)
+    n = shape[3]
+    _like(shape, kv, n, "q")
+    op, os_, oshape = _rows(out, "out", kv.dtype, shape[2])
+    _like(oshape, kv, n, "out")
+    if shared_rows.dim() != 1 or shared_rows.numel() == 0:
+        raise ValueError("shared_rows must be int32 [n_groups]")
+    ng = shared_rows.numel()
+    groups = MpcShared(ng, _batch_ints(first, "first", ng + 1, kv.device), _batch_ints(shared_rows, "shared_rows", ng, kv.device))
+    if ws is None:
+        ws = _call_ws(shared_attn_workspace_bytes(q, kv, ng), kv.device, stream)
+    _contig(ws)
+    st = _on(kv.device, stream, q, out, lse, ws)
+    cfg = _attn_cfg(sm_scale, window, sinks)
+    _call("mpc_shared_attn", lib().mpc_shared_attn, kv.device, kv.dims(shape[2]), kv.ref, n,
+          _batch_ints(n_valid, "n_valid", kv.B, kv.device), ctypes.byref(groups), ctypes.byref(cfg), qp, qs, op, os_,
+          _lse_of(lse, shape), ws.data_ptr(), ws.numel() * ws.element_size(), st)
 
 
 def mpc_prompt_attn(q, k, v, out, *, sm_scale, window=0, sinks=0, q_lens=None, k_lens=None, lse=None, stream=None):

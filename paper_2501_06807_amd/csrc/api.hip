@@ -194,6 +194,19 @@ mpc::PagedPlan plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n) {
                          kv->max_pages * kv->page_size);
 }
 
+mpc_status check_groups(const mpc_dims* d, int32_t n_new, int32_t n_groups) {
+  if (n_groups <= 0 || n_groups > d->batch) return fail(MPC_EINVAL, "n_groups %d not in [1, batch]", n_groups);
+  if (n_groups > mpc::kMaxGroups) return fail(MPC_EUNSUPPORTED, "more than %d groups", mpc::kMaxGroups);
+  if ((int64_t)d->batch * n_new * (d->n_q_heads / d->n_kv_heads) > mpc::kMaxRows)
+    return fail(MPC_EUNSUPPORTED, "more than 2^30 query rows to a kv head");
+  return MPC_OK;
+}
+
+mpc::SharedPlan shared_plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n, int groups) {
+  return mpc::shared_plan(d->dtype, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
+                          kv->max_pages * kv->page_size, groups);
+}
+
 mpc_status paged_cache(const mpc_dims* d, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid, mpc::PagedCache* c) {
   mpc_status s = check_pages(d, kv, n_new);
   if (s != MPC_OK) return s;
@@ -304,6 +317,12 @@ size_t mpc_workspace_bytes(int32_t op, const mpc_dims* dims, int32_t T_or_Ts, co
     const mpc_paged_kv* kv = (const mpc_paged_kv*)cfg;
     if (!kv || check_pages(dims, kv, T_or_Ts) != MPC_OK) return 0;
     const mpc::PagedPlan p = plan_of(dims, kv, T_or_Ts);
+    return p.blocks < ((long long)1 << 31) ? p.ws_bytes : 0;
+  }
+  if (op == MPC_OP_SHARED_ATTN) {
+    const mpc_shared_sizes* z = (const mpc_shared_sizes*)cfg;
+    if (!z || check_pages(dims, z->kv, T_or_Ts) != MPC_OK || check_groups(dims, T_or_Ts, z->n_groups) != MPC_OK) return 0;
+    const mpc::SharedPlan p = shared_plan_of(dims, z->kv, T_or_Ts, z->n_groups);
     return p.blocks < ((long long)1 << 31) ? p.ws_bytes : 0;
   }
   return 0;
@@ -931,6 +950,47 @@ mpc_status mpc_paged_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t 
   a.grid = p.grid;
   clear_stale_error();
   if ((s = launched(mpc::launch_paged_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "paged attention")) != MPC_OK)
+    return s;
+  return ok();
+}
+
+mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
+                           const mpc_shared* shared, const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides,
+                           void* out, const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  mpc_status s = check_dims(dims);
+  if (s != MPC_OK) return s;
+  mpc::PagedAttnArgs a{};
+  if ((s = paged_cache(dims, kv, n_new, n_valid, &a.c)) != MPC_OK) return s;
+  if (!shared || !shared->first || !shared->rows) return fail(MPC_EINVAL, "shared, or one of its pointers, is NULL");
+  if ((s = check_groups(dims, n_new, shared->n_groups)) != MPC_OK) return s;
+  if ((s = attn_args(dims, cfg, n_new, q, q_strides, out, out_strides, lse, &a)) != MPC_OK) return s;
+  const mpc::SharedPlan p = shared_plan_of(dims, kv, n_new, shared->n_groups);
+  if (p.blocks >= ((long long)1 << 31)) return fail(MPC_EUNSUPPORTED, "more than 2^31 key blocks in a call");
+  if (!ws || ws_bytes < p.ws_bytes)
+    return fail(MPC_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, p.ws_bytes);
+  if (!aligned16(ws)) return fail(MPC_EINVAL, "ws must be 16-byte aligned");
+  char* at = (char*)ws;
+  a.cnt = (int*)ws;
+  a.part = (float*)(at + mpc::kPagedCntBytes);
+  a.row_tiles = p.own.row_tiles;
+  a.log_g = __builtin_ctz((unsigned)(dims->n_q_heads / dims->n_kv_heads));
+  a.part_rows = p.own.part_rows;
+  a.grid = p.own.grid;
+  a.sh.first = shared->first;
+  a.sh.rows = shared->rows;
+  a.sh.groups = shared->n_groups;
+  a.sh.total = (unsigned*)(at + p.total);
+  a.sh.plan = (mpc::SharedGroup*)(at + p.plan);
+  a.sh.seq = (int2*)(at + p.seq);
+  a.sh.unit = (int2*)(at + p.unit);
+  a.sh.head = (float*)(at + p.head);
+  a.sh.more = (float*)(at + p.more);
+  a.sh.unit_rows = p.unit_rows;
+  a.sh.grid = p.grid;
+  a.sh.tile = p.tile;
+  a.sh.per_block = p.per_block;
+  clear_stale_error();
+  if ((s = launched(mpc::launch_shared_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "shared attention")) != MPC_OK)
     return s;
   return ok();
 }

@@ -442,10 +442,197 @@ struct PagedWave {
   }
 };
 
+// This lane's pieces of a query row (zeros where there is none).
 template <class DT, int D, int FMT, int RT>
-__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAttnArgs a) {
+__device__ __forceinline__ void load_query_row(PagedWave<DT, D, FMT, RT>& w, int rt, const char* row, bool ok) {
+  using TL = PagedTile<DT, D, FMT, RT>;
+  const int g = (threadIdx.x % kWave) / 16;
+  if constexpr (TL::F) {
+#pragma unroll
+    for (int i = 0; i < TL::QF; i += 4) {
+      const uint4 y = ldg16(row + TL::q_channel(i, g) * 4);
+      w.q[rt][i] = ok ? __uint_as_float(y.x) : 0.f;
+      w.q[rt][i + 1] = ok ? __uint_as_float(y.y) : 0.f;
+      w.q[rt][i + 2] = ok ? __uint_as_float(y.z) : 0.f;
+      w.q[rt][i + 3] = ok ? __uint_as_float(y.w) : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < TL::QF; ++i) {
+      const uint4 y = ldg16(row + TL::q_channel(i, g) * 2);
+      w.q[rt][i] = ok ? y : make_uint4(0, 0, 0, 0);
+      if constexpr (TL::SPLIT) split_bf16(w.q[rt][i], w.q[rt][TL::QF + i]);
+    }
+  }
+}
+
+// The pages' rows that a unit's rows look at, in tiles: [from, from + skip), then from `at` on; keys [base, full) of them.
+struct PageRows {
+  int skip, at, from, base, full;
+};
+
+// A wave's tiles i, i + NW, .. (before i_end) of (sequence b's table, layer l, kv head h), for rows at positions lo .. hi; takes
+// the queries in beside the first loads.
+template <class DT, int D, int FMT, int RT, class Queries>
+__device__ __forceinline__ void walk_pages(PagedWave<DT, D, FMT, RT>& w, const AttnArgs& a, const PagedCache& c, int b, int l, int h,
+                                           const PageRows& r, int i, int i_end, int lo, int hi, Queries load_queries) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr bool C8 = TL::C8, C4 = TL::C4;
+  constexpr int NT = TL::NT, NW = paged_waves(RT);
+  const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
+  auto page_tile = [&](int i) { return i < r.skip ? r.from + i : i - r.skip + r.at; };
+  auto page_at = [&](int i, int hf) { return (page_tile(i) * TL::TK + 16 * hf) >> c.log_page; };
+  // table entries of a tile's halves, and the page ids that they give (-1 where there is none)
+  auto entries_of = [&](int i, int* e) {
+#pragma unroll
+    for (int hf = 0; hf < TL::HALVES; ++hf) e[hf] = page_entry(c, b, page_at(i, hf));
+  };
+  auto ids_of = [&](int i, const int* e, int* id) {
+#pragma unroll
+    for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = page_of_entry(c, e[hf], page_at(i, hf));
+  };
+  // row 0 of a tile's half in the pool (page 0 where it has no page: its rows are not used)
+  auto place = [&](int i, int hf, int id) {
+    return page_unit(c, l, max(id, 0), h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
+  };
+  // scale byte of block `blk` of a half's first row (4 bits)
+  auto mx4_at = [&](const uint8_t* x, size_t row, int blk) {
+    return x + (row >> c.log_page) * (size_t)(TL::SB * c.page) + blk * c.page + (row & (c.page - 1));
+  };
+  auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks, uint32_t* kx) {
+#pragma unroll
+    for (int hf = 0; hf < TL::HALVES; ++hf) {
+      const size_t row = place(i, hf, id[hf]);
+      const char* p = c.k + row * TL::RB + col * TL::RB + g * (TL::RB < 64 ? 8 : 16);
+      if constexpr (TL::RB < 64) {
+        const uint2 x = *(const uint2*)p;
+        k[hf][0] = make_uint4(x.x, x.y, 0, 0);
+      } else {
+#pragma unroll
+        for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
+      }
+      if constexpr (C8) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
+      if constexpr (C4) kx[hf] = mx4_at(c.kx, row, g * TL::SB / 4)[col];
+    }
+  };
+  auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs, uint32_t* vx) {
+#pragma unroll
+    for (int hf = 0; hf < TL::HALVES; ++hf) {
+      const size_t row = place(i, hf, id[hf]);
+      const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::RB / 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (TL::RB < 64)
+          v[4 * hf + j][0] = *(const uint16_t*)(p + j * TL::RB);
+        else
+          load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
+      }
+      if constexpr (C8) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
+      if constexpr (C4) vx[hf] = *(const uint32_t*)(mx4_at(c.vx, row, col * TL::SB / 16) + 4 * g);
+    }
+  };
+  using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
+  if (i < i_end) {
+    // A tile's keys are dead after the scores and its values after the transpose: the next tile's loads go out there,
+    // into the same registers, and are waited for a tile's work later.
+    uint4 k[TL::HALVES][TL::KL];
+    uint32_t v[TL::VK][TL::VW];
+    float ks[TL::HALVES], vs[TL::HALVES];
+    uint32_t kx[TL::HALVES], vx[TL::HALVES];
+    int id[TL::HALVES], next[TL::HALVES], entry[TL::HALVES];
+    entries_of(i, entry);
+    ids_of(i, entry, id);
+    load_k(i, id, k, ks, kx);
+    load_v(i, id, v, vs, vx);
+    load_queries();
+    auto after = [&](int n) { return n + NW < i_end ? n + NW : n; };
+    entries_of(after(i), entry);
+    for (;;) {
+      // the last tile asks for itself again, so that every pass has the same loads in flight and waits for its own only
+      const int i1 = after(i);
+      const int k0 = page_tile(i) * TL::TK, k1 = k0 + TL::TK - 1;
+      bool have[TL::HALVES], all = true;
+      float sc[TL::HALVES], vf[TL::HALVES];
+#pragma unroll
+      for (int hf = 0; hf < TL::HALVES; ++hf) {
+        have[hf] = id[hf] >= 0 && k0 + 16 * hf < r.full && k0 + 16 * hf >= r.base;
+        all = all && have[hf];
+      }
+      const bool edge = !(all && k1 < r.full && k1 <= lo && (!a.window || k0 > hi - a.window || k1 < a.sinks));
+      f32x4 sr[RT][TL::HALVES];
+      w.template scores<false>(k, sr, kx);
+#pragma unroll
+      for (int hf = 0; hf < TL::HALVES; ++hf) {
+        sc[hf] = C8 ? (have[hf] ? a.qscale * ks[hf] : 0.f) : a.qscale;
+        vf[hf] = C8 ? (have[hf] ? vs[hf] : 0.f) : 1.f;
+      }
+      ids_of(i1, entry, next);
+      load_k(i1, next, k, ks, kx);
+      entries_of(after(i1), entry);
+      float p[RT][TL::VK];
+      w.weights(sr, sc, C8 && !TL::H ? vf : nullptr, a, edge, k0, r.full, have, p);
+      Operand x;
+      w.template operands<false>(v, x, vx);
+      load_v(i1, next, v, vs, vx);
+#pragma unroll
+      for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
+      w.add_values(x, p, a, edge, k0, r.full, have, lo, hi, C8 && TL::H ? vf : nullptr);
+      if (i1 == i) break;
+      i = i1;
+    }
+  }
+  else {
+    load_queries();
+  }
+}
+
+// Maxima, sums and accumulators of a workgroup's waves into those of wave 0 (M and Lsum: of every wave).
+template <class DT, int D, int FMT, int RT>
+__device__ __forceinline__ void join_waves(PagedWave<DT, D, FMT, RT>& w, int wave, float (*s_ml)[RT][2][kWave],
+                                           f32x4 (*s_o)[PagedTile<DT, D, FMT, RT>::NT][kWave], float* M, float* Lsum) {
+  constexpr int NT = PagedTile<DT, D, FMT, RT>::NT, NW = paged_waves(RT);
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    s_ml[wave][rt][0][lane] = w.m[rt];
+    s_ml[wave][rt][1][lane] = column_sum(w.l[rt]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    M[rt] = -INFINITY;
+    Lsum[rt] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NW; ++n) M[rt] = fmaxf(M[rt], s_ml[n][rt][0][lane]);
+    const float b0 = M[rt] == -INFINITY ? 0.f : M[rt];
+#pragma unroll
+    for (int n = 0; n < NW; ++n) Lsum[rt] += s_ml[n][rt][1][lane] * fast_exp2(s_ml[n][rt][0][lane] - b0);
+    const float move = fast_exp2(w.m[rt] - b0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) w.o[rt][t] *= move;
+  }
+  // half of the waves to the other half, until one has everything
+#pragma unroll
+  for (int n = NW / 2; n > 0; n /= 2) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      if (wave >= n && wave < 2 * n)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s_o[wave - n][t][lane] = w.o[rt][t];
+      __syncthreads();
+      if (wave < n)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w.o[rt][t] += s_o[wave][t][lane];
+      if (rt + 1 < RT || n > 1) __syncthreads();
+    }
+  }
+}
+
+// SHARED: the first rows of a sequence, up to those that its group shares, are taken elsewhere; their parts are joined here.
+template <class DT, int D, int FMT, int RT, bool SHARED>
+__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAttnArgs a) {
+  using TL = PagedTile<DT, D, FMT, RT>;
+  constexpr bool C8 = TL::C8;
   constexpr int NT = TL::NT, RW = 16 * RT, NW = paged_waves(RT), THREADS = NW * kWave;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
@@ -458,10 +645,14 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
 
   // Work of sequence b: units (layer, kv head, row group) of nb blocks each.
   struct Seq {
-    int valid, len, rows, start, groups, full, tiles, skip, at, nb;  // tiles of pages: [0, skip) and [at, at + tiles - skip)
+    int valid, len, rows, start, groups, full, tiles, skip, at, nb;  // tiles of pages: [from, from + skip) and [at, ..)
+    int from, base, group;  // SHARED: rows [0, base) are the group's
   };
-  auto seq_of = [&](int len, int valid) {
+  auto seq_of = [&](int len, int valid, int2 shared) {
     Seq s;
+    s.base = SHARED ? shared.x : 0;
+    s.group = SHARED ? shared.y : -1;
+    s.from = SHARED ? s.base / TL::TK : 0;
     s.valid = min(max(valid, 0), c.n_new);
     s.len = min(max(len, 0), kMaxRows);
     s.rows = min(s.len, c.cap());
@@ -469,28 +660,34 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     s.groups = ((s.valid << a.log_g) + RW - 1) / RW;
     s.full = C8 ? s.rows & ~(c.page - 1) : s.rows;
     const int all = (s.full + TL::TK - 1) / TL::TK;
-    s.skip = all;
-    s.at = all;
+    s.skip = max(all - s.from, 0);
+    s.at = max(all, s.from);
     if (a.window) {
-      s.skip = min((a.sinks + TL::TK - 1) / TL::TK, all);
-      s.at = max(s.skip, min(max(s.start - a.window + 1, 0) / TL::TK, all));
+      s.skip = max(min((a.sinks + TL::TK - 1) / TL::TK, all) - s.from, 0);
+      s.at = max(s.from + s.skip, min(max(s.start - a.window + 1, 0) / TL::TK, all));
     }
-    s.tiles = s.skip + all - s.at;
-    const int tail = (s.rows - s.full + TL::TK - 1) / TL::TK;
+    s.tiles = s.skip + max(all - s.at, 0);
+    const int tail = s.full < s.base ? 0 : (s.rows - s.full + TL::TK - 1) / TL::TK;
     s.nb = max(1, (s.tiles + tail + NW - 1) / NW);
     return s;
   };
-  auto seq = [&](int b) { return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new); };
+  auto seq = [&](int b) {
+    int2 shared = make_int2(0, -1);
+    if constexpr (SHARED) shared = make_int2(load_uniform(&a.sh.seq[b].x), load_uniform(&a.sh.seq[b].y));
+    return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new, shared);
+  };
   const int per_group = a.L * a.Hkv;
   auto blocks_of = [&](const Seq& s) { return (unsigned)(s.groups * per_group) * (unsigned)s.nb; };
   // all blocks (below 2^31, as the host has checked for the longest sequences), sequences to lanes
   unsigned total = 0, mine = 0;
   int my_len = 0, my_valid = 0;
+  int2 my_shared = make_int2(0, -1);
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const bool in = b0 + lane < a.B;
     my_len = in ? c.lens[b0 + lane] : 0;
     my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
-    mine = blocks_of(seq_of(my_len, my_valid));
+    if constexpr (SHARED) my_shared = in ? a.sh.seq[b0 + lane] : make_int2(0, -1);
+    mine = blocks_of(seq_of(my_len, my_valid, my_shared));
     total += wave_sum(mine);
   }
   total = __builtin_amdgcn_readfirstlane(total);
@@ -507,7 +704,8 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       const bool in = b0 + lane < a.B;
       my_len = in ? c.lens[b0 + lane] : 0;
       my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
-      mine = blocks_of(seq_of(my_len, my_valid));
+      if constexpr (SHARED) my_shared = in ? a.sh.seq[b0 + lane] : make_int2(0, -1);
+      mine = blocks_of(seq_of(my_len, my_valid, my_shared));
     }
     unsigned sum = mine;
 #pragma unroll
@@ -520,7 +718,8 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)past) - 1);
       b = b0 + at;
       base += __builtin_amdgcn_readlane(sum - mine, at);
-      s = seq_of(__builtin_amdgcn_readlane(my_len, at), __builtin_amdgcn_readlane(my_valid, at));
+      s = seq_of(__builtin_amdgcn_readlane(my_len, at), __builtin_amdgcn_readlane(my_valid, at),
+                 make_int2(__builtin_amdgcn_readlane(my_shared.x, at), __builtin_amdgcn_readlane(my_shared.y, at)));
       break;
     }
     base += __builtin_amdgcn_readlane(sum, kWave - 1);
@@ -544,58 +743,6 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     const int lo = s.start + (r0 >> a.log_g), hi = s.start + ((r_end - 1) >> a.log_g);
     w.clear();
 
-    // this wave's tiles of the run, a tile of every block; those of pages first
-    auto page_tile = [&](int i) { return i < s.skip ? i : i - s.skip + s.at; };
-    auto page_at = [&](int i, int hf) { return (page_tile(i) * TL::TK + 16 * hf) >> c.log_page; };
-    // table entries of a tile's halves, and the page ids that they give (-1 where there is none)
-    auto entries_of = [&](int i, int* e) {
-#pragma unroll
-      for (int hf = 0; hf < TL::HALVES; ++hf) e[hf] = page_entry(c, b, page_at(i, hf));
-    };
-    auto ids_of = [&](int i, const int* e, int* id) {
-#pragma unroll
-      for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = page_of_entry(c, e[hf], page_at(i, hf));
-    };
-    // row 0 of a tile's half in the pool (page 0 where it has no page: its rows are not used)
-    auto place = [&](int i, int hf, int id) {
-      return page_unit(c, l, max(id, 0), h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
-    };
-    // scale byte of block `blk` of a half's first row (4 bits)
-    auto mx4_at = [&](const uint8_t* x, size_t row, int blk) {
-      return x + (row >> c.log_page) * (size_t)(TL::SB * c.page) + blk * c.page + (row & (c.page - 1));
-    };
-    auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks, uint32_t* kx) {
-#pragma unroll
-      for (int hf = 0; hf < TL::HALVES; ++hf) {
-        const size_t row = place(i, hf, id[hf]);
-        const char* p = c.k + row * TL::RB + col * TL::RB + g * (TL::RB < 64 ? 8 : 16);
-        if constexpr (TL::RB < 64) {
-          const uint2 x = *(const uint2*)p;
-          k[hf][0] = make_uint4(x.x, x.y, 0, 0);
-        } else {
-#pragma unroll
-          for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
-        }
-        if constexpr (C8) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
-        if constexpr (C4) kx[hf] = mx4_at(c.kx, row, g * TL::SB / 4)[col];
-      }
-    };
-    auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs, uint32_t* vx) {
-#pragma unroll
-      for (int hf = 0; hf < TL::HALVES; ++hf) {
-        const size_t row = place(i, hf, id[hf]);
-        const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::RB / 16);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (TL::RB < 64)
-            v[4 * hf + j][0] = *(const uint16_t*)(p + j * TL::RB);
-          else
-            load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
-        }
-        if constexpr (C8) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
-        if constexpr (C4) vx[hf] = *(const uint32_t*)(mx4_at(c.vx, row, col * TL::SB / 16) + 4 * g);
-      }
-    };
     using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
     auto load_queries = [&]() {
 #pragma unroll
@@ -604,80 +751,10 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         const bool ok = r < r_end;
         const int t = ok ? r >> a.log_g : 0, hq = h * G + (ok ? r - t * G : 0);
         w.pos[rt] = ok ? s.start + t : -kMaxRows;
-        const char* row = a.q.at(l, b, hq, t);
-        if constexpr (TL::F) {
-#pragma unroll
-          for (int i = 0; i < TL::QF; i += 4) {
-            const uint4 y = ldg16(row + TL::q_channel(i, g) * 4);
-            w.q[rt][i] = ok ? __uint_as_float(y.x) : 0.f;
-            w.q[rt][i + 1] = ok ? __uint_as_float(y.y) : 0.f;
-            w.q[rt][i + 2] = ok ? __uint_as_float(y.z) : 0.f;
-            w.q[rt][i + 3] = ok ? __uint_as_float(y.w) : 0.f;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < TL::QF; ++i) {
-            const uint4 y = ldg16(row + TL::q_channel(i, g) * 2);
-            w.q[rt][i] = ok ? y : make_uint4(0, 0, 0, 0);
-            if constexpr (TL::SPLIT) split_bf16(w.q[rt][i], w.q[rt][TL::QF + i]);
-          }
-        }
+        load_query_row<DT, D, FMT, RT>(w, rt, a.q.at(l, b, hq, t), ok);
       }
     };
-    int i = blk * NW + wave;
-    const int i_end = min(blk_end * NW, s.tiles);
-    if (i < i_end) {
-      // A tile's keys are dead after the scores and its values after the transpose: the next tile's loads go out there,
-      // into the same registers, and are waited for a tile's work later.
-      uint4 k[TL::HALVES][TL::KL];
-      uint32_t v[TL::VK][TL::VW];
-      float ks[TL::HALVES], vs[TL::HALVES];
-      uint32_t kx[TL::HALVES], vx[TL::HALVES];
-      int id[TL::HALVES], next[TL::HALVES], entry[TL::HALVES];
-      entries_of(i, entry);
-      ids_of(i, entry, id);
-      load_k(i, id, k, ks, kx);
-      load_v(i, id, v, vs, vx);
-      load_queries();
-      auto after = [&](int n) { return n + NW < i_end ? n + NW : n; };
-      entries_of(after(i), entry);
-      for (;;) {
-        // the last tile asks for itself again, so that every pass has the same loads in flight and waits for its own only
-        const int i1 = after(i);
-        const int k0 = page_tile(i) * TL::TK, k1 = k0 + TL::TK - 1;
-        bool have[TL::HALVES], all = true;
-        float sc[TL::HALVES], vf[TL::HALVES];
-#pragma unroll
-        for (int hf = 0; hf < TL::HALVES; ++hf) {
-          have[hf] = id[hf] >= 0 && k0 + 16 * hf < s.full;
-          all = all && have[hf];
-        }
-        const bool edge = !(all && k1 < s.full && k1 <= lo && (!a.window || k0 > hi - a.window || k1 < a.sinks));
-        f32x4 sr[RT][TL::HALVES];
-        w.template scores<false>(k, sr, kx);
-#pragma unroll
-        for (int hf = 0; hf < TL::HALVES; ++hf) {
-          sc[hf] = C8 ? (have[hf] ? a.qscale * ks[hf] : 0.f) : a.qscale;
-          vf[hf] = C8 ? (have[hf] ? vs[hf] : 0.f) : 1.f;
-        }
-        ids_of(i1, entry, next);
-        load_k(i1, next, k, ks, kx);
-        entries_of(after(i1), entry);
-        float p[RT][TL::VK];
-        w.weights(sr, sc, C8 && !TL::H ? vf : nullptr, a, edge, k0, s.full, have, p);
-        Operand x;
-        w.template operands<false>(v, x, vx);
-        load_v(i1, next, v, vs, vx);
-#pragma unroll
-        for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = next[hf];
-        w.add_values(x, p, a, edge, k0, s.full, have, lo, hi, C8 && TL::H ? vf : nullptr);
-        if (i1 == i) break;
-        i = i1;
-      }
-    }
-    else {
-      load_queries();
-    }
+    walk_pages<DT, D, FMT, RT>(w, a, c, b, l, h, PageRows{s.skip, s.at, s.from, s.base, s.full}, blk * NW + wave, min(blk_end * NW, s.tiles), lo, hi, load_queries);
     if constexpr (C8) {
       // rows of the page that is not complete, from the ring
       const int t_end = blk_end * NW;
@@ -685,7 +762,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       if (n < s.tiles) n += (s.tiles - n + NW - 1) / NW * NW;
       for (; n < t_end; n += NW) {
         const int k0 = s.full + (n - s.tiles) * TL::TK;
-        if (k0 >= s.rows) break;
+        if (k0 >= s.rows || s.full < s.base) break;
         const size_t ring = (((size_t)l * c.B + b) * c.Hkv + h) * (2 * c.page);
         auto row = [&](const char* base_, int j) { return base_ + (ring + (j & (2 * c.page - 1))) * (size_t)(D * TL::KB); };
         uint4 kr[TL::HALVES][TL::KLT];
@@ -710,45 +787,11 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       }
     }
 
-    // join the waves: maxima and sums, then the accumulators in two steps
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      s_ml[wave][rt][0][lane] = w.m[rt];
-      s_ml[wave][rt][1][lane] = column_sum(w.l[rt]);
-    }
-    __syncthreads();
     float M[RT], Lsum[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      M[rt] = -INFINITY;
-      Lsum[rt] = 0.f;
-#pragma unroll
-      for (int n = 0; n < NW; ++n) M[rt] = fmaxf(M[rt], s_ml[n][rt][0][lane]);
-      const float b0 = M[rt] == -INFINITY ? 0.f : M[rt];
-#pragma unroll
-      for (int n = 0; n < NW; ++n) Lsum[rt] += s_ml[n][rt][1][lane] * fast_exp2(s_ml[n][rt][0][lane] - b0);
-      const float move = fast_exp2(w.m[rt] - b0);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) w.o[rt][t] *= move;
-    }
-    // half of the waves to the other half, until one has everything
-#pragma unroll
-    for (int n = NW / 2; n > 0; n /= 2) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        if (wave >= n && wave < 2 * n)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) s_o[wave - n][t][lane] = w.o[rt][t];
-        __syncthreads();
-        if (wave < n)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) w.o[rt][t] += s_o[wave][t][lane];
-        if (rt + 1 < RT || n > 1) __syncthreads();
-      }
-    }
+    join_waves<DT, D, FMT, RT>(w, wave, s_ml, s_o, M, Lsum);
 
     const unsigned w0 = unit0 / per, w1 = (unit0 + s.nb - 1) / per;  // workgroups that share the unit
-    const bool alone = w0 == w1;
+    const bool alone = !SHARED && w0 == w1;
     const int n_rows = r_end - r0;
     // parts: a workgroup's run starts inside at most one unit and ends inside at most one other
     float* part = a.part + ((size_t)blockIdx.x * 2 + (x > first ? 1 : 0)) * a.part_rows * (D + 2);
@@ -800,7 +843,9 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       __syncthreads();
       const int share = __builtin_amdgcn_readfirstlane((int)(w1 - w0) + 1);
       int* cnt = a.cnt + w0;  // (no other shared unit starts in that workgroup's run)
-      if (threadIdx.x == 0) {
+      if (SHARED && share == 1) {
+        if (threadIdx.x == 0) s_last = 1;
+      } else if (threadIdx.x == 0) {
         const int n = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = n == share - 1;
         if (s_last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -812,6 +857,91 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         const float* part1 = a.part + (size_t)w0 * 2 * a.part_rows * (D + 2);
         const unsigned step = 2 * a.part_rows * (D + 2);
         auto part_of = [&](int n) { return n == 0 ? part0 : part1 + (size_t)(n * step); };
+        if constexpr (SHARED) {
+          // a wave to a row: its parts here, and those of the shared rows
+          const SharedArgs& sh = a.sh;
+          const int lh = l * a.Hkv + h;
+          int nb = 0, f0 = 0, rt = 0;
+          unsigned unit0 = 0;
+          if (s.group >= 0) {
+            const SharedGroup* gp = sh.plan + s.group;
+            nb = load_uniform(&gp->nb), f0 = load_uniform(&gp->f0), rt = load_uniform(&gp->rt), unit0 = load_uniform(&gp->unit0);
+          }
+          for (int r = wave; r < n_rows; r += NW) {
+            const int in_seq = r0 + r;  // token and head of the group
+            const long long row = ((long long)lh * a.B + b) * ((long long)c.n_new << a.log_g) + in_seq;
+            int np = 0;
+            const float *head = nullptr, *more = nullptr;
+            if (nb > 0) {
+              const int in_group = (b - f0) * (c.n_new << a.log_g) + in_seq, u = lh * rt + in_group / sh.unit_rows;
+              const int w_first = load_uniform(&sh.unit[unit0 + u].x);
+              np = load_uniform(&sh.unit[unit0 + u].y);
+              head = sh.head + row * (D + 2);
+              more = sh.more + ((size_t)w_first * sh.unit_rows + in_group % sh.unit_rows) * (D + 2);
+            }
+            const size_t more_step = (size_t)sh.unit_rows * (D + 2);
+            const int all = share + np;
+            auto at = [&](int n) {
+              return n < share ? part_of(n) + r * (D + 2) : n == share ? head : more + (size_t)(n - share) * more_step;
+            };
+            auto stats = [&](int n) { return n < share ? ld_coherent2(at(n) + D) : *(const float2*)(at(n) + D); };
+            float mx = -INFINITY, sum = 0.f;
+            for (int n = lane; n < all; n += kWave) {
+              const float2 ml = stats(n);
+              const float top = fmaxf(mx, ml.x), b0 = top == -INFINITY ? 0.f : top;
+              sum = sum * fast_exp2(mx - b0) + ml.y * fast_exp2(ml.x - b0);
+              mx = top;
+            }
+            float top = mx;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+            const float b0 = top == -INFINITY ? 0.f : top;
+            sum = wave_sum(sum * fast_exp2(mx - b0));
+            // a lane to two channels, all parts; d 64: half of the lanes to every second part
+            constexpr int WAYS = 128 / D, AHEAD = 8;
+            const int way = lane / (D / 2), e = lane % (D / 2) * 2;
+            float x0 = 0.f, x1 = 0.f;
+            for (int c0 = 0; c0 < all; c0 += kWave) {
+              const float f = fast_exp2(c0 + lane < all ? stats(c0 + lane).x - b0 : -INFINITY);
+              const int m = min(all - c0, kWave);
+              for (int n0 = 0; n0 < m; n0 += AHEAD * WAYS) {
+                float2 y[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                  const int n = c0 + min(n0 + k * WAYS + way, m - 1);
+                  y[k] = n < share ? ld_coherent2(at(n) + e) : *(const float2*)(at(n) + e);
+                }
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                  const int n = n0 + k * WAYS + way;
+                  const float fn = __shfl(f, min(n, kWave - 1));
+                  if (n < m) {
+                    x0 = fmaf(y[k].x, fn, x0);
+                    x1 = fmaf(y[k].y, fn, x1);
+                  }
+                }
+              }
+            }
+            if constexpr (WAYS == 2) {
+              x0 += __shfl_xor(x0, 32);
+              x1 += __shfl_xor(x1, 32);
+            }
+            if (way == 0) {
+              const int t = in_seq >> a.log_g, hq = h * G + in_seq - t * G;
+              const float inv = sum == 0.f ? 0.f : 1.f / sum;
+              char* out = a.out.at(l, b, hq, t) + e * TL::KB;
+              x0 = sum == 0.f ? 0.f : x0 * inv;
+              x1 = sum == 0.f ? 0.f : x1 * inv;
+              if constexpr (TL::F)
+                *(float2*)out = make_float2(x0, x1);
+              else
+                *(uint32_t*)out = pack2<DT>(x0, x1);
+              if (e == 0 && a.lse)
+                a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
+                    sum == 0.f ? -INFINITY : (b0 - TL::LIFT + __log2f(sum)) * 0.69314718055994531f;
+            }
+          }
+        } else {
         float* s_m = (float*)&s_o[0][0][0];  // maxima of `fit` parts, all rows
         const int fit = (int)(sizeof(s_o) / sizeof(float)) / n_rows;
         // a wave to a row, a lane to a part: the row's maximum and sum
@@ -891,6 +1021,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
             a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
                 sum == 0.f ? -INFINITY : (b0 - TL::LIFT + __log2f(sum)) * 0.69314718055994531f;
         }
+        }
       }
     }
     __syncthreads();  // the LDS buffers are free again
@@ -900,7 +1031,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
 
 template <class DT, int D, int FMT, int RT>
 hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT, false>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
   return hipGetLastError();
 }
 
