@@ -203,7 +203,7 @@ mpc_status check_groups(const mpc_dims* d, int32_t n_new, int32_t n_groups) {
 }
 
 mpc::SharedPlan shared_plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n, int groups) {
-  return mpc::shared_plan(d->dtype, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
+  return mpc::shared_plan(d->dtype, kv->format, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
                           kv->max_pages * kv->page_size, groups);
 }
 
@@ -959,7 +959,7 @@ mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t
                            void* out, const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream) {
   mpc_status s = check_dims(dims);
   if (s != MPC_OK) return s;
-  mpc::PagedAttnArgs a{};
+  mpc::SharedArgs a{};
   if ((s = paged_cache(dims, kv, n_new, n_valid, &a.c)) != MPC_OK) return s;
   if (!shared || !shared->first || !shared->rows) return fail(MPC_EINVAL, "shared, or one of its pointers, is NULL");
   if ((s = check_groups(dims, n_new, shared->n_groups)) != MPC_OK) return s;
@@ -970,25 +970,19 @@ mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t
     return fail(MPC_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, p.ws_bytes);
   if (!aligned16(ws)) return fail(MPC_EINVAL, "ws must be 16-byte aligned");
   char* at = (char*)ws;
-  a.cnt = (int*)ws;
-  a.part = (float*)(at + mpc::kPagedCntBytes);
-  a.row_tiles = p.own.row_tiles;
   a.log_g = __builtin_ctz((unsigned)(dims->n_q_heads / dims->n_kv_heads));
-  a.part_rows = p.own.part_rows;
-  a.grid = p.own.grid;
-  a.sh.first = shared->first;
-  a.sh.rows = shared->rows;
-  a.sh.groups = shared->n_groups;
-  a.sh.total = (unsigned*)(at + p.total);
-  a.sh.plan = (mpc::SharedGroup*)(at + p.plan);
-  a.sh.seq = (int2*)(at + p.seq);
-  a.sh.unit = (int2*)(at + p.unit);
-  a.sh.head = (float*)(at + p.head);
-  a.sh.more = (float*)(at + p.more);
-  a.sh.unit_rows = p.unit_rows;
-  a.sh.grid = p.grid;
-  a.sh.tile = p.tile;
-  a.sh.per_block = p.per_block;
+  a.first = shared->first;
+  a.rows = shared->rows;
+  a.groups = shared->n_groups;
+  a.total = (mpc::SharedTotals*)(at + p.total);
+  a.group = (mpc::SharedGroup*)(at + p.group);
+  a.seq = (mpc::SharedSeq*)(at + p.seq);
+  a.shared = {(float*)(at + p.shared_head), (float*)(at + p.shared_more), p.shared_rows, p.shared_workers};
+  a.own = {(float*)(at + p.own_head), (float*)(at + p.own_more), p.own_rows, p.own_workers};
+  a.tile = p.tile;
+  a.shared_block = p.shared_block;
+  a.own_block = p.own_block;
+  a.wide = p.wide;
   clear_stale_error();
   if ((s = launched(mpc::launch_shared_attn(a, dims->dtype, dims->head_dim, (hipStream_t)stream), "shared attention")) != MPC_OK)
     return s;

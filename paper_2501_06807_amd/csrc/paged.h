@@ -67,31 +67,8 @@ struct AttnArgs {
 // all of them.
 __host__ __device__ constexpr int paged_waves(int row_tiles) { return row_tiles == 1 ? 8 : 4; }
 
-// Attention behind shared rows: the sequences of a group look at the first rows of the group's first sequence, which a kernel of
-// its own takes for all of them (k_shared_rows); each sequence's other rows, and the join, are the paged attention's.
-// What the first launch (k_shared_plan) makes of a group: sequences [f0, f1), shared rows [0, base), their tiles [0, skip) and
-// from `at` on, blocks of keys nb (0: nothing to look at), units of query rows rt to a (layer, kv head); the blocks and units
-// of the groups before it.
-struct SharedGroup {
-  int f0, f1, base, skip, at, tiles, nb, rt;
-  unsigned block0, unit0;
-};
-constexpr int kMaxGroups = 1024;
-struct SharedArgs {
-  const int32_t *first, *rows;
-  int groups;
-  SharedGroup* plan;
-  unsigned* total;   // blocks of all groups
-  int2* seq;         // of each sequence: shared rows, group
-  int2* unit;        // of each unit of the shared rows: its first workgroup, and how many share it
-  float* head;       // [L][Hkv][B][n G][D + 2]: what a unit's first workgroup has of each row: accumulator, maximum, sum
-  float* more;       // [grid][unit rows][D + 2]: and each of its other workgroups
-  int unit_rows, grid, tile, per_block;  // tile: keys; per_block: tiles of a block
-};
-
 struct PagedAttnArgs : AttnArgs {
   PagedCache c;
-  SharedArgs sh;
   int* cnt;       // arrivals at a shared unit, by its first workgroup; zero between launches
   float* part;    // [grid][2][part_rows][D + 2]: accumulator, maximum and sum of a unit's part
   int row_tiles;  // 16-row tiles of a unit
@@ -113,19 +90,55 @@ hipError_t launch_paged_attn_bf16(const PagedAttnArgs& a, int D, hipStream_t st)
 hipError_t launch_paged_attn_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 
-// Sizes of a call behind shared rows, and its workspace: that of the paged attention, then plan, sequences, units and parts.
-struct SharedPlan {
-  PagedPlan own;
-  int unit_rows, grid, tile, per_block;
-  long long blocks;
-  size_t total, plan, seq, unit, head, more, ws_bytes;
+// Attention behind shared rows, four launches: the plan, made on the device; the shared rows of every group, for the rows of all
+// its sequences; each sequence's own rows; and the join. Both of the middle ones divide blocks of keys evenly over their
+// workers (workgroups there, waves here), in the order of groups or sequences, units of query rows and keys, and leave what they
+// have of each row of a unit: the worker that has a unit's first block in `head`, by row, the ones that go on with it in `more`, a
+// place for each worker (whose run goes on with one unit at most).
+constexpr int kMaxGroups = 1024;
+constexpr int kPartTail = 2;  // maximum and sum, behind a row's D accumulators
+struct Parts {
+  float* head;   // [L][Hkv][B][n G][D + 2]
+  float* more;   // [workers][unit rows][D + 2]
+  int unit_rows, workers;
 };
-SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
-hipError_t launch_shared_fp32(const PagedAttnArgs& a, int D, hipStream_t st);
-hipError_t launch_shared_fp16(const PagedAttnArgs& a, int D, hipStream_t st);
-hipError_t launch_shared_bf16(const PagedAttnArgs& a, int D, hipStream_t st);
-hipError_t launch_shared_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
-hipError_t launch_shared_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
+// A group: sequences [f0, f1), shared rows [0, base), the tiles of them that its rows look at (the first `skip`, then those from
+// `at` on), blocks of keys nb and units of query rows rt to a (layer, kv head); blocks of the groups before it.
+struct SharedGroup {
+  int f0, f1, base, skip, at, tiles, nb, rt;
+  unsigned block0;
+};
+// A sequence: rows that its group shares, group (-1: none), blocks of its own keys, blocks of the sequences before it.
+struct SharedSeq {
+  int base, group, nb;
+  unsigned block0;
+};
+struct SharedTotals {
+  unsigned shared, own;  // blocks
+};
+struct SharedArgs : AttnArgs {
+  PagedCache c;
+  const int32_t *first, *rows;
+  int groups, log_g;
+  SharedTotals* total;
+  SharedGroup* group;
+  SharedSeq* seq;
+  Parts shared, own;
+  int tile, shared_block, own_block;  // keys of a tile; tiles of a block
+  int wide;                           // shared rows in units of 128 query rows
+};
+struct SharedPlan {
+  int shared_rows, own_rows, shared_workers, own_workers, tile, shared_block, own_block, wide;
+  long long blocks;  // the more of both kinds, at most
+  size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
+};
+constexpr int kOwnWaves = 4;  // waves of a workgroup that takes own rows
+SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
+hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);
+hipError_t launch_shared_fp16(const SharedArgs& a, int D, hipStream_t st);
+hipError_t launch_shared_bf16(const SharedArgs& a, int D, hipStream_t st);
+hipError_t launch_shared_mx4(const SharedArgs& a, int dtype, int D, hipStream_t st);
+hipError_t launch_shared_attn(const SharedArgs& a, int dtype, int D, hipStream_t st);
 
 struct PromptAttnArgs : AttnArgs {
   Rows k, v;

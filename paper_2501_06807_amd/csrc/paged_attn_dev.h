@@ -471,14 +471,14 @@ struct PageRows {
   int skip, at, from, base, full;
 };
 
-// A wave's tiles i, i + NW, .. (before i_end) of (sequence b's table, layer l, kv head h), for rows at positions lo .. hi; takes
+// A wave's tiles i, i + STEP, .. (before i_end) of (sequence b's table, layer l, kv head h), for rows at positions lo .. hi; takes
 // the queries in beside the first loads.
-template <class DT, int D, int FMT, int RT, class Queries>
+template <class DT, int D, int FMT, int RT, int STEP, class Queries>
 __device__ __forceinline__ void walk_pages(PagedWave<DT, D, FMT, RT>& w, const AttnArgs& a, const PagedCache& c, int b, int l, int h,
                                            const PageRows& r, int i, int i_end, int lo, int hi, Queries load_queries) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr bool C8 = TL::C8, C4 = TL::C4;
-  constexpr int NT = TL::NT, NW = paged_waves(RT);
+  constexpr int NT = TL::NT;
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
   auto page_tile = [&](int i) { return i < r.skip ? r.from + i : i - r.skip + r.at; };
   auto page_at = [&](int i, int hf) { return (page_tile(i) * TL::TK + 16 * hf) >> c.log_page; };
@@ -545,7 +545,7 @@ __device__ __forceinline__ void walk_pages(PagedWave<DT, D, FMT, RT>& w, const A
     load_k(i, id, k, ks, kx);
     load_v(i, id, v, vs, vx);
     load_queries();
-    auto after = [&](int n) { return n + NW < i_end ? n + NW : n; };
+    auto after = [&](int n) { return n + STEP < i_end ? n + STEP : n; };
     entries_of(after(i), entry);
     for (;;) {
       // the last tile asks for itself again, so that every pass has the same loads in flight and waits for its own only
@@ -583,6 +583,40 @@ __device__ __forceinline__ void walk_pages(PagedWave<DT, D, FMT, RT>& w, const A
   }
   else {
     load_queries();
+  }
+}
+
+// The same for tiles of a page that is not complete, rows [full, rows), from the ring (8-bit codes).
+template <class DT, int D, int RT, int STEP>
+__device__ __forceinline__ void walk_tail(PagedWave<DT, D, MPC_PAGE_E4M3, RT>& w, const AttnArgs& a, const PagedCache& c, int b, int l,
+                                          int h, int full, int rows, int i, int i_end, int lo, int hi) {
+  using TL = PagedTile<DT, D, MPC_PAGE_E4M3, RT>;
+  constexpr int NT = TL::NT;
+  const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
+  for (; i < i_end; i += STEP) {
+    const int k0 = full + i * TL::TK;
+    if (k0 >= rows) break;
+    const size_t ring = (((size_t)l * c.B + b) * c.Hkv + h) * (2 * c.page);
+    auto row = [&](const char* base_, int j) { return base_ + (ring + (j & (2 * c.page - 1))) * (size_t)(D * TL::KB); };
+    uint4 kr[TL::HALVES][TL::KLT];
+    uint32_t vr[TL::VK][TL::VWT];
+#pragma unroll
+    for (int hf = 0; hf < TL::HALVES; ++hf)
+#pragma unroll
+      for (int e = 0; e < TL::KLT; ++e)
+        kr[hf][e] = ldg16(row(c.k_tail, k0 + 16 * hf + col) + TL::q_channel(TL::F ? 4 * e : e, g) * TL::KB);
+#pragma unroll
+    for (int j = 0; j < TL::VK; ++j)
+      load_words<TL::VWT>(row(c.v_tail, k0 + TL::v_key(j, g)) + col * (TL::VWT * 4), vr[j]);
+    const bool have[2] = {true, true};
+    const float sc[2] = {a.qscale, a.qscale};
+    f32x4 sr[RT][TL::HALVES];
+    w.template scores<true>(kr, sr);
+    float p[RT][TL::VK];
+    w.weights(sr, sc, nullptr, a, true, k0, rows, have, p);
+    std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]> x;
+    w.template operands<true>(vr, x);
+    w.add_values(x, p, a, true, k0, rows, have, lo, hi, nullptr);
   }
 }
 
@@ -628,8 +662,7 @@ __device__ __forceinline__ void join_waves(PagedWave<DT, D, FMT, RT>& w, int wav
   }
 }
 
-// SHARED: the first rows of a sequence, up to those that its group shares, are taken elsewhere; their parts are joined here.
-template <class DT, int D, int FMT, int RT, bool SHARED>
+template <class DT, int D, int FMT, int RT>
 __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAttnArgs a) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr bool C8 = TL::C8;
@@ -646,13 +679,9 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
   // Work of sequence b: units (layer, kv head, row group) of nb blocks each.
   struct Seq {
     int valid, len, rows, start, groups, full, tiles, skip, at, nb;  // tiles of pages: [from, from + skip) and [at, ..)
-    int from, base, group;  // SHARED: rows [0, base) are the group's
   };
-  auto seq_of = [&](int len, int valid, int2 shared) {
+  auto seq_of = [&](int len, int valid) {
     Seq s;
-    s.base = SHARED ? shared.x : 0;
-    s.group = SHARED ? shared.y : -1;
-    s.from = SHARED ? s.base / TL::TK : 0;
     s.valid = min(max(valid, 0), c.n_new);
     s.len = min(max(len, 0), kMaxRows);
     s.rows = min(s.len, c.cap());
@@ -660,34 +689,28 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     s.groups = ((s.valid << a.log_g) + RW - 1) / RW;
     s.full = C8 ? s.rows & ~(c.page - 1) : s.rows;
     const int all = (s.full + TL::TK - 1) / TL::TK;
-    s.skip = max(all - s.from, 0);
-    s.at = max(all, s.from);
+    s.skip = all;
+    s.at = all;
     if (a.window) {
-      s.skip = max(min((a.sinks + TL::TK - 1) / TL::TK, all) - s.from, 0);
-      s.at = max(s.from + s.skip, min(max(s.start - a.window + 1, 0) / TL::TK, all));
+      s.skip = min((a.sinks + TL::TK - 1) / TL::TK, all);
+      s.at = max(s.skip, min(max(s.start - a.window + 1, 0) / TL::TK, all));
     }
-    s.tiles = s.skip + max(all - s.at, 0);
-    const int tail = s.full < s.base ? 0 : (s.rows - s.full + TL::TK - 1) / TL::TK;
+    s.tiles = s.skip + all - s.at;
+    const int tail = (s.rows - s.full + TL::TK - 1) / TL::TK;
     s.nb = max(1, (s.tiles + tail + NW - 1) / NW);
     return s;
   };
-  auto seq = [&](int b) {
-    int2 shared = make_int2(0, -1);
-    if constexpr (SHARED) shared = make_int2(load_uniform(&a.sh.seq[b].x), load_uniform(&a.sh.seq[b].y));
-    return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new, shared);
-  };
+  auto seq = [&](int b) { return seq_of(load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new); };
   const int per_group = a.L * a.Hkv;
   auto blocks_of = [&](const Seq& s) { return (unsigned)(s.groups * per_group) * (unsigned)s.nb; };
   // all blocks (below 2^31, as the host has checked for the longest sequences), sequences to lanes
   unsigned total = 0, mine = 0;
   int my_len = 0, my_valid = 0;
-  int2 my_shared = make_int2(0, -1);
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const bool in = b0 + lane < a.B;
     my_len = in ? c.lens[b0 + lane] : 0;
     my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
-    if constexpr (SHARED) my_shared = in ? a.sh.seq[b0 + lane] : make_int2(0, -1);
-    mine = blocks_of(seq_of(my_len, my_valid, my_shared));
+    mine = blocks_of(seq_of(my_len, my_valid));
     total += wave_sum(mine);
   }
   total = __builtin_amdgcn_readfirstlane(total);
@@ -704,8 +727,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       const bool in = b0 + lane < a.B;
       my_len = in ? c.lens[b0 + lane] : 0;
       my_valid = in ? c.n_valid ? c.n_valid[b0 + lane] : c.n_new : 0;
-      if constexpr (SHARED) my_shared = in ? a.sh.seq[b0 + lane] : make_int2(0, -1);
-      mine = blocks_of(seq_of(my_len, my_valid, my_shared));
+      mine = blocks_of(seq_of(my_len, my_valid));
     }
     unsigned sum = mine;
 #pragma unroll
@@ -718,8 +740,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)past) - 1);
       b = b0 + at;
       base += __builtin_amdgcn_readlane(sum - mine, at);
-      s = seq_of(__builtin_amdgcn_readlane(my_len, at), __builtin_amdgcn_readlane(my_valid, at),
-                 make_int2(__builtin_amdgcn_readlane(my_shared.x, at), __builtin_amdgcn_readlane(my_shared.y, at)));
+      s = seq_of(__builtin_amdgcn_readlane(my_len, at), __builtin_amdgcn_readlane(my_valid, at));
       break;
     }
     base += __builtin_amdgcn_readlane(sum, kWave - 1);
@@ -743,7 +764,6 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
     const int lo = s.start + (r0 >> a.log_g), hi = s.start + ((r_end - 1) >> a.log_g);
     w.clear();
 
-    using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
     auto load_queries = [&]() {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
@@ -754,44 +774,18 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         load_query_row<DT, D, FMT, RT>(w, rt, a.q.at(l, b, hq, t), ok);
       }
     };
-    walk_pages<DT, D, FMT, RT>(w, a, c, b, l, h, PageRows{s.skip, s.at, s.from, s.base, s.full}, blk * NW + wave, min(blk_end * NW, s.tiles), lo, hi, load_queries);
+    walk_pages<DT, D, FMT, RT, NW>(w, a, c, b, l, h, PageRows{s.skip, s.at, 0, 0, s.full}, blk * NW + wave, min(blk_end * NW, s.tiles), lo, hi, load_queries);
     if constexpr (C8) {
-      // rows of the page that is not complete, from the ring
-      const int t_end = blk_end * NW;
       int n = blk * NW + wave;
       if (n < s.tiles) n += (s.tiles - n + NW - 1) / NW * NW;
-      for (; n < t_end; n += NW) {
-        const int k0 = s.full + (n - s.tiles) * TL::TK;
-        if (k0 >= s.rows || s.full < s.base) break;
-        const size_t ring = (((size_t)l * c.B + b) * c.Hkv + h) * (2 * c.page);
-        auto row = [&](const char* base_, int j) { return base_ + (ring + (j & (2 * c.page - 1))) * (size_t)(D * TL::KB); };
-        uint4 kr[TL::HALVES][TL::KLT];
-        uint32_t vr[TL::VK][TL::VWT];
-#pragma unroll
-        for (int hf = 0; hf < TL::HALVES; ++hf)
-#pragma unroll
-          for (int e = 0; e < TL::KLT; ++e)
-            kr[hf][e] = ldg16(row(c.k_tail, k0 + 16 * hf + col) + TL::q_channel(TL::F ? 4 * e : e, g) * TL::KB);
-#pragma unroll
-        for (int j = 0; j < TL::VK; ++j)
-          load_words<TL::VWT>(row(c.v_tail, k0 + TL::v_key(j, g)) + col * (TL::VWT * 4), vr[j]);
-        const bool have[2] = {true, true};
-        const float sc[2] = {a.qscale, a.qscale};
-        f32x4 sr[RT][TL::HALVES];
-        w.template scores<true>(kr, sr);
-        float p[RT][TL::VK];
-        w.weights(sr, sc, nullptr, a, true, k0, s.rows, have, p);
-        Operand x;
-        w.template operands<true>(vr, x);
-        w.add_values(x, p, a, true, k0, s.rows, have, lo, hi, nullptr);
-      }
+      walk_tail<DT, D, RT, NW>(w, a, c, b, l, h, s.full, s.rows, n - s.tiles, blk_end * NW - s.tiles, lo, hi);
     }
 
     float M[RT], Lsum[RT];
     join_waves<DT, D, FMT, RT>(w, wave, s_ml, s_o, M, Lsum);
 
     const unsigned w0 = unit0 / per, w1 = (unit0 + s.nb - 1) / per;  // workgroups that share the unit
-    const bool alone = !SHARED && w0 == w1;
+    const bool alone = w0 == w1;
     const int n_rows = r_end - r0;
     // parts: a workgroup's run starts inside at most one unit and ends inside at most one other
     float* part = a.part + ((size_t)blockIdx.x * 2 + (x > first ? 1 : 0)) * a.part_rows * (D + 2);
@@ -843,9 +837,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
       __syncthreads();
       const int share = __builtin_amdgcn_readfirstlane((int)(w1 - w0) + 1);
       int* cnt = a.cnt + w0;  // (no other shared unit starts in that workgroup's run)
-      if (SHARED && share == 1) {
-        if (threadIdx.x == 0) s_last = 1;
-      } else if (threadIdx.x == 0) {
+      if (threadIdx.x == 0) {
         const int n = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = n == share - 1;
         if (s_last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -857,91 +849,6 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
         const float* part1 = a.part + (size_t)w0 * 2 * a.part_rows * (D + 2);
         const unsigned step = 2 * a.part_rows * (D + 2);
         auto part_of = [&](int n) { return n == 0 ? part0 : part1 + (size_t)(n * step); };
-        if constexpr (SHARED) {
-          // a wave to a row: its parts here, and those of the shared rows
-          const SharedArgs& sh = a.sh;
-          const int lh = l * a.Hkv + h;
-          int nb = 0, f0 = 0, rt = 0;
-          unsigned unit0 = 0;
-          if (s.group >= 0) {
-            const SharedGroup* gp = sh.plan + s.group;
-            nb = load_uniform(&gp->nb), f0 = load_uniform(&gp->f0), rt = load_uniform(&gp->rt), unit0 = load_uniform(&gp->unit0);
-          }
-          for (int r = wave; r < n_rows; r += NW) {
-            const int in_seq = r0 + r;  // token and head of the group
-            const long long row = ((long long)lh * a.B + b) * ((long long)c.n_new << a.log_g) + in_seq;
-            int np = 0;
-            const float *head = nullptr, *more = nullptr;
-            if (nb > 0) {
-              const int in_group = (b - f0) * (c.n_new << a.log_g) + in_seq, u = lh * rt + in_group / sh.unit_rows;
-              const int w_first = load_uniform(&sh.unit[unit0 + u].x);
-              np = load_uniform(&sh.unit[unit0 + u].y);
-              head = sh.head + row * (D + 2);
-              more = sh.more + ((size_t)w_first * sh.unit_rows + in_group % sh.unit_rows) * (D + 2);
-            }
-            const size_t more_step = (size_t)sh.unit_rows * (D + 2);
-            const int all = share + np;
-            auto at = [&](int n) {
-              return n < share ? part_of(n) + r * (D + 2) : n == share ? head : more + (size_t)(n - share) * more_step;
-            };
-            auto stats = [&](int n) { return n < share ? ld_coherent2(at(n) + D) : *(const float2*)(at(n) + D); };
-            float mx = -INFINITY, sum = 0.f;
-            for (int n = lane; n < all; n += kWave) {
-              const float2 ml = stats(n);
-              const float top = fmaxf(mx, ml.x), b0 = top == -INFINITY ? 0.f : top;
-              sum = sum * fast_exp2(mx - b0) + ml.y * fast_exp2(ml.x - b0);
-              mx = top;
-            }
-            float top = mx;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-            const float b0 = top == -INFINITY ? 0.f : top;
-            sum = wave_sum(sum * fast_exp2(mx - b0));
-            // a lane to two channels, all parts; d 64: half of the lanes to every second part
-            constexpr int WAYS = 128 / D, AHEAD = 8;
-            const int way = lane / (D / 2), e = lane % (D / 2) * 2;
-            float x0 = 0.f, x1 = 0.f;
-            for (int c0 = 0; c0 < all; c0 += kWave) {
-              const float f = fast_exp2(c0 + lane < all ? stats(c0 + lane).x - b0 : -INFINITY);
-              const int m = min(all - c0, kWave);
-              for (int n0 = 0; n0 < m; n0 += AHEAD * WAYS) {
-                float2 y[AHEAD];
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                  const int n = c0 + min(n0 + k * WAYS + way, m - 1);
-                  y[k] = n < share ? ld_coherent2(at(n) + e) : *(const float2*)(at(n) + e);
-                }
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                  const int n = n0 + k * WAYS + way;
-                  const float fn = __shfl(f, min(n, kWave - 1));
-                  if (n < m) {
-                    x0 = fmaf(y[k].x, fn, x0);
-                    x1 = fmaf(y[k].y, fn, x1);
-                  }
-                }
-              }
-            }
-            if constexpr (WAYS == 2) {
-              x0 += __shfl_xor(x0, 32);
-              x1 += __shfl_xor(x1, 32);
-            }
-            if (way == 0) {
-              const int t = in_seq >> a.log_g, hq = h * G + in_seq - t * G;
-              const float inv = sum == 0.f ? 0.f : 1.f / sum;
-              char* out = a.out.at(l, b, hq, t) + e * TL::KB;
-              x0 = sum == 0.f ? 0.f : x0 * inv;
-              x1 = sum == 0.f ? 0.f : x1 * inv;
-              if constexpr (TL::F)
-                *(float2*)out = make_float2(x0, x1);
-              else
-                *(uint32_t*)out = pack2<DT>(x0, x1);
-              if (e == 0 && a.lse)
-                a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
-                    sum == 0.f ? -INFINITY : (b0 - TL::LIFT + __log2f(sum)) * 0.69314718055994531f;
-            }
-          }
-        } else {
         float* s_m = (float*)&s_o[0][0][0];  // maxima of `fit` parts, all rows
         const int fit = (int)(sizeof(s_o) / sizeof(float)) / n_rows;
         // a wave to a row, a lane to a part: the row's maximum and sum
@@ -1021,7 +928,6 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
             a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
                 sum == 0.f ? -INFINITY : (b0 - TL::LIFT + __log2f(sum)) * 0.69314718055994531f;
         }
-        }
       }
     }
     __syncthreads();  // the LDS buffers are free again
@@ -1031,7 +937,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_paged_attn(PagedAtt
 
 template <class DT, int D, int FMT, int RT>
 hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT, false>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
   return hipGetLastError();
 }
 

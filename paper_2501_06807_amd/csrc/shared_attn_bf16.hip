@@ -3,7 +3,7 @@
 
 namespace mpc {
 
-hipError_t launch_shared_bf16(const PagedAttnArgs& a, int D, hipStream_t st) {
+hipError_t launch_shared_bf16(const SharedArgs& a, int D, hipStream_t st) {
   return a.c.format == MPC_PAGE_E4M3 ? dev::launch_shared_format<BF16, MPC_PAGE_E4M3>(a, D, st) : dev::launch_shared_format<BF16, MPC_PAGE_SAME>(a, D, st);
 }
 

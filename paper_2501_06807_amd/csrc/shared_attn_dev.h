@@ -1,33 +1,33 @@
-// Attention behind shared rows: the kernel of the shared rows, for units of 16 or 32 query rows.
+// Attention behind shared rows: the kernels of the shared rows for units of 16 or 32 query rows, and of the sequences' own rows.
 //
 // A group's query rows (all its sequences' tokens and the G heads of a kv head) are one unit's rows as far as they fit, so K and
-// V of the shared rows are read once for a unit instead of once for a sequence. The blocks of keys of all units are divided
-// evenly over the grid; each workgroup writes what it has of a unit (accumulators, maxima and sums of the unit's rows), and the
-// paged attention's kernel, which takes each sequence's own rows, joins these parts to its own.
+// V of the shared rows are read once for a unit instead of once for a sequence. The tiles' work is the paged attention's.
 #pragma once
 #include "paged_attn_dev.h"
 
 namespace mpc {
 namespace dev {
 
-// The group that block x falls to; groups to lanes.
-__device__ __forceinline__ int group_of(const SharedArgs& sh, unsigned x) {
+// The last of n entries (in order) that is not beyond x; entries to lanes, 64 steps at a time.
+template <class At>
+__device__ __forceinline__ int last_from(int n, unsigned x, At at) {
   const int lane = threadIdx.x % kWave;
-  int g = 0;
-  for (int g0 = 0; g0 < sh.groups; g0 += kWave) {
-    const bool before = g0 + lane < sh.groups && sh.plan[g0 + lane].block0 <= x;
-    const unsigned long long past = __ballot(before);
-    if (past) g = g0 + 63 - __clzll((long long)past);
+  int lo = 0;
+  for (int step = 1 << 24; step > 0; step /= kWave) {
+    if (step >= n) continue;
+    const int i = lo + lane * step;
+    const unsigned long long past = __ballot(i < n && at(i) <= x);
+    lo += (63 - __clzll((long long)past)) * step;
   }
-  return __builtin_amdgcn_readfirstlane(g);
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// A query row of a group: sequence, token, head of the kv head's group, position.
+// A query row of a group: sequence, token and head of it, position.
 struct SharedRow {
   int b, in_seq, pos;
   bool live;
 };
-__device__ __forceinline__ SharedRow shared_row(const PagedAttnArgs& a, int f0, int f1, int row) {
+__device__ __forceinline__ SharedRow shared_row(const SharedArgs& a, int f0, int f1, int row) {
   const PagedCache& c = a.c;
   const int per = c.n_new << a.log_g;
   SharedRow r;
@@ -40,34 +40,50 @@ __device__ __forceinline__ SharedRow shared_row(const PagedAttnArgs& a, int f0, 
   r.pos = c.len(r.b) - valid + t;
   return r;
 }
+// Row in_seq of (layer and kv head lh, sequence b) in a head array.
+__device__ __forceinline__ long long part_row(const SharedArgs& a, int lh, int b, int in_seq) {
+  return ((long long)lh * a.B + b) * ((long long)a.c.n_new << a.log_g) + in_seq;
+}
+
+// What a wave (one that holds the sums of its lanes' columns) has of its rows, written for the join: accumulators, the reference of
+// their exponents (its lift taken off) and the weights' sum.
+template <class DT, int D, int FMT, int RT>
+__device__ __forceinline__ void write_part(const PagedWave<DT, D, FMT, RT>& w, int rt, float m, float sum, float* part) {
+  using TL = PagedTile<DT, D, FMT, RT>;
+  constexpr int NT = TL::NT;
+  const int g = (threadIdx.x % kWave) / 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int n = 0; n < NT; n += 2) *(float2*)(part + (4 * g + e) * NT + n) = make_float2(w.o[rt][n][e], w.o[rt][n + 1][e]);
+  if (g == 0) *(float2*)(part + D) = make_float2(m - TL::LIFT, sum);
+}
 
 template <class DT, int D, int FMT, int RT>
-__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(PagedAttnArgs a) {
+__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedArgs a) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr int NT = TL::NT, RW = 16 * RT, NW = paged_waves(RT);
   const PagedCache& c = a.c;
-  const SharedArgs& sh = a.sh;
-  const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
+  const int lane = threadIdx.x % kWave, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   __shared__ __align__(16) f32x4 s_o[NW / 2][NT][kWave];
   __shared__ float s_ml[NW][RT][2][kWave];
 
-  const unsigned total = load_uniform(sh.total), id = by_die(blockIdx.x, gridDim.x);
+  const unsigned total = load_uniform(&a.total->shared), id = by_die(blockIdx.x, gridDim.x);
   const unsigned per = (total + gridDim.x - 1) / gridDim.x;
   if ((unsigned long long)id * per >= total) return;
   const unsigned first = id * per, last = min(first + per, total);
-  int gi = group_of(sh, first);
+  int gi = last_from(a.groups, first, [&](int i) { return a.group[i].block0; });
   PagedWave<DT, D, FMT, RT> w;
   unsigned x = first;
   while (x < last) {
-    while (gi + 1 < sh.groups && x >= load_uniform(&sh.plan[gi + 1].block0)) ++gi;
-    const SharedGroup* gp = sh.plan + gi;
+    while (gi + 1 < a.groups && x >= load_uniform(&a.group[gi + 1].block0)) ++gi;
+    const SharedGroup* gp = a.group + gi;
     const int f0 = load_uniform(&gp->f0), f1 = load_uniform(&gp->f1), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
-    const unsigned block0 = load_uniform(&gp->block0), in = x - block0;
+    const unsigned in = x - load_uniform(&gp->block0);
     const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
     const int blk_end = min(nb, blk + (int)(last - x));
     const int lh = u / rts, h = lh % a.Hkv, l = lh / a.Hkv, r0 = u % rts * RW;
-    const unsigned start = x - blk;  // the unit's first block
     w.clear();
     SharedRow row[RT];
     int lo = kMaxRows, hi = -kMaxRows;  // positions of the unit's rows
@@ -90,30 +106,19 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(PagedAt
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const int t = row[rt].in_seq >> a.log_g, hq = (h << a.log_g) + row[rt].in_seq - (t << a.log_g);
-        const char* p = a.q.at(l, row[rt].b, hq, t);
-        load_query_row<DT, D, FMT, RT>(w, rt, p, row[rt].live);
+        load_query_row<DT, D, FMT, RT>(w, rt, a.q.at(l, row[rt].b, hq, t), row[rt].live);
       }
     };
-    const int base = load_uniform(&gp->base);
-    const PageRows rows{load_uniform(&gp->skip), load_uniform(&gp->at), 0, 0, base};
-    walk_pages<DT, D, FMT, RT>(w, a, c, f0, l, h, rows, blk * NW + wave, min(blk_end * NW, load_uniform(&gp->tiles)), lo, hi, load_queries);
+    const PageRows rows{load_uniform(&gp->skip), load_uniform(&gp->at), 0, 0, load_uniform(&gp->base)};
+    walk_pages<DT, D, FMT, RT, NW>(w, a, c, f0, l, h, rows, blk * NW + wave, min(blk_end * NW, load_uniform(&gp->tiles)), lo, hi, load_queries);
     float M[RT], Lsum[RT];
     join_waves<DT, D, FMT, RT>(w, wave, s_ml, s_o, M, Lsum);
-    if (blk == 0 && threadIdx.x == 0) {
-      const unsigned w0 = start / per, w1 = (start + nb - 1) / per;
-      sh.unit[load_uniform(&gp->unit0) + u] = make_int2((int)w0, (int)(w1 - w0) + 1);
-    }
     if (wave == 0) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         if (!row[rt].live) continue;
-        float* part = blk == 0 ? sh.head + (((long long)lh * a.B + row[rt].b) * ((long long)c.n_new << a.log_g) + row[rt].in_seq) * (D + 2)
-                               : sh.more + ((size_t)id * sh.unit_rows + 16 * rt + col) * (D + 2);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int n = 0; n < NT; n += 2) *(float2*)(part + (4 * g + e) * NT + n) = make_float2(w.o[rt][n][e], w.o[rt][n + 1][e]);
-        if (g == 0) *(float2*)(part + D) = make_float2(M[rt], Lsum[rt]);
+        write_part(w, rt, M[rt], Lsum[rt], blk == 0 ? a.shared.head + part_row(a, lh, row[rt].b, row[rt].in_seq) * (D + kPartTail)
+                                                    : a.shared.more + ((size_t)id * RW + 16 * rt + col) * (D + kPartTail));
       }
     }
     __syncthreads();  // the LDS buffers are free again
@@ -121,22 +126,117 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(PagedAt
   }
 }
 
+// A sequence's own rows: the tiles of pages behind the shared ones (as PageRows has them), and of the ring.
+struct OwnRows {
+  int valid, len, rows, start, groups, full, tiles, all;  // tiles of pages, and with those of the ring
+  PageRows pages;
+};
+template <bool C8>
+__device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int len, int valid, int base, int unit_rows) {
+  const PagedCache& c = a.c;
+  const int tile = a.tile;
+  OwnRows s;
+  s.valid = min(max(valid, 0), c.n_new);
+  s.len = min(max(len, 0), kMaxRows);
+  s.rows = min(s.len, c.cap());
+  s.start = s.len - s.valid;
+  s.groups = ((s.valid << a.log_g) + unit_rows - 1) / unit_rows;
+  s.full = C8 ? s.rows & ~(c.page - 1) : s.rows;
+  const int all = (s.full + tile - 1) / tile;
+  PageRows& p = s.pages;
+  p.base = base;
+  p.full = s.full;
+  p.from = base / tile;
+  p.skip = max(all - p.from, 0);
+  p.at = max(all, p.from);
+  if (a.window) {
+    p.skip = max(min((a.sinks + tile - 1) / tile, all) - p.from, 0);
+    p.at = max(p.from + p.skip, min(max(s.start - a.window + 1, 0) / tile, all));
+  }
+  s.tiles = p.skip + max(all - p.at, 0);
+  s.all = s.tiles + (s.full < base ? 0 : (s.rows - s.full + tile - 1) / tile);
+  return s;
+}
+
+// A wave to a run of blocks: nothing of it waits for another wave.
 template <class DT, int D, int FMT, int RT>
-hipError_t launch_shared_rt(const PagedAttnArgs& a, hipStream_t st) {
-  hipError_t e;
-  if (a.sh.unit_rows == 16)
-    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1>), dim3((unsigned)a.sh.grid), dim3(paged_waves(1) * kWave), 0, st, a);
+__global__ __launch_bounds__(kOwnWaves * kWave, RT == 1 ? 2 : 1) void k_own_rows(SharedArgs a) {
+  using TL = PagedTile<DT, D, FMT, RT>;
+  constexpr int RW = 16 * RT;
+  const PagedCache& c = a.c;
+  const int lane = threadIdx.x % kWave, col = lane % 16;
+  const unsigned id = by_die(blockIdx.x, gridDim.x) * kOwnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned total = load_uniform(&a.total->own), workers = gridDim.x * kOwnWaves;
+  const unsigned per = (total + workers - 1) / workers;
+  if ((unsigned long long)id * per >= total) return;
+  const unsigned first = id * per, last = min(first + per, total);
+  int b = last_from(a.B, first, [&](int i) { return a.seq[i].block0; });
+  PagedWave<DT, D, FMT, RT> w;
+  unsigned x = first;
+  while (x < last) {
+    while (b + 1 < a.B && x >= load_uniform(&a.seq[b + 1].block0)) ++b;
+    const SharedSeq* sp = a.seq + b;
+    const int nb = load_uniform(&sp->nb);
+    const OwnRows s = own_rows<TL::C8>(a, load_uniform(c.lens + b), c.n_valid ? load_uniform(c.n_valid + b) : c.n_new, load_uniform(&sp->base), RW);
+    const unsigned in = x - load_uniform(&sp->block0);
+    const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
+    const int blk_end = min(nb, blk + (int)(last - x));
+    const int rg = u % s.groups, lh = u / s.groups, h = lh % a.Hkv, l = lh / a.Hkv;
+    const int r0 = rg * RW, r_end = min(s.valid << a.log_g, r0 + RW);
+    const int lo = s.start + (r0 >> a.log_g), hi = s.start + ((r_end - 1) >> a.log_g);
+    w.clear();
+    auto load_queries = [&]() {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + 16 * rt + col;
+        const bool ok = r < r_end;
+        const int t = ok ? r >> a.log_g : 0, hq = (h << a.log_g) + (ok ? r - (t << a.log_g) : 0);
+        w.pos[rt] = ok ? s.start + t : -kMaxRows;
+        load_query_row<DT, D, FMT, RT>(w, rt, a.q.at(l, b, hq, t), ok);
+      }
+    };
+    const int i = blk * a.own_block, i_end = min(blk_end * a.own_block, s.all);
+    walk_pages<DT, D, FMT, RT, 1>(w, a, c, b, l, h, s.pages, i, min(i_end, s.tiles), lo, hi, load_queries);
+    if constexpr (TL::C8) walk_tail<DT, D, RT, 1>(w, a, c, b, l, h, s.full, s.rows, max(i - s.tiles, 0), i_end - s.tiles, lo, hi);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float sum = column_sum(w.l[rt]);
+      const int r = 16 * rt + col;
+      if (r0 + r >= r_end) continue;
+      write_part(w, rt, w.m[rt], sum, blk == 0 ? a.own.head + part_row(a, lh, b, r0 + r) * (D + kPartTail)
+                                               : a.own.more + ((size_t)id * RW + r) * (D + kPartTail));
+    }
+    x += blk_end - blk;
+  }
+}
+
+template <class DT, int D, int FMT>
+hipError_t launch_narrow(const SharedArgs& a, hipStream_t st) {
+  if (a.shared.unit_rows == 16)
+    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1>), dim3((unsigned)a.shared.workers), dim3(paged_waves(1) * kWave), 0, st, a);
   else
-    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2>), dim3((unsigned)a.sh.grid), dim3(paged_waves(2) * kWave), 0, st, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((k_paged_attn<DT, D, FMT, RT, true>), dim3((unsigned)a.grid), dim3(paged_waves(RT) * kWave), 0, st, a);
+    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2>), dim3((unsigned)a.shared.workers), dim3(paged_waves(2) * kWave), 0, st, a);
   return hipGetLastError();
 }
 
+template <class DT, int D, int FMT>
+hipError_t launch_own(const SharedArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(a.own.workers / kOwnWaves)), block(kOwnWaves * kWave);
+  if (a.own.unit_rows == 16)
+    hipLaunchKernelGGL((k_own_rows<DT, D, FMT, 1>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_own_rows<DT, D, FMT, 2>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+template <class DT, int D, int FMT>
+hipError_t launch_shared_d(const SharedArgs& a, hipStream_t st) {
+  const hipError_t e = launch_narrow<DT, D, FMT>(a, st);
+  return e != hipSuccess ? e : launch_own<DT, D, FMT>(a, st);
+}
 template <class DT, int FMT>
-hipError_t launch_shared_format(const PagedAttnArgs& a, int D, hipStream_t st) {
-  if (a.row_tiles == 1) return D == 64 ? launch_shared_rt<DT, 64, FMT, 1>(a, st) : launch_shared_rt<DT, 128, FMT, 1>(a, st);
-  return D == 64 ? launch_shared_rt<DT, 64, FMT, 2>(a, st) : launch_shared_rt<DT, 128, FMT, 2>(a, st);
+hipError_t launch_shared_format(const SharedArgs& a, int D, hipStream_t st) {
+  return D == 64 ? launch_shared_d<DT, 64, FMT>(a, st) : launch_shared_d<DT, 128, FMT>(a, st);
 }
 
 }  // namespace dev

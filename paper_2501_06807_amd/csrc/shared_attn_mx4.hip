@@ -3,7 +3,7 @@
 
 namespace mpc {
 
-hipError_t launch_shared_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st) {
+hipError_t launch_shared_mx4(const SharedArgs& a, int dtype, int D, hipStream_t st) {
   if (dtype == MPC_FP32) return dev::launch_shared_format<F32, MPC_PAGE_MX4>(a, D, st);
   if (dtype == MPC_FP16) return dev::launch_shared_format<F16, MPC_PAGE_MX4>(a, D, st);
   return dev::launch_shared_format<BF16, MPC_PAGE_MX4>(a, D, st);
