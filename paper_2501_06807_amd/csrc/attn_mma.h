@@ -25,6 +25,31 @@ __device__ __forceinline__ f32x4 mma(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// The same in 32x32x16 products.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class DT>
+__device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, f32x16 c) {
+  if constexpr (DT::kCode == MPC_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that 16 rows' pieces of one column fall into
+// different banks, for the fragments of K (a chunk of 32 rows), and for the transposing reads of V (two chunks of four rows).
+// Cycles to a wave's read, as the shader clock counts them: K 4.1 (eight rows apart only: 7.8, not exchanged: 48), V 4.0
+// (not exchanged: 8.0).
+template <int D>
+__device__ __forceinline__ int tile_chunk_k(int row, int c) {
+  return row * (D / 8) + (c ^ (D == 128 ? row & 15 : row >> 1 & 7));
+}
+template <int D>
+__device__ __forceinline__ int tile_chunk_v(int row, int c) {
+  return row * (D / 8) + (c ^ ((row & 3) << 1));
+}
+
 // Two fp32 values as a pair of the 16-bit type, to nearest even.
 template <class DT>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {

@@ -96,10 +96,10 @@ hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream
 // have of each row of a unit: the worker that has a unit's first block in `head`, by row, the ones that go on with it in `more`, a
 // place for each worker (whose run goes on with one unit at most).
 constexpr int kMaxGroups = 1024;
-constexpr int kPartTail = 2;  // maximum and sum, behind a row's D accumulators
+constexpr int kPartTail = 4;  // maximum and sum behind a row's D accumulators, and what keeps rows 16-byte aligned
 struct Parts {
-  float* head;   // [L][Hkv][B][n G][D + 2]
-  float* more;   // [workers][unit rows][D + 2]
+  float* head;   // [L][Hkv][B][n G][D + 4]
+  float* more;   // [workers][unit rows][D + 4]
   int unit_rows, workers;
 };
 // A group: sequences [f0, f1), shared rows [0, base), the tiles of them that its rows look at (the first `skip`, then those from
@@ -132,8 +132,9 @@ struct SharedPlan {
   long long blocks;  // the more of both kinds, at most
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
+constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
 constexpr int kOwnWaves = 4;  // waves of a workgroup that takes own rows
-SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
+SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_fp16(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_bf16(const SharedArgs& a, int D, hipStream_t st);

@@ -26,17 +26,6 @@ namespace {
 
 using namespace dev;
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-template <class DT>
-__device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, f32x16 c) {
-  if constexpr (DT::kCode == MPC_BF16)
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
 constexpr int kRowsWave = 32, kRowsGroup = 4 * kRowsWave;
 constexpr float kSlack = 8.f;  // log2 of how far a weight may pass 1 before its row's reference moves
 
@@ -71,19 +60,6 @@ __device__ __forceinline__ Tiles tiles_of(const AttnArgs& a, int lo, int hi, int
 // Whether any row at positions lo .. hi sees any of the keys [k0, k1].
 __device__ __forceinline__ bool seen_by(const AttnArgs& a, int k0, int k1, int lo, int hi, int rows) {
   return k0 <= hi && k0 < rows && (!a.window || k1 > lo - a.window || k0 < a.sinks);
-}
-
-// LDS tiles: rows of D elements, 16-byte chunks exchanged within the row so that 16 rows' pieces of one column fall into
-// different banks, for the fragments of K (a chunk of 32 rows), and for the transposing reads of V (two chunks of four rows).
-// Cycles to a wave's read, as the shader clock counts them: K 4.1 (eight rows apart only: 7.8, not exchanged: 48), V 4.0
-// (not exchanged: 8.0).
-template <int D>
-__device__ __forceinline__ int k_chunk(int row, int c) {
-  return row * (D / 8) + (c ^ (D == 128 ? row & 15 : row >> 1 & 7));
-}
-template <int D>
-__device__ __forceinline__ int v_chunk(int row, int c) {
-  return row * (D / 8) + (c ^ ((row & 3) << 1));
 }
 
 template <class DT, int D, int NS>
@@ -168,8 +144,8 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
       const int x = tid + n * THREADS;
-      s_k[grp][buf][k_chunk<D>(x / CH, x % CH)] = kr[n];
-      s_v[grp][buf][v_chunk<D>(x / CH, x % CH)] = vr[n];
+      s_k[grp][buf][tile_chunk_k<D>(x / CH, x % CH)] = kr[n];
+      s_v[grp][buf][tile_chunk_v<D>(x / CH, x % CH)] = vr[n];
     }
   };
   auto staged_not_finite = [&]() {
@@ -192,7 +168,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int row = 32 * kb + 16 * st + 8 * e + vrow;
-          const char* at = sv + v_chunk<D>(row, 4 * d + vcol) * 16 + vbyte;
+          const char* at = sv + tile_chunk_v<D>(row, 4 * d + vcol) * 16 + vbyte;
           const auto x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
           const uint2 y = __builtin_bit_cast(uint2, x);
           v[d][2 * e] = y.x;
@@ -204,7 +180,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_prompt(PromptAttnArgs a) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) kf[kb][ks] = sk[k_chunk<D>(kb * 32 + q32, 2 * ks + hl)];
+      for (int ks = 0; ks < KSTEPS; ++ks) kf[kb][ks] = sk[tile_chunk_k<D>(kb * 32 + q32, 2 * ks + hl)];
     // the values are asked for before the scores are taken, so that they are there when the weights are
     uint32_t vf[KB][2][DB][4];
 #pragma unroll

@@ -219,18 +219,18 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 
 }  // namespace
 
-// Units of as many query rows as a group has on average, up to 32; own rows in units of 16 where a sequence's fit, else 32. Blocks
+// Units of as many query rows as a group has on average, up to 32, and of 128 in 16-bit types beyond that; own rows in units of 16 where a sequence's fit, else 32. Blocks
 // are a tile to each wave of a workgroup (shared rows), and 128 keys to a wave (own rows).
-SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
+SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
   SharedPlan p{};
   const long long each_seq = (long long)n * (Hq / Hkv), rows = B * each_seq, each = (rows + groups - 1) / groups, lh = (long long)L * Hkv;
-  (void)format;
-  p.shared_rows = each <= 16 ? 16 : 32;
+  p.wide = dtype != MPC_FP32 && each > 32;
+  p.shared_rows = p.wide ? 128 : each <= 16 ? 16 : 32;
   p.own_rows = each_seq <= 16 ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
-  p.shared_block = paged_waves(p.shared_rows / 16);
+  p.shared_block = p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16);
   p.own_block = 128 / p.tile;
-  p.shared_workers = kNumCU;
+  p.shared_workers = p.wide ? kNumCU * 2 / kWideGroups : kNumCU;
   p.own_workers = kNumCU * kOwnWaves * (p.own_rows == 16 ? 2 : 1);
   auto blocks = [&](long long units, long long block) {
     const double nb = cap / (p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short

@@ -229,15 +229,5 @@ hipError_t launch_own(const SharedArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <class DT, int D, int FMT>
-hipError_t launch_shared_d(const SharedArgs& a, hipStream_t st) {
-  const hipError_t e = launch_narrow<DT, D, FMT>(a, st);
-  return e != hipSuccess ? e : launch_own<DT, D, FMT>(a, st);
-}
-template <class DT, int FMT>
-hipError_t launch_shared_format(const SharedArgs& a, int D, hipStream_t st) {
-  return D == 64 ? launch_shared_d<DT, 64, FMT>(a, st) : launch_shared_d<DT, 128, FMT>(a, st);
-}
-
 }  // namespace dev
 }  // namespace mpc

@@ -1,5 +1,5 @@
 // Attention behind shared rows, fp32 caches (one file per element type: they build in parallel).
-#include "shared_attn_dev.h"
+#include "shared_launch.h"
 
 namespace mpc {
 

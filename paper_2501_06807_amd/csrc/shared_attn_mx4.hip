@@ -1,5 +1,5 @@
 // Attention behind shared rows, caches of 4-bit codes.
-#include "shared_attn_dev.h"
+#include "shared_launch.h"
 
 namespace mpc {
 

@@ -1,0 +1,397 @@
+// Attention behind shared rows, 16-bit types: the kernel of the shared rows for units of 128 query rows.
+//
+// A workgroup has NS groups of four waves, a wave 32 of the unit's rows; the groups take every NS-th tile of 32 keys. A tile goes
+// through LDS once for the four waves, double-buffered, the next one in registers meanwhile; codes become 16-bit values on the
+// way. S^T = K Q^T and O^T += V^T P^T are 32x32x16 products, as in the prompt attention: a lane has 16 scores of one row for
+// each 32 keys, and its weights, packed, are the next product's operand; V comes from LDS through the transposing reads.
+// A row's reference moves only when a score passes it by 2^8. Weights are rounded once to the type; over codes fp16 takes them
+// in two bf16 parts, since values times page or block scales have no place in fp16's range.
+#pragma once
+#include "shared_attn_dev.h"
+
+namespace mpc {
+namespace dev {
+
+template <class DT, int D, int FMT, int NS>
+__global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
+  constexpr bool C8 = FMT == MPC_PAGE_E4M3, C4 = FMT == MPC_PAGE_MX4, CODES = C8 || C4;
+  constexpr bool H = DT::kCode == MPC_FP16, SPLIT = C4 && H, TWO = CODES && H;
+  using QT = std::conditional_t<C4, BF16, DT>;    // type of the scores' product
+  using PV = std::conditional_t<CODES, BF16, DT>;  // and of the values'
+  constexpr int KT = 32, CH = D / 8, KSTEPS = D / 16, DB = D / 32, THREADS = 256, PS = D + kPartTail;
+  constexpr float LIFT = PV::kCode == MPC_FP16 ? 7.f : 0.f;  // of the weights' exponents, also in their sum
+  constexpr float SLACK = 8.f;                               // log2 of how far a weight may pass 1 before its reference moves
+  constexpr int PER = CODES ? 1 : KT * CH / THREADS;         // pieces of K (and of V) that a thread stages
+  constexpr int PCH = CODES ? D / 8 : 8;                     // channels of a piece
+  constexpr int RB = C4 ? D / 2 : C8 ? D : 2 * D;            // bytes of a page's row
+  __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
+  __shared__ int s_bad[NS][2];     // the last round whose values, staged for an edge, were not all finite
+  __shared__ int s_range[4][2];    // positions of the waves' rows
+  const PagedCache& c = a.c;
+  const int tid = threadIdx.x % THREADS, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
+  const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+
+  const unsigned total = load_uniform(&a.total->shared), id = by_die(blockIdx.x, gridDim.x);
+  const unsigned per = (total + gridDim.x - 1) / gridDim.x;
+  if ((unsigned long long)id * per >= total) return;
+  const unsigned first = id * per, last = min(first + per, total);
+  int gi = last_from(a.groups, first, [&](int i) { return a.group[i].block0; });
+  // a negative scale is taken into the queries (8-bit codes: it stays with the pages' scales); zero times a masked score would be
+  // NaN: the smallest number that is not zero instead
+  const float qs = C8 ? a.qscale : fmaxf(fabsf(a.qscale), 0x1p-149f);
+  const uint32_t flip = !C8 && a.qscale < 0.f ? 0x80008000u : 0u;
+
+  unsigned x = first;
+  while (x < last) {
+    while (gi + 1 < a.groups && x >= load_uniform(&a.group[gi + 1].block0)) ++gi;
+    const SharedGroup* gp = a.group + gi;
+    const int f0 = load_uniform(&gp->f0), f1 = load_uniform(&gp->f1), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
+    const int base = load_uniform(&gp->base), skip = load_uniform(&gp->skip), at = load_uniform(&gp->at);
+    const unsigned in = x - load_uniform(&gp->block0);
+    const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
+    const int blk_end = min(nb, blk + (int)(last - x));
+    const int lh = u / rts, h = lh % a.Hkv, l = lh / a.Hkv, r0 = u % rts * 128;
+    const int i0 = blk * a.shared_block, i1 = min(blk_end * a.shared_block, load_uniform(&gp->tiles));
+
+    const SharedRow row = shared_row(a, f0, f1, r0 + 32 * wave + q32);
+    // a row that is not there sees every key, so that it makes no tile an edge; nobody reads it
+    const int pos = row.live ? row.pos : kMaxRows;
+    int lo = row.live ? pos : kMaxRows, hi = row.live ? pos : -kMaxRows;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      lo = min(lo, __shfl_xor(lo, o));
+      hi = max(hi, __shfl_xor(hi, o));
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    if (lane == 0 && grp == 0) {
+      s_range[wave][0] = lo;
+      s_range[wave][1] = hi;
+    }
+    if (threadIdx.x < 2 * NS) (&s_bad[0][0])[threadIdx.x] = -1;
+    uint4 q[KSTEPS], q2[SPLIT ? KSTEPS : 1];
+    {
+      const int t = row.in_seq >> a.log_g, hq = (h << a.log_g) + row.in_seq - (t << a.log_g);
+      const char* p = a.q.at(l, row.b, hq, t) + hl * 16;
+#pragma unroll
+      for (int i = 0; i < KSTEPS; ++i) {
+        const uint4 y = ldg16(p + i * 32);
+        q[i] = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
+        if constexpr (SPLIT) split_bf16(q[i], q2[i]);
+      }
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    float ref = -INFINITY, sum = 0.f;  // reference (in units of the exponent) and sum over this lane's keys
+    __syncthreads();
+    int g_lo = kMaxRows, g_hi = -kMaxRows;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      g_lo = min(g_lo, s_range[i][0]);
+      g_hi = max(g_hi, s_range[i][1]);
+    }
+    g_lo = __builtin_amdgcn_readfirstlane(g_lo);
+    g_hi = __builtin_amdgcn_readfirstlane(g_hi);
+
+    // The run's tiles: first those that some row may not see whole (ahead of [w0, w1) and behind it), then those that every row
+    // sees as far as their pages have rows.
+    int w0 = i0, w1 = min(i1, (max(g_lo, -1) + 1) / KT - (a.window ? at - skip : 0));
+    if (a.window) w0 = skip + max(0, (max(g_hi - a.window + 1, 0) + KT - 1) / KT - at);
+    w0 = min(max(w0, i0), i1);
+    w1 = max(w1, w0);
+    const int edges = w0 - i0 + i1 - w1;
+    auto key0 = [&](int j) {
+      const int i = j >= edges ? w0 + j - edges : j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0);
+      return (i < skip ? i : i - skip + at) * KT;
+    };
+    auto page_at = [&](int i, int hf) { return (key0(i) + 16 * hf) >> c.log_page; };
+    int entry[2], pid[2];
+    auto ask = [&](int i) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) entry[hf] = page_entry(c, f0, page_at(i, hf));
+    };
+    uint4 kr[PER], vr[PER];
+    uint32_t kx = 0, vx = 0;                       // 4-bit codes: the piece's scale bytes
+    float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};  // 8-bit codes: the halves' page scales
+    auto fetch = [&](int i) {
+      size_t at_row[2];  // row 0 of a half in the pool (page 0 where it has no page: its rows are not used)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        pid[hf] = page_of_entry(c, entry[hf], page_at(i, hf));
+        at_row[hf] = page_unit(c, l, max(pid[hf], 0), h) * c.page + ((key0(i) + 16 * hf) & (c.page - 1));
+        if constexpr (C8) {
+          ks[hf] = load_uniform(c.ks + (at_row[hf] >> c.log_page));
+          vs[hf] = load_uniform(c.vs + (at_row[hf] >> c.log_page));
+        }
+      }
+      if constexpr (CODES) {
+        const int r = tid / 8, piece = tid % 8;  // (a wave's rows lie in one half)
+        const size_t rr = (wave >= 2 ? at_row[1] : at_row[0]) + (r & 15);
+        const char *kp = c.k + rr * RB + piece * (RB / 8), *vp = c.v + rr * RB + piece * (RB / 8);
+        if constexpr (RB / 8 == 16) {
+          kr[0] = ldg16(kp);
+          vr[0] = ldg16(vp);
+        } else if constexpr (RB / 8 == 8) {
+          const uint2 y = *(const uint2*)kp, z = *(const uint2*)vp;
+          kr[0] = make_uint4(y.x, y.y, 0, 0);
+          vr[0] = make_uint4(z.x, z.y, 0, 0);
+        } else {
+          kr[0] = make_uint4(*(const uint32_t*)kp, 0, 0, 0);
+          vr[0] = make_uint4(*(const uint32_t*)vp, 0, 0, 0);
+        }
+        if constexpr (C4) {
+          const size_t s_at = (rr >> c.log_page) * (size_t)(D / kMx4Block * c.page) + piece * PCH / kMx4Block * c.page + (rr & (c.page - 1));
+          kx = c.kx[s_at];
+          vx = c.vx[s_at];
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+          const int y = tid + n * THREADS, r = y / CH;  // (a half to each n, or to each pair of waves)
+          const size_t rr = ((PER == 2 ? n == 1 : wave >= 2) ? at_row[1] : at_row[0]) + (r & 15);
+          kr[n] = ldg16(c.k + rr * RB + y % CH * 16);
+          vr[n] = ldg16(c.v + rr * RB + y % CH * 16);
+        }
+      }
+    };
+    // Eight channels of a piece as 16-bit values.
+    auto widened = [&](auto type, const uint4& y, int part, uint32_t xb) {
+      using T = decltype(type);
+      if constexpr (C4) {
+        return widen8(part == 0 ? y.x : y.y, mx4_scale(xb));
+      } else {
+        const uint32_t w0 = part == 0 ? y.x : y.z, w1 = part == 0 ? y.y : y.w;
+        return make_uint4(widen2<T, false>(w0), widen2<T, true>(w0), widen2<T, false>(w1), widen2<T, true>(w1));
+      }
+    };
+    // Stages the fetched tile, with zeros for values that have no page; whether it held values that are not finite (edge).
+    auto stash = [&](auto edge_, int buf, const bool* have) {
+      constexpr bool edge = decltype(edge_)::value;
+      uint32_t top = 0;
+      auto seen = [&](const uint4& y) { top = max_magnitude(max_magnitude(max_magnitude(max_magnitude(top, y.x), y.y), y.z), y.w); };
+      if constexpr (CODES) {
+        const int r = tid / 8, piece = tid % 8;
+#pragma unroll
+        for (int n = 0; n < PCH / 8; ++n) {
+          const int chunk = piece * (PCH / 8) + n;
+          uint4 y = widened(PV{}, vr[0], n, vx);
+          if (!(wave >= 2 ? have[1] : have[0])) y = make_uint4(0, 0, 0, 0);
+          if (edge) seen(y);
+          s_k[grp][buf][tile_chunk_k<D>(r, chunk)] = widened(QT{}, kr[0], n, kx);
+          s_v[grp][buf][tile_chunk_v<D>(r, chunk)] = y;
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+          const int y = tid + n * THREADS;
+          if (!((PER == 2 ? n == 1 : wave >= 2) ? have[1] : have[0])) vr[n] = make_uint4(0, 0, 0, 0);
+          if (edge) seen(vr[n]);
+          s_k[grp][buf][tile_chunk_k<D>(y / CH, y % CH)] = kr[n];
+          s_v[grp][buf][tile_chunk_v<D>(y / CH, y % CH)] = vr[n];
+        }
+      }
+      return not_finite<PV>(top);
+    };
+    // The tile of round n at key k0; EDGE: some row of the wave may not see some key of it.
+    auto tile = [&](auto edge, int k0, int buf, int n, const bool* have, const float* kss, const float* vss) {
+      constexpr bool EDGE = decltype(edge)::value;
+      const uint4* sk = s_k[grp][buf];
+      const char* sv = (const char*)s_v[grp][buf];
+      // places 0..3 and 4..7 of half hl in a product over 16 keys are keys 4 hl .. and 8 + 4 hl ..
+      const int vrow = 4 * hl + ((lane & 15) >> 2);  // row whose piece this lane asks for, and the piece's 16-byte chunk
+      const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
+      const int bad = EDGE ? s_bad[grp][buf] : 0;
+      uint4 kf[KSTEPS];
+#pragma unroll
+      for (int i = 0; i < KSTEPS; ++i) kf[i] = sk[tile_chunk_k<D>(q32, 2 * i + hl)];
+      // the values are asked for before the scores are taken, so that they are there when the weights are
+      uint32_t vf[2][DB][4];
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const char* p = sv + tile_chunk_v<D>(16 * st + 8 * e + vrow, 4 * d + vcol) * 16 + vbyte;
+            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+            vf[st][d][2 * e] = y.x;
+            vf[st][d][2 * e + 1] = y.y;
+          }
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 s;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KSTEPS; ++i) {
+        if constexpr (SPLIT) s = mma32<QT>(kf[i], q2[i], s);
+        s = mma32<QT>(kf[i], q[i], s);
+      }
+      // the lane's keys lie 8 (r / 4) + r % 4 behind this one
+      const int j0 = k0 + 4 * hl;
+      auto sees = [&](int j) { return j <= pos && (!a.window || j > pos - a.window || j < a.sinks); };  // (of those that exist)
+      const float cc[2] = {C8 ? (have[0] ? qs * kss[0] : 1.f) : qs, C8 ? (have[1] ? qs * kss[1] : 1.f) : qs};
+      auto key = [&](int r) { return j0 + 8 * (r >> 2) + (r & 3); };
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+        if (!have[hf])
+#pragma unroll
+          for (int r = 0; r < 8; ++r) s[8 * hf + r] = -INFINITY;
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (C8) {
+          const float y = s[r] * cc[r >> 3];
+          top = fmaxf(top, !EDGE || sees(key(r)) ? y : -INFINITY);
+        } else {
+          if constexpr (EDGE) s[r] = sees(key(r)) ? s[r] : -INFINITY;
+          top = fmaxf(top, s[r]);
+        }
+      }
+      if constexpr (!C8) top *= qs;
+      if (__any(top > ref + SLACK || (ref == -INFINITY && top > -INFINITY))) {
+        top = xor_combine<32>(top, [](float p, float q) { return fmaxf(p, q); });
+        const float was = ref;
+        ref = top == -INFINITY ? ref : fmaxf(ref, top);
+        // exp2(-inf - 0) = 0: nothing was there to move
+        const float move = fast_exp2(was - (ref == -INFINITY ? 0.f : ref));
+        sum *= move;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= move;
+      }
+      const float zero = (ref == -INFINITY ? 0.f : ref) - LIFT;
+      uint32_t p[8], p2[TWO ? 8 : 1];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float w0 = fast_exp2(fmaf(s[r], cc[r >> 3], -zero)), w1 = fast_exp2(fmaf(s[r + 1], cc[r >> 3], -zero));
+        if constexpr (C8 && EDGE) {
+          w0 = sees(key(r)) ? w0 : 0.f;
+          w1 = sees(key(r + 1)) ? w1 : 0.f;
+        }
+        sum += w0 + w1;
+        if constexpr (C8) {  // a page that the row sees nothing of does not reach it, whatever its scale is
+          const float f = have[r >> 3] ? vss[r >> 3] : 0.f;
+          w0 = EDGE && w0 == 0.f ? 0.f : w0 * f;
+          w1 = EDGE && w1 == 0.f ? 0.f : w1 * f;
+        }
+        p[r / 2] = pack2<PV>(w0, w1);
+        if constexpr (TWO) p2[r / 2] = pack2<PV>(w0 - bf16_to_f32(p[r / 2] & 0xFFFFu), w1 - bf16_to_f32(p[r / 2] >> 16));
+      }
+      // O^T += V^T P^T, 16 keys at a time
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const uint4 w = make_uint4(p[4 * st], p[4 * st + 1], p[4 * st + 2], p[4 * st + 3]);
+        uint32_t(*v)[4] = vf[st];
+        if constexpr (EDGE) {
+          // Values that are not finite, in keys that some row does not see, must not meet that row's weight of zero: they are
+          // added apart, to the rows that see them
+          if (__builtin_amdgcn_readfirstlane(bad) == n) {
+            float one[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) one[e] = sees(j0 + 16 * st + (e >= 4 ? 8 : 0) + (e & 3)) ? 1.f : 0.f;
+            const uint4 w1 = make_uint4(pack2<PV>(one[0], one[1]), pack2<PV>(one[2], one[3]), pack2<PV>(one[4], one[5]), pack2<PV>(one[6], one[7]));
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+              uint32_t what[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) what[e] = take_not_finite<PV>(v[d][e]);
+              f32x16 y;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) y[r] = 0.f;
+              y = mma32<PV>(make_uint4(what[0], what[1], what[2], what[3]), w1, y);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[d][r] += not_finite_sum(y[r]);
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const uint4 y = make_uint4(v[d][0], v[d][1], v[d][2], v[d][3]);
+          if constexpr (TWO) o[d] = mma32<PV>(y, make_uint4(p2[4 * st], p2[4 * st + 1], p2[4 * st + 2], p2[4 * st + 3]), o[d]);
+          o[d] = mma32<PV>(y, w, o[d]);
+        }
+      }
+    };
+
+    const int tiles = i1 - i0, rounds = (tiles + NS - 1) / NS, edge_rounds = (edges + NS - 1) / NS;
+    if (grp < tiles) {
+      ask(grp);
+      fetch(grp);
+      ask(min(grp + NS, tiles - 1));
+    }
+    auto round = [&](auto edge, int n) {
+      constexpr bool EDGE = decltype(edge)::value;
+      const int j = n * NS + grp, buf = n & 1;
+      const int k0 = key0(j);
+      const bool have[2] = {pid[0] >= 0 && k0 < base, pid[1] >= 0 && k0 + 16 < base};
+      const float kss[2] = {ks[0], ks[1]}, vss[2] = {vs[0], vs[1]};
+      if (j < tiles && stash(edge, buf, have) && EDGE) s_bad[grp][buf] = n;
+      __syncthreads();
+      if (j + NS < tiles) {
+        fetch(j + NS);
+        ask(min(j + 2 * NS, tiles - 1));
+      }
+      if (j < tiles && lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
+    };
+    for (int n = 0; n < edge_rounds; ++n) round(std::true_type{}, n);
+    for (int n = edge_rounds; n < rounds; ++n) round(std::false_type{}, n);
+
+    sum = xor_combine<32>(sum, [](float p, float q) { return p + q; });
+    if constexpr (NS == 2) {
+      // the second group's part to the first, through the tiles' LDS
+      constexpr int HALF = DB / 2;
+      float* s_o = (float*)&s_k[0][0][0];  // [4 waves][HALF * 16][64 lanes] each for a half of the channels
+      float* s_st = (float*)&s_v[0][0][0];
+      const float mine = ref;
+      __syncthreads();
+      if (grp == 1) {
+        s_st[(wave * 2) * kWave + lane] = ref;
+        s_st[(wave * 2 + 1) * kWave + lane] = sum;
+      }
+      __syncthreads();
+      float p0 = 1.f, p1 = 0.f;
+      if (grp == 0) {
+        const float r1 = s_st[(wave * 2) * kWave + lane], sum1 = s_st[(wave * 2 + 1) * kWave + lane];
+        ref = fmaxf(mine, r1);
+        const float b0 = ref == -INFINITY ? 0.f : ref;
+        p0 = fast_exp2(mine - b0);
+        p1 = fast_exp2(r1 - b0);
+        sum = sum * p0 + sum1 * p1;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        __syncthreads();
+        if (grp == 1)
+#pragma unroll
+          for (int d = 0; d < HALF; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s_o[((wave * HALF + d) * 16 + r) * kWave + lane] = o[e * HALF + d][r];
+        __syncthreads();
+        if (grp == 0)
+#pragma unroll
+          for (int d = 0; d < HALF; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              o[e * HALF + d][r] = o[e * HALF + d][r] * p0 + s_o[((wave * HALF + d) * 16 + r) * kWave + lane] * p1;
+      }
+    }
+    if (grp == 0 && row.live) {
+      float* part = blk == 0 ? a.shared.head + part_row(a, lh, row.b, row.in_seq) * PS : a.shared.more + ((size_t)id * 128 + 32 * wave + q32) * PS;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) *(float4*)(part + 32 * d + 2 * r + 4 * hl) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+      if (hl == 0) *(float2*)(part + D) = make_float2(ref - LIFT, sum);
+    }
+    __syncthreads();  // the LDS buffers are free again
+    x += blk_end - blk;
+  }
+}
+
+}  // namespace dev
+}  // namespace mpc
