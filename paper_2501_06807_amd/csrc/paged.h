@@ -132,7 +132,7 @@ struct SharedPlan {
   long long blocks;  // the more of both kinds, at most
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
-constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
+constexpr int kWideGroups = 1;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
 constexpr int kOwnWaves = 4;  // waves of a workgroup that takes own rows
 SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);

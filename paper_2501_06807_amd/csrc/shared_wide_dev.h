@@ -104,25 +104,29 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     w0 = min(max(w0, i0), i1);
     w1 = max(w1, w0);
     const int edges = w0 - i0 + i1 - w1;
-    auto key0 = [&](int j) {
-      const int i = j >= edges ? w0 + j - edges : j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0);
-      return (i < skip ? i : i - skip + at) * KT;
-    };
-    auto page_at = [&](int i, int hf) { return (key0(i) + 16 * hf) >> c.log_page; };
-    int entry[2], pid[2];
-    auto ask = [&](int i) {
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) entry[hf] = page_entry(c, f0, page_at(i, hf));
+    auto key_of = [&](int i) { return (i < skip ? i : i - skip + at) * KT; };
+    const int whole0 = key_of(w0) - edges * KT;  // (whole tiles lie side by side)
+    auto key0 = [&](int j) { return j >= edges ? whole0 + j * KT : key_of(j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0)); };
+    // Table entries of 64 pages from page `ev0` on, a lane to each: a tile's page ids cost no load.
+    int ev = 0, ev0 = -kWave, pid[2];
+    auto ids_at = [&](int k0) {
+      const int pa = k0 >> c.log_page, pb = (k0 + 16) >> c.log_page;
+      if (pa < ev0 || pb >= ev0 + kWave) {
+        ev0 = pa;
+        ev = c.table[(size_t)f0 * c.max_pages + min(pa + lane, c.max_pages - 1)];
+      }
+      pid[0] = page_of_entry(c, __builtin_amdgcn_readlane(ev, pa - ev0), pa);
+      pid[1] = page_of_entry(c, __builtin_amdgcn_readlane(ev, pb - ev0), pb);
     };
     uint4 kr[PER], vr[PER];
     uint32_t kx = 0, vx = 0;                       // 4-bit codes: the piece's scale bytes
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};  // 8-bit codes: the halves' page scales
-    auto fetch = [&](int i) {
+    auto fetch = [&](int k0) {
+      ids_at(k0);
       size_t at_row[2];  // row 0 of a half in the pool (page 0 where it has no page: its rows are not used)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        pid[hf] = page_of_entry(c, entry[hf], page_at(i, hf));
-        at_row[hf] = page_unit(c, l, max(pid[hf], 0), h) * c.page + ((key0(i) + 16 * hf) & (c.page - 1));
+        at_row[hf] = page_unit(c, l, max(pid[hf], 0), h) * c.page + ((k0 + 16 * hf) & (c.page - 1));
         if constexpr (C8) {
           ks[hf] = load_uniform(c.ks + (at_row[hf] >> c.log_page));
           vs[hf] = load_uniform(c.vs + (at_row[hf] >> c.log_page));
@@ -235,11 +239,11 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
       auto sees = [&](int j) { return j <= pos && (!a.window || j > pos - a.window || j < a.sinks); };  // (of those that exist)
       const float cc[2] = {C8 ? (have[0] ? qs * kss[0] : 1.f) : qs, C8 ? (have[1] ? qs * kss[1] : 1.f) : qs};
       auto key = [&](int r) { return j0 + 8 * (r >> 2) + (r & 3); };
+      if (!(have[0] && have[1])) {
+        asm volatile("");  // (a branch, not a selection for each score)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-        if (!have[hf])
-#pragma unroll
-          for (int r = 0; r < 8; ++r) s[8 * hf + r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) s[r] = have[r >> 3] ? s[r] : -INFINITY;
+      }
       float top = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -320,22 +324,17 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
 
     const int tiles = i1 - i0, rounds = (tiles + NS - 1) / NS, edge_rounds = (edges + NS - 1) / NS;
     if (grp < tiles) {
-      ask(grp);
-      fetch(grp);
-      ask(min(grp + NS, tiles - 1));
+      fetch(key0(grp));
     }
     auto round = [&](auto edge, int n) {
       constexpr bool EDGE = decltype(edge)::value;
       const int j = n * NS + grp, buf = n & 1;
-      const int k0 = key0(j);
+      const int k0 = EDGE ? key0(j) : whole0 + j * KT;
       const bool have[2] = {pid[0] >= 0 && k0 < base, pid[1] >= 0 && k0 + 16 < base};
       const float kss[2] = {ks[0], ks[1]}, vss[2] = {vs[0], vs[1]};
       if (j < tiles && stash(edge, buf, have) && EDGE) s_bad[grp][buf] = n;
       __syncthreads();
-      if (j + NS < tiles) {
-        fetch(j + NS);
-        ask(min(j + 2 * NS, tiles - 1));
-      }
+      if (j + NS < tiles) fetch(EDGE ? key0(j + NS) : k0 + NS * KT);
       if (j < tiles && lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
     };
     for (int n = 0; n < edge_rounds; ++n) round(std::true_type{}, n);
