@@ -102,15 +102,15 @@ struct Parts {
   float* more;   // [workers][unit rows][D + 4]
   int unit_rows, workers;
 };
-// A group: sequences [f0, f1), shared rows [0, base), the tiles of them that its rows look at (the first `skip`, then those from
+// A group: sequences [f0, f1), their query rows (to a kv head) from number row0 on, shared rows [0, base), the tiles of them that its rows look at (the first `skip`, then those from
 // `at` on), blocks of keys nb and units of query rows rt to a (layer, kv head); blocks of the groups before it.
 struct SharedGroup {
-  int f0, f1, base, skip, at, tiles, nb, rt;
+  int f0, f1, row0, query_rows, base, skip, at, tiles, nb, rt;
   unsigned block0;
 };
-// A sequence: rows that its group shares, group (-1: none), blocks of its own keys, blocks of the sequences before it.
+// A sequence: number of its first query row, rows that its group shares, group (-1: none), blocks of its own keys, blocks of the sequences before it.
 struct SharedSeq {
-  int base, group, nb;
+  int row0, base, group, nb;
   unsigned block0;
 };
 struct SharedTotals {
@@ -132,7 +132,7 @@ struct SharedPlan {
   long long blocks;  // the more of both kinds, at most
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
-constexpr int kWideGroups = 1;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
+constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
 constexpr int kOwnWaves = 4;  // waves of a workgroup that takes own rows
 SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);

@@ -53,11 +53,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
     s_hi[tid] = -1;
   }
   __syncthreads();
-  unsigned own = 0;  // blocks of the sequences so far
+  unsigned own = 0, rows = 0;  // blocks and query rows of the sequences so far
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
-    SharedSeq q{0, -1, 0, 0};
-    unsigned blocks = 0;
+    SharedSeq q{0, 0, -1, 0, 0};
+    unsigned blocks = 0, mine = 0;
     if (b < a.B) {
       if (b >= s_f[0] && b < s_f[ng]) {  // the last group that begins at or before b
         int g = 0, z = ng;
@@ -75,10 +75,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
       }
       q.nb = (s.all + a.own_block - 1) / a.own_block;
       blocks = (unsigned)(s.groups * a.L * a.Hkv) * (unsigned)q.nb;
+      mine = (unsigned)s.valid << a.log_g;
     }
     unsigned all;
     q.block0 = own + sum_before(blocks, s_wave, &all);
     own += all;
+    q.row0 = (int)(rows + sum_before(mine, s_wave, &all));
+    rows += all;
     if (b < a.B) a.seq[b] = q;
   }
   __syncthreads();
@@ -87,8 +90,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
     p.f0 = s_f[tid];
     p.f1 = s_f[tid + 1];
     p.base = s_base[tid];
-    const long long rows = (long long)(p.f1 - p.f0) * ((long long)c.n_new << a.log_g);
-    p.rt = (int)((rows + a.shared.unit_rows - 1) / a.shared.unit_rows);
+    p.row0 = p.f0 < a.B ? a.seq[p.f0].row0 : (int)rows;
+    p.query_rows = (p.f1 < a.B ? a.seq[p.f1].row0 : (int)rows) - p.row0;
+    p.rt = (p.query_rows + a.shared.unit_rows - 1) / a.shared.unit_rows;
     const int all = (max(0, min(p.base, s_hi[tid] + 1)) + a.tile - 1) / a.tile;
     p.skip = p.at = all;
     if (a.window) {
@@ -104,20 +108,23 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
   if (tid == 0) *a.total = SharedTotals{total, own};
 }
 
-// The join: a wave to a query row, whose parts are those of its own rows and of the shared ones.
-template <class DT, int D>
+// The join. A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the shared ones; where
+// there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
+template <class DT, int D, bool ALL>
 __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
-  constexpr int PS = D + kPartTail;
+  constexpr int PS = D + kPartTail, LANES = D / 4, TEAMS = kJoinThreads / LANES, T = ALL ? TEAMS : 1, AHEAD = 4;
+  __shared__ float4 s_x[ALL ? TEAMS : 1][LANES];
+  __shared__ float2 s_ml[ALL ? TEAMS : 1];
   const PagedCache& c = a.c;
-  const int lane = threadIdx.x % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int team = threadIdx.x / LANES, e = threadIdx.x % LANES * 4, way = ALL ? team : 0;
   const int per = c.n_new << a.log_g;
-  const long long row = (long long)blockIdx.x * (kJoinThreads / kWave) + wave;
+  const long long row = ALL ? (long long)blockIdx.x : (long long)blockIdx.x * TEAMS + team;
   if (row >= (long long)a.L * a.Hkv * a.B * per) return;
-  const int in_seq = (int)(row % per), lhb = (int)(row / per), b = lhb % a.B, lh = lhb / a.B;
-  const int t = in_seq >> a.log_g, valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
+  const int in_seq = (int)(row % per), lhb = (int)(row / per), b = lhb % a.B, lh = lhb / a.B, t = in_seq >> a.log_g;
+  const int valid = c.valid(b);
   if (t >= valid) return;
-  // the parts of a unit: its first worker's, then those of the workers that go on with it
+  const SharedSeq q = a.seq[b];
+  // the parts of a unit: its first worker's, by row, then those of the workers that go on with it
   struct Side {
     const float *head, *more;
     int n;
@@ -131,90 +138,97 @@ __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
     }
     return s;
   };
-  const SharedSeq* sp = a.seq + b;
-  const int gi = load_uniform(&sp->group), nb = load_uniform(&sp->nb);
-  const unsigned own_total = load_uniform(&a.total->own), shared_total = load_uniform(&a.total->shared);
   const int units = ((valid << a.log_g) + a.own.unit_rows - 1) / a.own.unit_rows;
-  const Side o = side(a.own, own_total, load_uniform(&sp->block0) + (unsigned)(lh * units + in_seq / a.own.unit_rows) * (unsigned)nb, nb,
+  const Side o = side(a.own, a.total->own, q.block0 + (unsigned)(lh * units + in_seq / a.own.unit_rows) * (unsigned)q.nb, q.nb,
                       in_seq % a.own.unit_rows);
   Side s{nullptr, nullptr, 0};
-  if (gi >= 0) {
-    const SharedGroup* gp = a.group + gi;
-    const int gb = load_uniform(&gp->nb), in_group = (b - load_uniform(&gp->f0)) * per + in_seq;
-    const unsigned u = (unsigned)(lh * load_uniform(&gp->rt) + in_group / a.shared.unit_rows);
-    s = side(a.shared, shared_total, load_uniform(&gp->block0) + u * (unsigned)gb, gb, in_group % a.shared.unit_rows);
+  if (q.group >= 0) {
+    const SharedGroup g = a.group[q.group];
+    const int in_group = q.row0 - g.row0 + in_seq;
+    const unsigned u = (unsigned)(lh * g.rt + in_group / a.shared.unit_rows);
+    s = side(a.shared, a.total->shared, g.block0 + u * (unsigned)g.nb, g.nb, in_group % a.shared.unit_rows);
   }
   const int all = o.n + s.n;
+  const size_t own_step = (size_t)a.own.unit_rows * PS, shared_step = (size_t)a.shared.unit_rows * PS;
   auto at = [&](int n) {
     const bool own = n < o.n;
     const int k = own ? n : n - o.n;
-    const Parts& p = own ? a.own : a.shared;
-    return k == 0 ? (own ? o.head : s.head) : (own ? o.more : s.more) + (size_t)k * p.unit_rows * PS;
+    return k == 0 ? (own ? o.head : s.head) : own ? o.more + k * own_step : s.more + k * shared_step;
   };
-  // a lane to a part: the row's reference and sum
-  float mx = -INFINITY, sum = 0.f;
-  for (int n = lane; n < all; n += kWave) {
-    const float2 ml = *(const float2*)(at(n) + D);
-    const float top = fmaxf(mx, ml.x), ref = top == -INFINITY ? 0.f : top;
-    sum = sum * fast_exp2(mx - ref) + ml.y * fast_exp2(ml.x - ref);
-    mx = top;
-  }
-  float top = mx;
+  float m = -INFINITY, sum = 0.f;  // reference and sum so far
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int n0 = way; n0 < all; n0 += AHEAD * T) {
+    float2 ml[AHEAD];
+    float4 y[AHEAD];
 #pragma unroll
-  for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-  const float ref = top == -INFINITY ? 0.f : top;
-  sum = wave_sum(sum * fast_exp2(mx - ref));
-  // a lane to two channels, all parts; d 64: half of the lanes to every second part
-  constexpr int WAYS = 128 / D, AHEAD = 8;
-  const int way = lane / (D / 2), e = lane % (D / 2) * 2;
-  float x0 = 0.f, x1 = 0.f;
-  for (int c0 = 0; c0 < all; c0 += kWave) {
-    const float f = c0 + lane < all ? fast_exp2(at(c0 + lane)[D] - ref) : 0.f;
-    const int m = min(all - c0, kWave);
-    for (int n0 = 0; n0 < m; n0 += AHEAD * WAYS) {
-      float2 y[AHEAD];
+    for (int k = 0; k < AHEAD; ++k) {
+      const float* p = at(min(n0 + k * T, all - 1));
+      ml[k] = *(const float2*)(p + D);
+      y[k] = *(const float4*)(p + e);
+    }
+    float top = m;
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) y[k] = *(const float2*)(at(c0 + min(n0 + k * WAYS + way, m - 1)) + e);
+    for (int k = 0; k < AHEAD; ++k) top = n0 + k * T < all ? fmaxf(top, ml[k].x) : top;
+    const float ref = top == -INFINITY ? 0.f : top, move = fast_exp2(m - ref);
+    m = top;
+    sum *= move;
+    x = make_float4(x.x * move, x.y * move, x.z * move, x.w * move);
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int n = n0 + k * WAYS + way;
-        const float fn = __shfl(f, min(n, kWave - 1));
-        if (n < m) {
-          x0 = fmaf(y[k].x, fn, x0);
-          x1 = fmaf(y[k].y, fn, x1);
-        }
-      }
+    for (int k = 0; k < AHEAD; ++k) {
+      if (n0 + k * T >= all) continue;
+      const float f = fast_exp2(ml[k].x - ref);
+      sum = fmaf(ml[k].y, f, sum);
+      x = make_float4(fmaf(y[k].x, f, x.x), fmaf(y[k].y, f, x.y), fmaf(y[k].z, f, x.z), fmaf(y[k].w, f, x.w));
     }
   }
-  if constexpr (WAYS == 2) {
-    x0 += __shfl_xor(x0, 32);
-    x1 += __shfl_xor(x1, 32);
+  if constexpr (ALL) {
+    s_x[team][e / 4] = x;
+    if (e == 0) s_ml[team] = make_float2(m, sum);
+    __syncthreads();
+    if (team > 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < TEAMS; ++k) top = fmaxf(top, s_ml[k].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    m = top;
+    sum = 0.f;
+    x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < TEAMS; ++k) {
+      const float f = fast_exp2(s_ml[k].x - ref);
+      const float4 y = s_x[k][e / 4];
+      sum = fmaf(s_ml[k].y, f, sum);
+      x = make_float4(fmaf(y.x, f, x.x), fmaf(y.y, f, x.y), fmaf(y.z, f, x.z), fmaf(y.w, f, x.w));
+    }
   }
-  if (way > 0) return;
   const int h = lh % a.Hkv, l = lh / a.Hkv, hq = (h << a.log_g) + in_seq - (t << a.log_g);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   char* out = a.out.at(l, b, hq, t) + e * DT::kElt;
-  x0 = sum == 0.f ? 0.f : x0 * inv;
-  x1 = sum == 0.f ? 0.f : x1 * inv;
+  x = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
   if constexpr (DT::kElt == 4)
-    *(float2*)out = make_float2(x0, x1);
+    *(float4*)out = x;
   else
-    *(uint32_t*)out = pack2<DT>(x0, x1);
+    *(uint2*)out = make_uint2(pack2<DT>(x.x, x.y), pack2<DT>(x.z, x.w));
   if (e == 0 && a.lse)
-    a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * 0.69314718055994531f;
+    a.lse[(((size_t)l * a.B + b) * a.Hq + hq) * a.n + t] =
+        sum == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __log2f(sum)) * 0.69314718055994531f;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+template <class DT, int D>
+hipError_t launch_join_d(const SharedArgs& a, hipStream_t st) {
+  constexpr int teams = kJoinThreads / (D / 4);
+  const long long rows = (long long)a.L * a.Hkv * a.B * ((long long)a.c.n_new << a.log_g);
+  if (rows < 16 * kNumCU)
+    hipLaunchKernelGGL((k_shared_join<DT, D, true>), dim3((unsigned)rows), dim3(kJoinThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_shared_join<DT, D, false>), dim3((unsigned)((rows + teams - 1) / teams)), dim3(kJoinThreads), 0, st, a);
+  return hipGetLastError();
+}
 template <class DT>
 hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
-  const long long rows = (long long)a.L * a.Hkv * a.B * ((long long)a.c.n_new << a.log_g);
-  const dim3 grid((unsigned)((rows + kJoinThreads / kWave - 1) / (kJoinThreads / kWave)));
-  if (D == 64)
-    hipLaunchKernelGGL((k_shared_join<DT, 64>), grid, dim3(kJoinThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_shared_join<DT, 128>), grid, dim3(kJoinThreads), 0, st, a);
-  return hipGetLastError();
+  return D == 64 ? launch_join_d<DT, 64>(a, st) : launch_join_d<DT, 128>(a, st);
 }
 
 }  // namespace

@@ -22,22 +22,34 @@ __device__ __forceinline__ int last_from(int n, unsigned x, At at) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// A query row of a group: sequence, token and head of it, position.
+// A query row of a group: sequence, token and head of it, position. The rows of a group's sequences lie one after the other.
 struct SharedRow {
   int b, in_seq, pos;
   bool live;
 };
-__device__ __forceinline__ SharedRow shared_row(const SharedArgs& a, int f0, int f1, int row) {
+__device__ __forceinline__ SharedRow shared_row(const SharedArgs& a, const SharedGroup* gp, int row) {
   const PagedCache& c = a.c;
-  const int per = c.n_new << a.log_g;
+  const int f0 = load_uniform(&gp->f0), f1 = load_uniform(&gp->f1);
   SharedRow r;
-  const int k = row / per;
-  r.live = f0 + k < f1;
-  r.b = r.live ? f0 + k : f0;
-  r.in_seq = r.live ? row - k * per : 0;
-  const int valid = c.valid(r.b), t = r.in_seq >> a.log_g;
-  r.live = r.live && t < valid;
-  r.pos = c.len(r.b) - valid + t;
+  r.live = row < load_uniform(&gp->query_rows);
+  r.b = f0;
+  r.in_seq = 0;
+  if (r.live) {
+    if (!c.n_valid) {
+      const int per = c.n_new << a.log_g, k = row / per;
+      r.b += k;
+      r.in_seq = row - k * per;
+    } else {  // the last sequence that begins at or before the row
+      const int at = load_uniform(&gp->row0) + row;
+      int z = f1;
+      while (z - r.b > 1) {
+        const int m = (r.b + z) / 2;
+        (a.seq[m].row0 <= at ? r.b : z) = m;
+      }
+      r.in_seq = at - a.seq[r.b].row0;
+    }
+  }
+  r.pos = c.len(r.b) - c.valid(r.b) + (r.in_seq >> a.log_g);
   return r;
 }
 // Row in_seq of (layer and kv head lh, sequence b) in a head array.
@@ -79,7 +91,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedA
   while (x < last) {
     while (gi + 1 < a.groups && x >= load_uniform(&a.group[gi + 1].block0)) ++gi;
     const SharedGroup* gp = a.group + gi;
-    const int f0 = load_uniform(&gp->f0), f1 = load_uniform(&gp->f1), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
+    const int f0 = load_uniform(&gp->f0), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
     const unsigned in = x - load_uniform(&gp->block0);
     const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
     const int blk_end = min(nb, blk + (int)(last - x));
@@ -89,7 +101,7 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedA
     int lo = kMaxRows, hi = -kMaxRows;  // positions of the unit's rows
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      row[rt] = shared_row(a, f0, f1, r0 + 16 * rt + col);
+      row[rt] = shared_row(a, gp, r0 + 16 * rt + col);
       // a row that is not there sees every key, so that it makes no tile an edge; nobody reads it
       w.pos[rt] = row[rt].live ? row[rt].pos : kMaxRows;
       lo = min(lo, row[rt].live ? row[rt].pos : kMaxRows);

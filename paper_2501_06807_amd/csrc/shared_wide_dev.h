@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
   while (x < last) {
     while (gi + 1 < a.groups && x >= load_uniform(&a.group[gi + 1].block0)) ++gi;
     const SharedGroup* gp = a.group + gi;
-    const int f0 = load_uniform(&gp->f0), f1 = load_uniform(&gp->f1), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
+    const int f0 = load_uniform(&gp->f0), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
     const int base = load_uniform(&gp->base), skip = load_uniform(&gp->skip), at = load_uniform(&gp->at);
     const unsigned in = x - load_uniform(&gp->block0);
     const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     const int lh = u / rts, h = lh % a.Hkv, l = lh / a.Hkv, r0 = u % rts * 128;
     const int i0 = blk * a.shared_block, i1 = min(blk_end * a.shared_block, load_uniform(&gp->tiles));
 
-    const SharedRow row = shared_row(a, f0, f1, r0 + 32 * wave + q32);
+    const SharedRow row = shared_row(a, gp, r0 + 32 * wave + q32);
     // a row that is not there sees every key, so that it makes no tile an edge; nobody reads it
     const int pos = row.live ? row.pos : kMaxRows;
     int lo = row.live ? pos : kMaxRows, hi = row.live ? pos : -kMaxRows;
