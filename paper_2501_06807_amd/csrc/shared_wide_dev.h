@@ -36,21 +36,25 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
   const unsigned per = (total + gridDim.x - 1) / gridDim.x;
   if ((unsigned long long)id * per >= total) return;
   const unsigned first = id * per, last = min(first + per, total);
-  int gi = last_from(a.groups, first, [&](int i) { return a.group[i].block0; });
+  int gi = last_from(a.groups, last - 1, [&](int i) { return a.group[i].block0; });
   // a negative scale is taken into the queries (8-bit codes: it stays with the pages' scales); zero times a masked score would be
   // NaN: the smallest number that is not zero instead
   const float qs = C8 ? a.qscale : fmaxf(fabsf(a.qscale), 0x1p-149f);
   const uint32_t flip = !C8 && a.qscale < 0.f ? 0x80008000u : 0u;
 
-  unsigned x = first;
-  while (x < last) {
-    while (gi + 1 < a.groups && x >= load_uniform(&a.group[gi + 1].block0)) ++gi;
+  // The run is taken from its end on, and a whole unit's blocks from the one on that the time says, so that workgroups with units
+  // of the same keys are at the same keys at a time (their L2 has them once for all): what a run ends with begins at a
+  // unit's first key, what it begins with ends at a unit's last one.
+  unsigned x_end = last;
+  while (x_end > first) {
+    while (gi > 0 && x_end <= load_uniform(&a.group[gi].block0)) --gi;
     const SharedGroup* gp = a.group + gi;
     const int f0 = load_uniform(&gp->f0), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
     const int base = load_uniform(&gp->base), skip = load_uniform(&gp->skip), at = load_uniform(&gp->at);
-    const unsigned in = x - load_uniform(&gp->block0);
-    const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb);
-    const int blk_end = min(nb, blk + (int)(last - x));
+    const unsigned block0 = load_uniform(&gp->block0), in = x_end - 1 - block0;
+    const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk_end = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb) + 1;
+    const unsigned unit0 = block0 + u * (unsigned)nb;  // the unit's first block
+    const int blk = first > unit0 ? (int)(first - unit0) : 0;
     const int lh = u / rts, h = lh % a.Hkv, l = lh / a.Hkv, r0 = u % rts * 128;
     const int i0 = blk * a.shared_block, i1 = min(blk_end * a.shared_block, load_uniform(&gp->tiles));
 
@@ -105,8 +109,14 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     w1 = max(w1, w0);
     const int edges = w0 - i0 + i1 - w1;
     auto key_of = [&](int i) { return (i < skip ? i : i - skip + at) * KT; };
-    const int whole0 = key_of(w0) - edges * KT;  // (whole tiles lie side by side)
-    auto key0 = [&](int j) { return j >= edges ? whole0 + j * KT : key_of(j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0)); };
+    // whole tiles lie side by side; they are taken from number `turn` on
+    const int whole0 = key_of(w0), n_whole = w1 - w0;
+    const int turn = blk == 0 && blk_end == nb ? min((int)((last - x_end) % (unsigned)nb) * a.shared_block, max(n_whole - 1, 0)) : 0;
+    auto whole_key = [&](int j) {
+      const int i = j - edges + turn;
+      return whole0 + (i >= n_whole ? i - n_whole : i) * KT;
+    };
+    auto key0 = [&](int j) { return j >= edges ? whole_key(j) : key_of(j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0)); };
     // Table entries of 64 pages from page `ev0` on, a lane to each: a tile's page ids cost no load.
     int ev = 0, ev0 = -kWave, pid[2];
     auto ids_at = [&](int k0) {
@@ -121,21 +131,25 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     uint4 kr[PER], vr[PER];
     uint32_t kx = 0, vx = 0;                       // 4-bit codes: the piece's scale bytes
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};  // 8-bit codes: the halves' page scales
+    // This (layer, kv head)'s rows of page 0, and bytes from a page to the next; the same of the scales.
+    const size_t page_unit0 = page_unit(c, l, 0, h), page_bytes = (size_t)c.Hkv * c.page * RB;
+    const char *k_page = c.k + page_unit0 * c.page * RB, *v_page = c.v + page_unit0 * c.page * RB;
+    const int lane_row = CODES ? (tid / 8 & 15) * RB + tid % 8 * (RB / 8) : (tid / CH & 15) * RB + tid % CH * 16;
     auto fetch = [&](int k0) {
       ids_at(k0);
-      size_t at_row[2];  // row 0 of a half in the pool (page 0 where it has no page: its rows are not used)
+      size_t at[2];  // a half's first row, in bytes (page 0 where it has no page: its rows are not used)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        at_row[hf] = page_unit(c, l, max(pid[hf], 0), h) * c.page + ((k0 + 16 * hf) & (c.page - 1));
+        const int id = max(pid[hf], 0);
+        at[hf] = id * page_bytes + ((k0 + 16 * hf) & (c.page - 1)) * RB;
         if constexpr (C8) {
-          ks[hf] = load_uniform(c.ks + (at_row[hf] >> c.log_page));
-          vs[hf] = load_uniform(c.vs + (at_row[hf] >> c.log_page));
+          ks[hf] = load_uniform(c.ks + page_unit0 + (size_t)id * c.Hkv);
+          vs[hf] = load_uniform(c.vs + page_unit0 + (size_t)id * c.Hkv);
         }
       }
-      if constexpr (CODES) {
-        const int r = tid / 8, piece = tid % 8;  // (a wave's rows lie in one half)
-        const size_t rr = (wave >= 2 ? at_row[1] : at_row[0]) + (r & 15);
-        const char *kp = c.k + rr * RB + piece * (RB / 8), *vp = c.v + rr * RB + piece * (RB / 8);
+      if constexpr (CODES) {  // (a wave's rows lie in one half)
+        const size_t from = wave >= 2 ? at[1] : at[0];
+        const char *kp = k_page + from + lane_row, *vp = v_page + from + lane_row;
         if constexpr (RB / 8 == 16) {
           kr[0] = ldg16(kp);
           vr[0] = ldg16(vp);
@@ -148,17 +162,18 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
           vr[0] = make_uint4(*(const uint32_t*)vp, 0, 0, 0);
         }
         if constexpr (C4) {
-          const size_t s_at = (rr >> c.log_page) * (size_t)(D / kMx4Block * c.page) + piece * PCH / kMx4Block * c.page + (rr & (c.page - 1));
-          kx = c.kx[s_at];
-          vx = c.vx[s_at];
+          const int id = max(wave >= 2 ? pid[1] : pid[0], 0), slot = (k0 + (wave >= 2 ? 16 : 0)) & (c.page - 1);
+          const size_t s_at = (page_unit0 + (size_t)id * c.Hkv) * (D / kMx4Block * c.page) + slot;
+          const int lane_scale = tid % 8 * PCH / kMx4Block * c.page + (tid / 8 & 15);
+          kx = (c.kx + s_at)[lane_scale];
+          vx = (c.vx + s_at)[lane_scale];
         }
       } else {
 #pragma unroll
-        for (int n = 0; n < PER; ++n) {
-          const int y = tid + n * THREADS, r = y / CH;  // (a half to each n, or to each pair of waves)
-          const size_t rr = ((PER == 2 ? n == 1 : wave >= 2) ? at_row[1] : at_row[0]) + (r & 15);
-          kr[n] = ldg16(c.k + rr * RB + y % CH * 16);
-          vr[n] = ldg16(c.v + rr * RB + y % CH * 16);
+        for (int n = 0; n < PER; ++n) {  // (a half to each n, or to each pair of waves)
+          const size_t from = (PER == 2 ? n == 1 : wave >= 2) ? at[1] : at[0];
+          kr[n] = ldg16(k_page + from + lane_row);
+          vr[n] = ldg16(v_page + from + lane_row);
         }
       }
     };
@@ -329,12 +344,12 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     auto round = [&](auto edge, int n) {
       constexpr bool EDGE = decltype(edge)::value;
       const int j = n * NS + grp, buf = n & 1;
-      const int k0 = EDGE ? key0(j) : whole0 + j * KT;
+      const int k0 = EDGE ? key0(j) : whole_key(j);
       const bool have[2] = {pid[0] >= 0 && k0 < base, pid[1] >= 0 && k0 + 16 < base};
       const float kss[2] = {ks[0], ks[1]}, vss[2] = {vs[0], vs[1]};
       if (j < tiles && stash(edge, buf, have) && EDGE) s_bad[grp][buf] = n;
       __syncthreads();
-      if (j + NS < tiles) fetch(EDGE ? key0(j + NS) : k0 + NS * KT);
+      if (j + NS < tiles) fetch(EDGE ? key0(j + NS) : whole_key(j + NS));
       if (j < tiles && lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
     };
     for (int n = 0; n < edge_rounds; ++n) round(std::true_type{}, n);
@@ -388,7 +403,7 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
       if (hl == 0) *(float2*)(part + D) = make_float2(ref - LIFT, sum);
     }
     __syncthreads();  // the LDS buffers are free again
-    x += blk_end - blk;
+    x_end = unit0 + blk;
   }
 }
 
