@@ -110,41 +110,56 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     const int edges = w0 - i0 + i1 - w1;
     auto key_of = [&](int i) { return (i < skip ? i : i - skip + at) * KT; };
     // whole tiles lie side by side; they are taken from number `turn` on
-    const int whole0 = key_of(w0), n_whole = w1 - w0;
+    const int whole0 = key_of(w0), n_whole = w1 - w0, whole_end = whole0 + n_whole * KT;
     const int turn = blk == 0 && blk_end == nb ? min((int)((last - x_end) % (unsigned)nb) * a.shared_block, max(n_whole - 1, 0)) : 0;
     auto whole_key = [&](int j) {
       const int i = j - edges + turn;
       return whole0 + (i >= n_whole ? i - n_whole : i) * KT;
     };
     auto key0 = [&](int j) { return j >= edges ? whole_key(j) : key_of(j < w0 - i0 ? i0 + j : w1 + j - (w0 - i0)); };
-    // Table entries of 64 pages from page `ev0` on, a lane to each: a tile's page ids cost no load.
-    int ev = 0, ev0 = -kWave, pid[2];
-    auto ids_at = [&](int k0) {
-      const int pa = k0 >> c.log_page, pb = (k0 + 16) >> c.log_page;
-      if (pa < ev0 || pb >= ev0 + kWave) {
-        ev0 = pa;
-        ev = c.table[(size_t)f0 * c.max_pages + min(pa + lane, c.max_pages - 1)];
+    // This (layer, kv head)'s rows of page 0, and bytes from a page to the next.
+    const size_t page0 = page_unit(c, l, 0, h), page_bytes = (size_t)c.Hkv * c.page * RB;
+    const char *k_page = c.k + page0 * c.page * RB, *v_page = c.v + page0 * c.page * RB;
+    // A window of 64 halves (16 keys) from number `win` on, a lane to each: where its first row lies behind page 0's (that one where
+    // there is no page: its rows are not used), whether there is one, and (8-bit codes) its page's scales.
+    int win = -kWave;
+    uint32_t w_lo = 0, w_hi = 0;
+    unsigned long long w_has = 0;
+    float w_ks = 0.f, w_vs = 0.f;
+    auto load_window = [&](int half) {
+      win = half;
+      const int i = half + lane, pg = (16 * i) >> c.log_page;
+      const int entry = c.table[(size_t)f0 * c.max_pages + min(pg, c.max_pages - 1)], id = page_of_entry(c, entry, pg);
+      const size_t at = max(id, 0) * page_bytes + (size_t)((16 * i) & (c.page - 1)) * RB;
+      w_lo = (uint32_t)at;
+      w_hi = (uint32_t)(at >> 32);
+      w_has = __ballot(id >= 0 && 16 * i < base);
+      if constexpr (C8) {
+        w_ks = c.ks[page0 + (size_t)max(id, 0) * c.Hkv];
+        w_vs = c.vs[page0 + (size_t)max(id, 0) * c.Hkv];
       }
-      pid[0] = page_of_entry(c, __builtin_amdgcn_readlane(ev, pa - ev0), pa);
-      pid[1] = page_of_entry(c, __builtin_amdgcn_readlane(ev, pb - ev0), pb);
     };
     uint4 kr[PER], vr[PER];
     uint32_t kx = 0, vx = 0;                       // 4-bit codes: the piece's scale bytes
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};  // 8-bit codes: the halves' page scales
-    // This (layer, kv head)'s rows of page 0, and bytes from a page to the next; the same of the scales.
-    const size_t page_unit0 = page_unit(c, l, 0, h), page_bytes = (size_t)c.Hkv * c.page * RB;
-    const char *k_page = c.k + page_unit0 * c.page * RB, *v_page = c.v + page_unit0 * c.page * RB;
     const int lane_row = CODES ? (tid / 8 & 15) * RB + tid % 8 * (RB / 8) : (tid / CH & 15) * RB + tid % CH * 16;
+    int k_at = 0;         // the fetched tile's first key
+    unsigned has_at = 0;  // and whether its halves have a page
     auto fetch = [&](int k0) {
-      ids_at(k0);
-      size_t at[2];  // a half's first row, in bytes (page 0 where it has no page: its rows are not used)
+      int i = (k0 >> 4) - win;
+      if ((unsigned)i >= kWave - 1) {
+        load_window(k0 >> 4);
+        i = 0;
+      }
+      k_at = k0;
+      has_at = (unsigned)(w_has >> i) & 3u;
+      size_t at[2];
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const int id = max(pid[hf], 0);
-        at[hf] = id * page_bytes + ((k0 + 16 * hf) & (c.page - 1)) * RB;
+        at[hf] = (uint32_t)__builtin_amdgcn_readlane(w_lo, i + hf) | (size_t)(uint32_t)__builtin_amdgcn_readlane(w_hi, i + hf) << 32;
         if constexpr (C8) {
-          ks[hf] = load_uniform(c.ks + page_unit0 + (size_t)id * c.Hkv);
-          vs[hf] = load_uniform(c.vs + page_unit0 + (size_t)id * c.Hkv);
+          ks[hf] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w_ks), i + hf));
+          vs[hf] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w_vs), i + hf));
         }
       }
       if constexpr (CODES) {  // (a wave's rows lie in one half)
@@ -162,8 +177,9 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
           vr[0] = make_uint4(*(const uint32_t*)vp, 0, 0, 0);
         }
         if constexpr (C4) {
-          const int id = max(wave >= 2 ? pid[1] : pid[0], 0), slot = (k0 + (wave >= 2 ? 16 : 0)) & (c.page - 1);
-          const size_t s_at = (page_unit0 + (size_t)id * c.Hkv) * (D / kMx4Block * c.page) + slot;
+          constexpr int SB = D / kMx4Block;
+          const int slot = (k0 + (wave >= 2 ? 16 : 0)) & (c.page - 1);
+          const size_t s_at = page0 * SB * c.page + from / RB * SB - slot * (SB - 1);
           const int lane_scale = tid % 8 * PCH / kMx4Block * c.page + (tid / 8 & 15);
           kx = (c.kx + s_at)[lane_scale];
           vx = (c.vx + s_at)[lane_scale];
@@ -344,12 +360,19 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     auto round = [&](auto edge, int n) {
       constexpr bool EDGE = decltype(edge)::value;
       const int j = n * NS + grp, buf = n & 1;
-      const int k0 = EDGE ? key0(j) : whole_key(j);
-      const bool have[2] = {pid[0] >= 0 && k0 < base, pid[1] >= 0 && k0 + 16 < base};
+      const int k0 = k_at;
+      const bool have[2] = {(has_at & 1) != 0, (has_at & 2) != 0};
       const float kss[2] = {ks[0], ks[1]}, vss[2] = {vs[0], vs[1]};
       if (j < tiles && stash(edge, buf, have) && EDGE) s_bad[grp][buf] = n;
       __syncthreads();
-      if (j + NS < tiles) fetch(EDGE ? key0(j + NS) : whole_key(j + NS));
+      if (j + NS < tiles) {
+        int next = k0 + NS * KT;
+        if (EDGE)
+          next = key0(j + NS);
+        else if (next >= whole_end)
+          next -= n_whole * KT;
+        fetch(next);
+      }
       if (j < tiles && lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
     };
     for (int n = 0; n < edge_rounds; ++n) round(std::true_type{}, n);
