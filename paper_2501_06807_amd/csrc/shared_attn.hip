@@ -7,9 +7,10 @@ namespace mpc {
 namespace {
 
 using namespace dev;
-constexpr int kPlanThreads = 1024, kJoinThreads = 256;
+constexpr int kJoinThreads = 256;
 
 // Sum of x over the threads before this one, and over all of them.
+template <int THREADS>
 __device__ __forceinline__ unsigned sum_before(unsigned x, unsigned* s_wave, unsigned* total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   unsigned sum = x;
@@ -18,10 +19,14 @@ __device__ __forceinline__ unsigned sum_before(unsigned x, unsigned* s_wave, uns
     const unsigned y = __shfl_up(sum, o);
     if (lane >= o) sum += y;
   }
+  if constexpr (THREADS == kWave) {
+    *total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    return sum - x;
+  }
   if (lane == kWave - 1) s_wave[wave] = sum;
   __syncthreads();
   unsigned before = 0, all = 0;
-  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+  for (int w = 0; w < THREADS / kWave; ++w) {
     before += w < wave ? s_wave[w] : 0;
     all += s_wave[w];
   }
@@ -30,12 +35,12 @@ __device__ __forceinline__ unsigned sum_before(unsigned x, unsigned* s_wave, uns
   return before + sum - x;
 }
 
-// One workgroup: a thread to a group, and the sequences over the threads. Bounds of the groups are brought into [0, B] and in
+// One workgroup (a wave where that has the groups and sequences): a thread to a group, and the sequences over the threads. Bounds of the groups are brought into [0, B] and in
 // order, so that every sequence is in one group at most, whatever `first` holds.
-template <bool C8>
-__global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
-  __shared__ int s_f[kMaxGroups + 1], s_base[kMaxGroups], s_lo[kMaxGroups], s_hi[kMaxGroups];
-  __shared__ unsigned s_wave[kPlanThreads / kWave];
+template <bool C8, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_shared_plan(SharedArgs a) {
+  __shared__ int s_f[THREADS + 1], s_base[THREADS], s_lo[THREADS], s_hi[THREADS];
+  __shared__ unsigned s_wave[THREADS / kWave];
   const PagedCache& c = a.c;
   const int tid = threadIdx.x, ng = a.groups;
   s_f[tid] = tid < ng ? min(max(a.first[tid], 0), a.B) : 0;
@@ -54,7 +59,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
   }
   __syncthreads();
   unsigned own = 0, rows = 0;  // blocks and query rows of the sequences so far
-  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < a.B; b0 += THREADS) {
     const int b = b0 + tid;
     SharedSeq q{0, 0, -1, 0, 0};
     unsigned blocks = 0, mine = 0;
@@ -78,9 +83,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
       mine = (unsigned)s.valid << a.log_g;
     }
     unsigned all;
-    q.block0 = own + sum_before(blocks, s_wave, &all);
+    q.block0 = own + sum_before<THREADS>(blocks, s_wave, &all);
     own += all;
-    q.row0 = (int)(rows + sum_before(mine, s_wave, &all));
+    q.row0 = (int)(rows + sum_before<THREADS>(mine, s_wave, &all));
     rows += all;
     if (b < a.B) a.seq[b] = q;
   }
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a) {
     p.nb = (p.tiles + a.shared_block - 1) / a.shared_block;
   }
   unsigned total;
-  p.block0 = sum_before((unsigned)(p.rt * a.L * a.Hkv) * (unsigned)p.nb, s_wave, &total);
+  p.block0 = sum_before<THREADS>((unsigned)(p.rt * a.L * a.Hkv) * (unsigned)p.nb, s_wave, &total);
   if (tid < ng) a.group[tid] = p;
   if (tid == 0) *a.total = SharedTotals{total, own};
 }
@@ -243,7 +248,7 @@ SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, i
   p.own_rows = each_seq <= 16 ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
   p.shared_block = p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16);
-  p.own_block = 128 / p.tile;
+  p.own_block = 64 / p.tile;
   p.shared_workers = p.wide ? kNumCU * 2 / kWideGroups : kNumCU;
   p.own_workers = kNumCU * kOwnWaves * (p.own_rows == 16 ? 2 : 1);
   auto blocks = [&](long long units, long long block) {
@@ -265,10 +270,15 @@ SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, i
 }
 
 hipError_t launch_shared_attn(const SharedArgs& a, int dtype, int D, hipStream_t st) {
-  if (a.c.format == MPC_PAGE_E4M3)
-    hipLaunchKernelGGL(k_shared_plan<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
+  const bool small = a.B <= kWave, codes8 = a.c.format == MPC_PAGE_E4M3;
+  if (small && codes8)
+    hipLaunchKernelGGL((k_shared_plan<true, kWave>), dim3(1), dim3(kWave), 0, st, a);
+  else if (small)
+    hipLaunchKernelGGL((k_shared_plan<false, kWave>), dim3(1), dim3(kWave), 0, st, a);
+  else if (codes8)
+    hipLaunchKernelGGL((k_shared_plan<true, kMaxGroups>), dim3(1), dim3(kMaxGroups), 0, st, a);
   else
-    hipLaunchKernelGGL(k_shared_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
+    hipLaunchKernelGGL((k_shared_plan<false, kMaxGroups>), dim3(1), dim3(kMaxGroups), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   e = a.c.format == MPC_PAGE_MX4 ? launch_shared_mx4(a, dtype, D, st)
