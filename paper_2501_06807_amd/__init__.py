@@ -6,7 +6,7 @@ mpc_sparse_decode_attn, mpc_decode_step (selection and attention in one launch) 
 mpc_decode_step_status (its workspace's error word), mpc_append_kv (decode-time growth of the kept
 cache) and mpc_commonality (agreement of adjacent layers' top-k sets). ``MPCachePath`` strings them together for one prefill and repeated
 decode steps, with all buffers preallocated. Beside them, for serving from a paged cache (``PagedKV``): mpc_paged_append,
-mpc_paged_attn and mpc_prompt_attn, which ``PagedPath`` strings together.
+mpc_paged_read, mpc_paged_attn, mpc_shared_attn and mpc_prompt_attn, which ``PagedPath`` strings together.
 """
 from ._lib import (  # noqa: F401
     GROUP, MPC_OP_DECODE_ATTN, MPC_OP_DECODE_STEP, MPC_OP_PAGED_ATTN, MPC_OP_SELECT, MPC_OP_SHARED_ATTN, MPC_OP_STATIC_EVICT, MpcDims, MpcError,

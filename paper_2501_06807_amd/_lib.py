@@ -451,7 +451,7 @@ def _call(name, fn, device, *args):
 
 
 class PagedKV:
-    """A paged cache over the caller's tensors, as mpc_paged_append and mpc_paged_attn take it.
+    """A paged cache over the caller's tensors, as the mpc_paged_* calls and mpc_shared_attn take it.
 
     k_pages, v_pages [L][P][Hkv][page][d] of the element type, or torch.float8_e4m3fn codes with k_scale, v_scale
     [L][P][Hkv] float32 and the rings k_tail, v_tail [L][B][Hkv][2 page][d] of the element type, or torch.uint8 [L][P][Hkv]

@@ -156,18 +156,21 @@ class MPCachePath:
 
 
 class PagedPath:
-    """Serving from a paged cache over mpc_paged_append, mpc_paged_attn and mpc_prompt_attn: a batch of `batch` sequences of
-    up to `max_rows` rows each, all layers of the block per call, the pages drawn from one pool as the sequences grow.
+    """Serving from a paged cache over mpc_paged_append, mpc_paged_attn, mpc_shared_attn, mpc_paged_read and mpc_prompt_attn: a
+    batch of `batch` sequences of up to `max_rows` rows each, all layers of the block per call, the pages drawn from one pool as
+    the sequences grow.
 
     prefill() starts every sequence with a prompt, extend() adds tokens to them (one each, drafted ones, or a chunk of a
-    prompt) and attends over the cache, take_back() drops the newest rows again (rejected drafts), and adopt() starts the
+    prompt) and attends over the cache, take_back() drops the newest rows again (rejected drafts), fork() lets sequences go on
+    from the rows of another, whose whole pages they share, held() gives rows of the cache back, and adopt() starts the
     sequences with the rows that a MPCachePath kept. A call that is refused has changed nothing. All calls of a path, and the
-    replays of its captured steps, share its cache and workspace, so they run in one stream's order. fp8: pages of e4m3 codes
-    with a scale for each page and head. window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
+    replays of its captured steps, share its cache and workspaces, so they run in one stream's order. fmt: the pages' format,
+    "same", "e4m3" (codes with a scale for each page and head) or "mx4" (4-bit codes with a scale for each 32 channels of a
+    row); by default what fp8 says, "e4m3" or "same". window, sinks: what a row sees of the rows before it (0: all of them). rope: a table [n_pos][rot_dim / 2][2] of
     (cos, sin); None where q and k arrive rotated."""
 
     def __init__(self, *, n_layers, batch, n_q_heads, n_kv_heads, head_dim, dtype, max_rows, page_size=64, n_pages=None,
-                 fp8=True, window=0, sinks=0, rope=None, rope_style="interleaved", sm_scale=None, device="cuda"):
+                 fp8=True, fmt=None, window=0, sinks=0, rope=None, rope_style="interleaved", sm_scale=None, device="cuda"):
         self.Hq, self.window, self.sinks, self.rope, self.rope_style = n_q_heads, window, sinks, rope, rope_style
         self.sm_scale = 1.0 / math.sqrt(head_dim) if sm_scale is None else sm_scale
         if not 0 <= window < 2 ** 31 or not 0 <= sinks < 2 ** 31 or not math.isfinite(self.sm_scale):
@@ -177,7 +180,8 @@ class PagedPath:
         max_pages = -(-max_rows // page_size)
         n_pages = batch * max_pages if n_pages is None else n_pages
         self.kv = L.paged_kv(n_layers=n_layers, batch=batch, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype,
-                             n_pages=n_pages, max_pages=max_pages, page_size=page_size, fp8=fp8, device=device)
+                             n_pages=n_pages, max_pages=max_pages, page_size=page_size, device=device,
+                             fmt=("e4m3" if fp8 else "same") if fmt is None else fmt)
         if rope is not None:
             p, n_pos, rot = L._rope_of(rope)
             if rope.device != self.kv.device or p % 16 or n_pos == 0 or rot == 0 or rot % 16 or rot > head_dim:
@@ -186,6 +190,10 @@ class PagedPath:
         self.rows = [0] * batch  # the lengths again, on the host
         self._kept = [0] * batch  # first row of each sequence that its tail still holds
         self._pages = [[] for _ in range(batch)]
+        self._lent = [0] * batch  # pages at the front of each that belong to another sequence
+        self._floor = [0] * batch  # rows that other sequences share, or that are shared with them
+        self._groups = None  # (first, shared_rows, most new tokens of a step, workspace) for mpc_shared_attn
+        self._retired = []  # those of earlier forks, which captured steps may still read: they say that nothing is shared
         self._free = list(range(n_pages - 1, -1, -1))
         # for steps of any number of tokens (the bytes do not grow beyond 32 query rows to a kv head), and cleared here, so
         # that a step may be captured before one has run
@@ -232,15 +240,18 @@ class PagedPath:
 
     def _start(self, rows):
         """Empties every sequence and books rows[b] rows for each, if the whole pool has pages for them."""
-        self._lacking(rows, [0] * self.kv.B, len(self._free) + sum(len(p) for p in self._pages))
+        self._lacking(rows, [0] * self.kv.B, len(self._free) + sum(len(p) - n for p, n in zip(self._pages, self._lent)))
         self.clear()
         self.grown(rows)
 
     def clear(self):
         """Empties every sequence; the pages go back to the pool."""
         for b, pages in enumerate(self._pages):
-            self._free += pages[::-1]
+            self._free += pages[self._lent[b]:][::-1]
             self._pages[b] = []
+        self._lent = [0] * self.kv.B
+        self._floor = [0] * self.kv.B
+        self._share(None)
         self.rows = [0] * self.kv.B
         self._kept = [0] * self.kv.B
         self.kv.table.fill_(-1)
@@ -270,8 +281,11 @@ class PagedPath:
                            pos0=self.pos, n_valid=n_valid)
         self.pos.add_(n if n_valid is None else n_valid)
         out = torch.zeros_like(q) if out is None else out
-        L.mpc_paged_attn(q, self.kv, out, sm_scale=self.sm_scale, window=self.window, sinks=self.sinks, n_valid=n_valid,
-                         lse=lse, ws=self.ws)
+        kw = dict(sm_scale=self.sm_scale, window=self.window, sinks=self.sinks, n_valid=n_valid, lse=lse)
+        if self._groups is not None and n <= self._groups[2]:
+            L.mpc_shared_attn(q, self.kv, out, first=self._groups[0], shared_rows=self._groups[1], ws=self._groups[3], **kw)
+        else:
+            L.mpc_paged_attn(q, self.kv, out, ws=self.ws, **kw)
         return out
 
     def extend(self, q, k, v, new=None, out=None, lse=None):
@@ -292,14 +306,17 @@ class PagedPath:
         self._kept = [max(k, ((r - 1) // page - 1) * page) for k, r in zip(self._kept, rows)]
 
     def take_back(self, dropped):
-        """Drops the newest dropped[b] rows of each sequence; the pages stay reserved. With 8-bit pages the page that a
+        """Drops the newest dropped[b] rows of each sequence; the pages stay reserved, and rows that sequences share stay. With
+        8-bit pages the page that a
         sequence then ends in has to be in its tail still, which holds the last two pages that it ever reached: a page's
         rows at least."""
         dropped = self._counts(dropped, "dropped")
         page, rows = self.kv.page, [r - d for r, d in zip(self.rows, dropped)]
         for r, d, kept in zip(rows, dropped, self._kept):
-            if r < 0 or (d and self.kv.k_scale is not None and r % page and r // page * page < kept):
+            if r < 0 or (d and self.kv.k_tail is not None and r % page and r // page * page < kept):
                 raise ValueError("more rows than the sequence has, or than its tail keeps")
+        if any(d and r < f for r, d, f in zip(rows, dropped, self._floor)):
+            raise ValueError("rows that sequences share cannot be dropped")
         d = self._ints(dropped)
         self.rows = rows
         # where a page begins nothing of the tail is needed, and what follows is written into it again
@@ -327,6 +344,72 @@ class PagedPath:
         L.mpc_prompt_attn(q, k if turned is None else turned, v, out, sm_scale=self.sm_scale, window=self.window,
                           sinks=self.sinks, q_lens=n, k_lens=n, lse=lse)
         return out
+
+    def _share(self, groups):
+        """Makes `groups` what steps share; what was shared before says from now on that nothing is."""
+        if self._groups is not None:
+            self._groups[1].zero_()
+            self._retired.append(self._groups)
+        self._groups = groups
+
+    def fork(self, first, n_new=1):
+        """Groups of neighbours, sequences first[g] <= b < first[g + 1]: each of them goes on from the rows of its group's first one,
+        whose whole pages they share from then on (the rows behind these are copied); the others of a group have to be empty. Steps
+        of up to n_new tokens read the shared rows once for a group (mpc_shared_attn), longer ones once for each sequence."""
+        kv, page = self.kv, self.kv.page
+        first, n_new = [operator.index(b) for b in first], operator.index(n_new)
+        if not 2 <= len(first) <= 1025 or first[0] < 0 or first[-1] > kv.B or any(x >= y for x, y in zip(first, first[1:])) or n_new < 1:
+            raise ValueError(f"first: numbers from 0 to {kv.B}, each larger than the one before it, and n_new from 1 on are wanted")
+        if self._groups is not None:
+            raise ValueError("the sequences share rows already: clear() first")
+        others = [(a, b) for a, z in zip(first, first[1:]) for b in range(a + 1, z)]
+        if any(self.rows[b] or self._pages[b] for _, b in others):
+            raise ValueError("a sequence that goes on from another's rows has to be empty")
+        n_copies = sum(1 for a, _ in others if self.rows[a] % page)
+        if n_copies > len(self._free):
+            raise ValueError(f"{n_copies} pages wanted, {len(self._free)} free")
+        shape = torch.empty(kv.L, kv.B, self.Hq, n_new, kv.d, device="meta")
+        size = L.shared_attn_workspace_bytes(shape, kv, len(first) - 1)
+        if size == 0:
+            raise ValueError(f"sizes that the library does not take ({L.lib().mpc_last_error().decode()})")
+        shared = [self.rows[a] // page * page for a in first[:-1]]
+        groups = (self._ints(first), self._ints(shared), n_new, L.workspace(size, kv.device))
+        src, dst = [], []
+        for a, b in others:
+            whole = self.rows[a] // page
+            self._pages[b] = self._pages[a][:whole]
+            self._lent[b] = whole
+            if self.rows[a] % page:
+                src.append(self._pages[a][whole])
+                dst.append(self._free.pop())
+                self._pages[b].append(dst[-1])
+            self.rows[b], self._kept[b], self._floor[b], self._floor[a] = self.rows[a], self._kept[a], whole * page, whole * page
+        if others:
+            a, b = (torch.tensor(x, device=kv.device) for x in zip(*others))
+            for t in (kv.lens, self.pos):
+                t[b] = t[a]
+            for t in (kv.k_tail, kv.v_tail):
+                if t is not None:
+                    t[:, b] = t[:, a]
+            if src and kv.k_tail is None:  # (with 8-bit pages the rows behind the whole pages are in the tail)
+                s, d = (torch.tensor(x, device=kv.device) for x in (src, dst))
+                for t in (kv.k_pages, kv.v_pages, kv.k_scale, kv.v_scale):
+                    if t is not None:
+                        t[:, d] = t[:, s]
+            M = kv.table.shape[1]
+            kv.table.copy_(self._ints([p + [-1] * (M - len(p)) for p in self._pages]))
+        self._share(groups)
+
+    def held(self, n, first=None):
+        """(k, v), each [L][B][Hkv][n][d] in the element type: rows first[b] .. first[b] + n - 1 of each sequence as the cache has them
+        (the newest n by default), zeros for rows that it does not have."""
+        kv, n = self.kv, operator.index(n)
+        if n < 1:
+            raise ValueError("no rows")
+        first = None if first is None else self._ints(self._counts(first, "first", 2 ** 31 - 1))
+        k, v = (torch.zeros(kv.L, kv.B, kv.Hkv, n, kv.d, dtype=kv.dtype, device=kv.device) for _ in range(2))
+        L.mpc_paged_read(kv, k, v, first=first)
+        return k, v
 
     def adopt(self, path, position):
         """Starts every sequence with the rows that `path` (a MPCachePath of the same shape) keeps, as they are: its evicted
