@@ -72,7 +72,7 @@ __device__ __forceinline__ void write_part(const PagedWave<DT, D, FMT, RT>& w, i
 }
 
 template <class DT, int D, int FMT, int RT>
-__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedArgs a) {
+__device__ __forceinline__ void shared_rows(const SharedArgs& a) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr int NT = TL::NT, RW = 16 * RT, NW = paged_waves(RT);
   const PagedCache& c = a.c;
@@ -170,15 +170,15 @@ __device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int len, int va
   return s;
 }
 
-// A wave to a run of blocks: nothing of it waits for another wave.
-template <class DT, int D, int FMT, int RT>
-__global__ __launch_bounds__(kOwnWaves * kWave, RT == 1 ? 2 : 1) void k_own_rows(SharedArgs a) {
+// A wave to a run of blocks: nothing of it waits for another wave. Workgroups of WAVES waves.
+template <class DT, int D, int FMT, int RT, int WAVES>
+__device__ __forceinline__ void own_rows_of(const SharedArgs& a) {
   using TL = PagedTile<DT, D, FMT, RT>;
   constexpr int RW = 16 * RT;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x % kWave, col = lane % 16;
-  const unsigned id = by_die(blockIdx.x, gridDim.x) * kOwnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const unsigned total = load_uniform(&a.total->own), workers = gridDim.x * kOwnWaves;
+  const unsigned id = by_die(blockIdx.x, gridDim.x) * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned total = load_uniform(&a.total->own), workers = gridDim.x * WAVES;
   const unsigned per = (total + workers - 1) / workers;
   if ((unsigned long long)id * per >= total) return;
   const unsigned first = id * per, last = min(first + per, total);
@@ -222,22 +222,21 @@ __global__ __launch_bounds__(kOwnWaves * kWave, RT == 1 ? 2 : 1) void k_own_rows
   }
 }
 
+// Shared rows, then own ones: a workgroup that is done with its run of the shared rows goes on with own rows.
+template <class DT, int D, int FMT, int RT, int OWN_RT>
+__global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedArgs a) {
+  shared_rows<DT, D, FMT, RT>(a);
+  own_rows_of<DT, D, FMT, OWN_RT, paged_waves(RT)>(a);
+}
 template <class DT, int D, int FMT>
 hipError_t launch_narrow(const SharedArgs& a, hipStream_t st) {
-  if (a.shared.unit_rows == 16)
-    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1>), dim3((unsigned)a.shared.workers), dim3(paged_waves(1) * kWave), 0, st, a);
+  const dim3 grid((unsigned)a.shared.workers);
+  if (a.shared.unit_rows == 16)  // (then a sequence's rows fit 16 too)
+    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1, 1>), grid, dim3(paged_waves(1) * kWave), 0, st, a);
+  else if (a.own.unit_rows == 16)
+    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2, 1>), grid, dim3(paged_waves(2) * kWave), 0, st, a);
   else
-    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2>), dim3((unsigned)a.shared.workers), dim3(paged_waves(2) * kWave), 0, st, a);
-  return hipGetLastError();
-}
-
-template <class DT, int D, int FMT>
-hipError_t launch_own(const SharedArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.own.workers / kOwnWaves)), block(kOwnWaves * kWave);
-  if (a.own.unit_rows == 16)
-    hipLaunchKernelGGL((k_own_rows<DT, D, FMT, 1>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_own_rows<DT, D, FMT, 2>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2, 2>), grid, dim3(paged_waves(2) * kWave), 0, st, a);
   return hipGetLastError();
 }
 

@@ -13,7 +13,7 @@ namespace mpc {
 namespace dev {
 
 template <class DT, int D, int FMT, int NS>
-__global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
+__device__ __forceinline__ void shared_wide(const SharedArgs& a) {
   constexpr bool C8 = FMT == MPC_PAGE_E4M3, C4 = FMT == MPC_PAGE_MX4, CODES = C8 || C4;
   constexpr bool H = DT::kCode == MPC_FP16, SPLIT = C4 && H, TWO = CODES && H;
   using QT = std::conditional_t<C4, BF16, DT>;    // type of the scores' product
@@ -428,6 +428,17 @@ __global__ __launch_bounds__(256 * NS, 2) void k_shared_wide(SharedArgs a) {
     __syncthreads();  // the LDS buffers are free again
     x_end = unit0 + blk;
   }
+}
+
+// With the own rows where their units have 16 query rows (OWN); units of 32 take more registers than are left here.
+template <class DT, int D, int FMT, bool OWN>
+__global__ __launch_bounds__(256 * kWideGroups, 2) void k_shared_wide(SharedArgs a) {
+  shared_wide<DT, D, FMT, kWideGroups>(a);
+  if constexpr (OWN) own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a);
+}
+template <class DT, int D, int FMT>
+__global__ __launch_bounds__(kOwnWaves * kWave) void k_own_rows(SharedArgs a) {
+  own_rows_of<DT, D, FMT, 2, kOwnWaves>(a);
 }
 
 }  // namespace dev
