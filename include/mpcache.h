@@ -444,7 +444,7 @@ typedef struct {
  * roundings of another order of summation.
  * ws: mpc_workspace_bytes(MPC_OP_SHARED_ATTN, dims, n_new, &sizes) bytes, zero-filled before its first use; every completed
  * call leaves it ready for the next, of this or any other sizes whose bytes it has, and for mpc_paged_attn (calls sharing
- * it must not overlap). The sizes, not the lengths or the groups' contents, give the launches, so a captured call follows
+ * it must not overlap). The bytes never fall with n_new, batch, n_layers, the heads or n_groups. The sizes, not the lengths or the groups' contents, give the launches, so a captured call follows
  * lengths, tables and groups as they change.
  * Limits: those of mpc_paged_attn, B * n_new * G <= 2^30. */
 mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,

@@ -339,58 +339,59 @@ __device__ __forceinline__ uint32_t block_max(const uint4& x) {
   return __float_as_uint(DT::kCode == MPC_BF16 ? bf16_to_f32(m) : f16_to_f32(m));
 }
 
-// Rows of K and V into pages of 4-bit codes: a row's blocks of 32 channels have a scale each, so a row is final as it is
-// written. Work is laid out as in move_rows; a row's lanes (of one wave) exchange the maxima of their vectors through LDS,
-// since the partners of a rotated pair may lie in different blocks.
+// Rows of K or V into pages of 4-bit codes: a row's blocks of 32 channels have a scale each, so a row is final as it is
+// written. Work is laid out as in move_rows, K and V apart; a row's lanes (of one wave) exchange the maxima of their vectors
+// through LDS, since the partners of a rotated pair may lie in different blocks.
 template <class DT, int D, int HPT>
 __device__ __forceinline__ void move_rows4(const PagedAppendArgs& a, const Moves& m, unsigned block) {
   constexpr int NI = D / DT::kVec / 2, V = DT::kVec, NB = kMx4Block / V;  // vectors of a block
   __shared__ __align__(16) uint32_t s_max[kThreads / NI][2 * NI];
   const PagedCache& c = a.c;
-  const int heads = 2 * c.Hkv;
-  const int chunk = block % (unsigned)m.chunks, run = block / (unsigned)m.chunks % (unsigned)m.runs;
-  const int lb = block / (unsigned)m.chunks / (unsigned)m.runs, b = lb % c.B, l = lb / c.B;
+  const int chunk = block % (unsigned)m.chunks, rest = block / (unsigned)m.chunks;
+  const bool is_v = rest & 1;
+  const int run = (unsigned)rest / 2 % (unsigned)m.runs, lb = (unsigned)rest / 2 / (unsigned)m.runs, b = lb % c.B, l = lb / c.B;
   const int tr = threadIdx.x / NI, t = run * m.tokens + (tr & (m.tokens - 1)), lane = tr / m.tokens;
   const int valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
-  if (t >= valid) return;
+  const int h0 = chunk * HPT * m.lanes + lane;
+  if (t >= valid || h0 >= c.Hkv) return;
   const int j = min(max(load_uniform(c.lens + b), 0), kMaxRows) - valid + t;
   const int pos = a.pos0 ? load_uniform(a.pos0 + b) + t : j;
   const Item it = item_of<DT>(threadIdx.x % NI, a.rope.rot);
-  const int h0 = chunk * HPT * m.lanes + lane;
-  const bool turned = a.rope.table && it.turn && h0 < c.Hkv;
+  const bool turned = a.rope.table && it.turn && !is_v;
+  const Rows& in = is_v ? a.v : a.k;
+  const char* src = in.at(l, b, h0, t);
+  const int64_t src_step = m.lanes * in.head;
   uint4 x[HPT], y[HPT];
 #pragma unroll
   for (int k = 0; k < HPT; ++k) {
-    const int hh = h0 + k * m.lanes;
-    if (hh >= heads) continue;
-    const char* src = hh < c.Hkv ? a.k.at(l, b, hh, t) : a.v.at(l, b, hh - c.Hkv, t);
-    x[k] = ldg16(src + it.va * 16);
-    y[k] = ldg16(src + it.vb * 16);
+    if (h0 + k * m.lanes >= c.Hkv) continue;
+    x[k] = ldg16(src + k * src_step + it.va * 16);
+    y[k] = ldg16(src + k * src_step + it.vb * 16);
   }
   Angles<DT> g;
   if (turned) g = angles_of<DT>(a.rope, it, pos);
   const int id = j >= 0 ? page_id_lane(c, b, j >> c.log_page) : -1;
+  const bool plain = a.k_out.p && !is_v && j >= 0 && j < c.cap();
+  const size_t unit = page_unit(c, l, max(id, 0), h0);
+  const int slot = j & (c.page - 1);
+  char* row = (is_v ? c.v : c.k) + (unit * c.page + slot) * (size_t)(D / 2);
+  uint8_t* scale = (is_v ? c.vx : c.kx) + unit * (size_t)(D / kMx4Block * c.page) + slot;
 #pragma unroll
   for (int k = 0; k < HPT; ++k) {
-    const int hh = h0 + k * m.lanes;
-    if (hh >= heads) continue;
-    const bool is_v = hh >= c.Hkv;
-    const int h = hh - (is_v ? c.Hkv : 0);
-    if (turned && !is_v) turn_item<DT>(x[k], y[k], a.rope.half, g);
-    if (a.k_out.p && !is_v && j >= 0 && j < c.cap()) {
-      char* row = a.k_out.at(l, b, h, t);
-      *(uint4*)(row + it.va * 16) = x[k];
-      *(uint4*)(row + it.vb * 16) = y[k];
+    if (h0 + k * m.lanes >= c.Hkv) continue;
+    if (turned) turn_item<DT>(x[k], y[k], a.rope.half, g);
+    if (plain) {
+      char* o = a.k_out.at(l, b, h0 + k * m.lanes, t);
+      *(uint4*)(o + it.va * 16) = x[k];
+      *(uint4*)(o + it.vb * 16) = y[k];
     }
     if (id < 0) continue;
     s_max[tr][it.va] = block_max<DT>(x[k]);
     s_max[tr][it.vb] = block_max<DT>(y[k]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const size_t unit = page_unit(c, l, id, h);
-    const int slot = j & (c.page - 1);
-    char* row = (is_v ? c.v : c.k) + (unit * c.page + slot) * (size_t)(D / 2);
-    uint8_t* scale = (is_v ? c.vx : c.kx) + unit * (size_t)(D / kMx4Block * c.page) + slot;
+    char* to = row + (size_t)(k * m.lanes) * c.page * (D / 2);
+    uint8_t* to_scale = scale + (size_t)(k * m.lanes) * (D / kMx4Block * c.page);
     auto put = [&](const uint4& z, int v) {
       uint32_t top = 0;
 #pragma unroll
@@ -407,10 +408,10 @@ __device__ __forceinline__ void move_rows4(const PagedAppendArgs& a, const Moves
       for (int n = 0; n < V; ++n) f[n] *= inv;
       const uint32_t w = encode8(f);
       if constexpr (V == 8)
-        *(uint32_t*)(row + v * 4) = w;
+        *(uint32_t*)(to + v * 4) = w;
       else
-        *(uint16_t*)(row + v * 2) = (uint16_t)w;
-      if (v % NB == 0) scale[(size_t)(v / NB) * c.page] = nan ? 255 : (uint8_t)(e + 127);
+        *(uint16_t*)(to + v * 2) = (uint16_t)w;
+      if (v % NB == 0) to_scale[v / NB * c.page] = nan ? 255 : (uint8_t)(e + 127);
     };
     put(x[k], it.va);
     put(y[k], it.vb);
@@ -459,9 +460,9 @@ hipError_t launch_mx4(const PagedAppendArgs& a, hipStream_t st) {
   const int64_t lb = (int64_t)a.c.L * a.c.B;
   auto blocks = [&](const Moves& m) { return lb * m.runs * m.chunks; };
   // four heads to a thread, where that leaves a few workgroups to a compute unit
-  const int hpt = blocks(moves_of(a.c, 2 * a.c.Hkv, slots, 4)) >= 4 * kNumCU ? 4 : 1;
-  const Moves m4 = moves_of(a.c, 2 * a.c.Hkv, slots, hpt), m = moves_of(a.c, a.Hq, slots, hpt);
-  const int64_t rows = blocks(m4), all = rows + (a.Hq ? blocks(m) : 0);
+  const int hpt = 2 * blocks(moves_of(a.c, a.c.Hkv, slots, 4)) >= 4 * kNumCU ? 4 : 1;
+  const Moves m4 = moves_of(a.c, a.c.Hkv, slots, hpt), m = moves_of(a.c, a.Hq, slots, hpt);
+  const int64_t rows = 2 * blocks(m4), all = rows + (a.Hq ? blocks(m) : 0);
   if (all >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
   if (hpt == 4)
     hipLaunchKernelGGL((k_append_mx4<DT, D, 4>), dim3((unsigned)all), dim3(kThreads), 0, st, a, m4, m, (unsigned)rows);

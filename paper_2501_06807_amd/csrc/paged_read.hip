@@ -1,7 +1,7 @@
 // Rows of a paged cache, of any page format, as rows of the element type.
 //
 // A row's value is its code times its scale, rounded once to the element type (bf16 and fp32 hold it exactly). A thread has one
-// 16-byte vector of one token's row, in up to HPT heads of K and V, so that a token's page id is looked up once for them.
+// 16-byte vector of a row, in up to HPT heads of K or V, so that a token's page id is looked up once for them.
 #include "attn_mma.h"
 
 namespace mpc {
@@ -11,8 +11,8 @@ using namespace dev;
 constexpr int kThreads = 256;
 
 struct Reads {
-  int tokens, lanes;  // tokens of a workgroup (a power of two), and heads side by side
-  int chunks, runs;   // head chunks and token runs of a (layer, sequence)
+  int tokens, lanes;        // tokens of a workgroup (a power of two), and heads side by side
+  int chunks, sides, runs;  // head chunks, K and V, and token runs of a (layer, sequence)
 };
 
 template <class DT>
@@ -45,6 +45,7 @@ struct Piece {
     if constexpr (FMT == MPC_PAGE_SAME) return w;
     float f[8];
     if constexpr (FMT == MPC_PAGE_MX4) {
+      if constexpr (DT::kCode == MPC_BF16) return widen8(w.x, scale);
       decode8(w.x, scale, f);
     } else {
       decode4(w.x, f);
@@ -56,55 +57,73 @@ struct Piece {
   }
 };
 
-template <class DT, int D, int FMT, int HPT>
+// TPT tokens (a run apart) and HPT heads to a thread, all of their loads on the way at once.
+template <class DT, int D, int FMT, int HPT, int TPT>
 __global__ __launch_bounds__(kThreads) void k_read(PagedReadArgs a, Reads m) {
   constexpr int V = DT::kVec, NV = D / V;
   constexpr int BITS = FMT == MPC_PAGE_MX4 ? 4 : FMT == MPC_PAGE_E4M3 ? 8 : 8 * DT::kElt, RB = D * BITS / 8;
   const PagedCache& c = a.c;
-  const int nk = a.k.p ? c.Hkv : 0, heads = nk + (a.v.p ? c.Hkv : 0);
-  const int chunk = blockIdx.x % (unsigned)m.chunks, run = blockIdx.x / (unsigned)m.chunks % (unsigned)m.runs;
-  const int lb = blockIdx.x / (unsigned)m.chunks / (unsigned)m.runs, b = lb % c.B, l = lb / c.B;
-  const int tr = threadIdx.x / NV, v = threadIdx.x % NV, t = run * m.tokens + (tr & (m.tokens - 1)), lane = tr / m.tokens;
+  // a workgroup has heads of K or of V, then a run of tokens
+  const int chunk = blockIdx.x % (unsigned)m.chunks, side = blockIdx.x / (unsigned)m.chunks % (unsigned)m.sides;
+  const unsigned rest = blockIdx.x / (unsigned)m.chunks / (unsigned)m.sides;
+  const int run = rest % (unsigned)m.runs, lb = rest / (unsigned)m.runs, b = lb % c.B, l = lb / c.B;
+  const bool is_v = side == 1 || !a.k.p;
+  const Rows& out = is_v ? a.v : a.k;
+  const int tr = threadIdx.x / NV, v = threadIdx.x % NV, lane = tr / m.tokens, h0 = chunk * HPT * m.lanes + lane;
+  if (h0 >= c.Hkv) return;
   const int valid = c.n_valid ? min(max(load_uniform(c.n_valid + b), 0), c.n_new) : c.n_new;
-  if (t >= valid) return;
   const int len = min(max(load_uniform(c.lens + b), 0), kMaxRows), rows = min(len, c.cap());
-  const long long at = (a.first ? (long long)load_uniform(a.first + b) : (long long)(len - valid)) + t;
-  if (at < 0 || at >= rows) return;
-  const int j = (int)at;
-  const bool tail = FMT == MPC_PAGE_E4M3 && j >= (rows & ~(c.page - 1));
-  const int id = tail ? 0 : page_id_lane(c, b, j >> c.log_page);
-  if (id < 0) return;
-  const int h0 = chunk * HPT * m.lanes + lane;
-  if (tail) {
-    for (int k = 0; k < HPT; ++k) {
-      const int hh = h0 + k * m.lanes;
-      if (hh >= heads) continue;
-      const bool is_v = hh >= nk;
-      const int h = hh - (is_v ? nk : 0);
-      const size_t row = ((size_t)lb * c.Hkv + h) * (2 * c.page) + (j & (2 * c.page - 1));
-      *(uint4*)((is_v ? a.v : a.k).at(l, b, h, t) + v * 16) = ldg16((is_v ? c.v_tail : c.k_tail) + row * (size_t)(D * DT::kElt) + v * 16);
+  const int full = FMT == MPC_PAGE_E4M3 ? rows & ~(c.page - 1) : rows;
+  const long long from = a.first ? (long long)load_uniform(a.first + b) : (long long)(len - valid);
+  const int t0 = run * TPT * m.tokens + (tr & (m.tokens - 1));
+  int j[TPT], id[TPT];  // rows of the cache, and their pages (-1: no such row)
+#pragma unroll
+  for (int q = 0; q < TPT; ++q) {
+    const int t = t0 + q * m.tokens;
+    const long long at = from + t;
+    const bool ok = t < valid && at >= 0 && at < rows;
+    j[q] = ok ? (int)at : 0;
+    id[q] = page_id_lane(c, b, j[q] >> c.log_page);
+    if (j[q] >= full) id[q] = 0;  // (a row of the ring needs no page)
+    if (!ok) id[q] = -1;
+  }
+  // from one of the thread's heads to the next: pieces and scales of a page, rows
+  const size_t step = (size_t)m.lanes * c.page * RB, scale_step = (size_t)m.lanes * (FMT == MPC_PAGE_MX4 ? D / kMx4Block * c.page : 1);
+  const int64_t out_step = m.lanes * out.head;
+  Piece<DT, FMT> x[TPT][HPT];
+#pragma unroll
+  for (int q = 0; q < TPT; ++q) {
+    if (id[q] < 0) continue;
+    if (FMT == MPC_PAGE_E4M3 && j[q] >= full) {
+      const char* p = (is_v ? c.v_tail : c.k_tail) + (((size_t)lb * c.Hkv + h0) * (2 * c.page) + (j[q] & (2 * c.page - 1))) * (size_t)(D * DT::kElt) + v * 16;
+      char* o = out.at(l, b, h0, t0 + q * m.tokens) + v * 16;
+      for (int k = 0; k < HPT && h0 + k * m.lanes < c.Hkv; ++k) {
+        *(uint4*)o = ldg16(p);
+        p += (size_t)m.lanes * (2 * c.page) * (D * DT::kElt);
+        o += out_step;
+      }
+      continue;
     }
-    return;
-  }
-  Piece<DT, FMT> x[HPT];
+    const size_t unit = page_unit(c, l, id[q], h0);
+    const int slot = j[q] & (c.page - 1);
+    const char* p = (is_v ? c.v : c.k) + (unit * c.page + slot) * RB + v * (V * BITS / 8);
+    const uint8_t* px = FMT == MPC_PAGE_MX4 ? (is_v ? c.vx : c.kx) + unit * (size_t)(D / kMx4Block * c.page) + v * V / kMx4Block * c.page + slot : nullptr;
+    const float* ps = FMT == MPC_PAGE_E4M3 ? (is_v ? c.vs : c.ks) + unit : nullptr;
 #pragma unroll
-  for (int k = 0; k < HPT; ++k) {
-    const int hh = h0 + k * m.lanes;
-    if (hh >= heads) continue;
-    const bool is_v = hh >= nk;
-    const size_t unit = page_unit(c, l, id, hh - (is_v ? nk : 0));
-    const int slot = j & (c.page - 1);
-    x[k].load((is_v ? c.v : c.k) + (unit * c.page + slot) * RB + v * (V * BITS / 8));
-    if constexpr (FMT == MPC_PAGE_E4M3) x[k].scale = (is_v ? c.vs : c.ks)[unit];
-    if constexpr (FMT == MPC_PAGE_MX4)
-      x[k].scale = mx4_scale((is_v ? c.vx : c.kx)[unit * (size_t)(D / kMx4Block * c.page) + v * V / kMx4Block * c.page + slot]);
+    for (int k = 0; k < HPT; ++k) {
+      if (h0 + k * m.lanes >= c.Hkv) continue;
+      x[q][k].load(p + k * step);
+      if constexpr (FMT == MPC_PAGE_E4M3) x[q][k].scale = ps[k * scale_step];
+      if constexpr (FMT == MPC_PAGE_MX4) x[q][k].scale = mx4_scale(px[k * scale_step]);
+    }
   }
 #pragma unroll
-  for (int k = 0; k < HPT; ++k) {
-    const int hh = h0 + k * m.lanes;
-    if (hh >= heads) continue;
-    const bool is_v = hh >= nk;
-    *(uint4*)((is_v ? a.v : a.k).at(l, b, hh - (is_v ? nk : 0), t) + v * 16) = x[k].rows();
+  for (int q = 0; q < TPT; ++q) {
+    if (id[q] < 0 || (FMT == MPC_PAGE_E4M3 && j[q] >= full)) continue;
+    char* o = out.at(l, b, h0, t0 + q * m.tokens) + v * 16;
+#pragma unroll
+    for (int k = 0; k < HPT; ++k)
+      if (h0 + k * m.lanes < c.Hkv) *(uint4*)(o + k * out_step) = x[q][k].rows();
   }
 }
 
@@ -112,24 +131,24 @@ template <class DT, int D, int FMT>
 hipError_t launch(const PagedReadArgs& a, hipStream_t st) {
   constexpr int slots = kThreads / (D / DT::kVec);
   const PagedCache& c = a.c;
-  const int heads = ((a.k.p ? 1 : 0) + (a.v.p ? 1 : 0)) * c.Hkv;
   Reads m{};
+  m.sides = (a.k.p ? 1 : 0) + (a.v.p ? 1 : 0);
   m.tokens = 1;
   while (m.tokens < slots && m.tokens < c.n_new) m.tokens *= 2;
   m.lanes = slots / m.tokens;
-  m.runs = (int)(((int64_t)c.n_new + m.tokens - 1) / m.tokens);
-  auto blocks = [&](int hpt) {
-    m.chunks = (heads + hpt * m.lanes - 1) / (hpt * m.lanes);
-    return (int64_t)c.L * c.B * m.runs * m.chunks;
+  auto blocks = [&](int hpt, int tpt) {
+    m.runs = (int)(((int64_t)c.n_new + m.tokens * tpt - 1) / (m.tokens * tpt));
+    m.chunks = (c.Hkv + hpt * m.lanes - 1) / (hpt * m.lanes);
+    return (int64_t)c.L * c.B * m.runs * m.sides * m.chunks;
   };
-  // four heads to a thread, where that leaves a few workgroups to a compute unit
-  const int hpt = blocks(4) >= 4 * kNumCU ? 4 : 1;
-  const int64_t n = blocks(hpt);
+  // four heads and four tokens to a thread, where that leaves a few workgroups to a compute unit
+  const bool many = blocks(4, 4) >= 4 * kNumCU;
+  const int64_t n = many ? blocks(4, 4) : blocks(1, 1);
   if (n >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-  if (hpt == 4)
-    hipLaunchKernelGGL((k_read<DT, D, FMT, 4>), dim3((unsigned)n), dim3(kThreads), 0, st, a, m);
+  if (many)
+    hipLaunchKernelGGL((k_read<DT, D, FMT, 4, 4>), dim3((unsigned)n), dim3(kThreads), 0, st, a, m);
   else
-    hipLaunchKernelGGL((k_read<DT, D, FMT, 1>), dim3((unsigned)n), dim3(kThreads), 0, st, a, m);
+    hipLaunchKernelGGL((k_read<DT, D, FMT, 1, 1>), dim3((unsigned)n), dim3(kThreads), 0, st, a, m);
   return hipGetLastError();
 }
 

@@ -263,10 +263,12 @@ SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, i
   p.group = p.total + align256(sizeof(SharedTotals));
   p.seq = p.group + align256((size_t)groups * sizeof(SharedGroup));
   p.shared_head = p.seq + align256((size_t)B * sizeof(SharedSeq));
+  // as many places for the workers' parts as any form has, so that a workspace made for the most tokens serves calls of fewer
+  const size_t most_shared = (size_t)kNumCU * (dtype == MPC_FP32 ? 32 : 128), most_own = (size_t)kNumCU * 128;
   p.shared_more = p.shared_head + heads;
-  p.own_head = p.shared_more + align256((size_t)p.shared_workers * p.shared_rows * row);
+  p.own_head = p.shared_more + align256(most_shared * row);
   p.own_more = p.own_head + heads;
-  p.ws_bytes = std::max(p.own_more + (size_t)p.own_workers * p.own_rows * row, paged_plan(dtype, D, L, B, Hq, Hkv, n, cap).ws_bytes);
+  p.ws_bytes = std::max(p.own_more + most_own * row, paged_plan(dtype, D, L, B, Hq, Hkv, n, cap).ws_bytes);
   return p;
 }
 

@@ -44,3 +44,17 @@ def test_workspace():
         assert bad == 0
     huge = cache(max_pages=1 << 24, page_size=64)
     assert size(dims(batch=1024), 1, huge, 1) == 0 and shared(d=dims(batch=1024), kv=huge, groups=1, ws_bytes=1 << 50)[0] == L.MPC_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("heads", [(8, 8), (8, 2), (8, 1)])
+def test_bytes_never_fall(dtype, heads):
+    """A workspace made for the most tokens, sequences and groups serves calls of fewer, whatever form each takes."""
+    make = lambda b, L=2: dims(batch=b, n_layers=L, n_q_heads=heads[0], n_kv_heads=heads[1], dtype=dtype)  # noqa: E731
+    for groups in (1, 3, 16):
+        sizes = [size(make(16), n, cache(), groups) for n in (1, 2, 3, 4, 5, 8, 9, 16, 17, 33, 64, 100, 1000)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+    for n in (1, 4, 40):
+        assert sorted(s := [size(make(16), n, cache(), g) for g in range(1, 17)]) == s
+        assert sorted(s := [size(make(b), n, cache(), 1) for b in range(1, 80)]) == s
+        assert size(make(8, 1), n, cache(), 2) <= size(make(8, 5), n, cache(), 2)
