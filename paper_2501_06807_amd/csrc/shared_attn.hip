@@ -9,108 +9,10 @@ namespace {
 using namespace dev;
 constexpr int kJoinThreads = 256;
 
-// Sum of x over the threads before this one, and over all of them.
-template <int THREADS>
-__device__ __forceinline__ unsigned sum_before(unsigned x, unsigned* s_wave, unsigned* total) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  unsigned sum = x;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const unsigned y = __shfl_up(sum, o);
-    if (lane >= o) sum += y;
-  }
-  if constexpr (THREADS == kWave) {
-    *total = __builtin_amdgcn_readlane(sum, kWave - 1);
-    return sum - x;
-  }
-  if (lane == kWave - 1) s_wave[wave] = sum;
-  __syncthreads();
-  unsigned before = 0, all = 0;
-  for (int w = 0; w < THREADS / kWave; ++w) {
-    before += w < wave ? s_wave[w] : 0;
-    all += s_wave[w];
-  }
-  __syncthreads();
-  *total = all;
-  return before + sum - x;
-}
-
-// One workgroup (a wave where that has the groups and sequences): a thread to a group, and the sequences over the threads. Bounds of the groups are brought into [0, B] and in
-// order, so that every sequence is in one group at most, whatever `first` holds.
-template <bool C8, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_shared_plan(SharedArgs a) {
-  __shared__ int s_f[THREADS + 1], s_base[THREADS], s_lo[THREADS], s_hi[THREADS];
-  __shared__ unsigned s_wave[THREADS / kWave];
-  const PagedCache& c = a.c;
-  const int tid = threadIdx.x, ng = a.groups;
-  s_f[tid] = tid < ng ? min(max(a.first[tid], 0), a.B) : 0;
-  __syncthreads();
-  for (int o = 1; o < ng; o <<= 1) {
-    const int y = tid >= o ? s_f[tid - o] : 0;
-    __syncthreads();
-    s_f[tid] = max(s_f[tid], y);
-    __syncthreads();
-  }
-  if (tid == 0) s_f[ng] = max(s_f[ng - 1], min(max(a.first[ng], 0), a.B));
-  if (tid < ng) {
-    s_base[tid] = min(max(a.rows[tid], 0), c.cap()) & ~(c.page - 1);
-    s_lo[tid] = kMaxRows;
-    s_hi[tid] = -1;
-  }
-  __syncthreads();
-  unsigned own = 0, rows = 0;  // blocks and query rows of the sequences so far
-  for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-    const int b = b0 + tid;
-    SharedSeq q{0, 0, -1, 0, 0};
-    unsigned blocks = 0, mine = 0;
-    if (b < a.B) {
-      if (b >= s_f[0] && b < s_f[ng]) {  // the last group that begins at or before b
-        int g = 0, z = ng;
-        while (z - g > 1) {
-          const int m = (g + z) / 2;
-          (s_f[m] <= b ? g : z) = m;
-        }
-        q.group = g;
-        q.base = s_base[g];
-      }
-      const OwnRows s = own_rows<C8>(a, c.lens[b], c.n_valid ? c.n_valid[b] : c.n_new, q.base, a.own.unit_rows);
-      if (q.group >= 0 && s.valid > 0) {
-        atomicMin(&s_lo[q.group], s.start);
-        atomicMax(&s_hi[q.group], s.len - 1);
-      }
-      q.nb = (s.all + a.own_block - 1) / a.own_block;
-      blocks = (unsigned)(s.groups * a.L * a.Hkv) * (unsigned)q.nb;
-      mine = (unsigned)s.valid << a.log_g;
-    }
-    unsigned all;
-    q.block0 = own + sum_before<THREADS>(blocks, s_wave, &all);
-    own += all;
-    q.row0 = (int)(rows + sum_before<THREADS>(mine, s_wave, &all));
-    rows += all;
-    if (b < a.B) a.seq[b] = q;
-  }
-  __syncthreads();
-  SharedGroup p{};
-  if (tid < ng) {
-    p.f0 = s_f[tid];
-    p.f1 = s_f[tid + 1];
-    p.base = s_base[tid];
-    p.row0 = p.f0 < a.B ? a.seq[p.f0].row0 : (int)rows;
-    p.query_rows = (p.f1 < a.B ? a.seq[p.f1].row0 : (int)rows) - p.row0;
-    p.rt = (p.query_rows + a.shared.unit_rows - 1) / a.shared.unit_rows;
-    const int all = (max(0, min(p.base, s_hi[tid] + 1)) + a.tile - 1) / a.tile;
-    p.skip = p.at = all;
-    if (a.window) {
-      p.skip = min((a.sinks + a.tile - 1) / a.tile, all);
-      p.at = max(p.skip, min(max(s_lo[tid] - a.window + 1, 0) / a.tile, all));
-    }
-    p.tiles = p.skip + all - p.at;
-    p.nb = (p.tiles + a.shared_block - 1) / a.shared_block;
-  }
-  unsigned total;
-  p.block0 = sum_before<THREADS>((unsigned)(p.rt * a.L * a.Hkv) * (unsigned)p.nb, s_wave, &total);
-  if (tid < ng) a.group[tid] = p;
-  if (tid == 0) *a.total = SharedTotals{total, own};
+template <bool C8>
+__global__ __launch_bounds__(kMaxGroups) void k_shared_plan(SharedArgs a) {
+  __shared__ PlanScratch<kMaxGroups> tmp;
+  make_plan<C8, kMaxGroups>(a, tmp, a.group, a.seq, a.total);
 }
 
 // The join. A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the shared ones; where
@@ -273,17 +175,14 @@ SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, i
 }
 
 hipError_t launch_shared_attn(const SharedArgs& a, int dtype, int D, hipStream_t st) {
-  const bool small = a.B <= kWave, codes8 = a.c.format == MPC_PAGE_E4M3;
-  if (small && codes8)
-    hipLaunchKernelGGL((k_shared_plan<true, kWave>), dim3(1), dim3(kWave), 0, st, a);
-  else if (small)
-    hipLaunchKernelGGL((k_shared_plan<false, kWave>), dim3(1), dim3(kWave), 0, st, a);
-  else if (codes8)
-    hipLaunchKernelGGL((k_shared_plan<true, kMaxGroups>), dim3(1), dim3(kMaxGroups), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_shared_plan<false, kMaxGroups>), dim3(1), dim3(kMaxGroups), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  hipError_t e;
+  if (a.B > kPlanLanes) {  // fewer: every workgroup makes the plan for itself
+    if (a.c.format == MPC_PAGE_E4M3)
+      hipLaunchKernelGGL(k_shared_plan<true>, dim3(1), dim3(kMaxGroups), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_shared_plan<false>, dim3(1), dim3(kMaxGroups), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   e = a.c.format == MPC_PAGE_MX4 ? launch_shared_mx4(a, dtype, D, st)
       : dtype == MPC_FP32        ? launch_shared_fp32(a, D, st)
       : dtype == MPC_FP16        ? launch_shared_fp16(a, D, st)

@@ -13,7 +13,7 @@ namespace mpc {
 namespace dev {
 
 template <class DT, int D, int FMT, int NS>
-__device__ __forceinline__ void shared_wide(const SharedArgs& a) {
+__device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& plan) {
   constexpr bool C8 = FMT == MPC_PAGE_E4M3, C4 = FMT == MPC_PAGE_MX4, CODES = C8 || C4;
   constexpr bool H = DT::kCode == MPC_FP16, SPLIT = C4 && H, TWO = CODES && H;
   using QT = std::conditional_t<C4, BF16, DT>;    // type of the scores' product
@@ -32,11 +32,11 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a) {
   const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
 
-  const unsigned total = load_uniform(&a.total->shared), id = by_die(blockIdx.x, gridDim.x);
+  const unsigned total = plan.shared, id = by_die(blockIdx.x, gridDim.x);
   const unsigned per = (total + gridDim.x - 1) / gridDim.x;
   if ((unsigned long long)id * per >= total) return;
   const unsigned first = id * per, last = min(first + per, total);
-  int gi = last_from(a.groups, last - 1, [&](int i) { return a.group[i].block0; });
+  int gi = last_from(a.groups, last - 1, [&](int i) { return plan.group[i].block0; });
   // a negative scale is taken into the queries (8-bit codes: it stays with the pages' scales); zero times a masked score would be
   // NaN: the smallest number that is not zero instead
   const float qs = C8 ? a.qscale : fmaxf(fabsf(a.qscale), 0x1p-149f);
@@ -47,18 +47,18 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a) {
   // unit's first key, what it begins with ends at a unit's last one.
   unsigned x_end = last;
   while (x_end > first) {
-    while (gi > 0 && x_end <= load_uniform(&a.group[gi].block0)) --gi;
-    const SharedGroup* gp = a.group + gi;
-    const int f0 = load_uniform(&gp->f0), nb = load_uniform(&gp->nb), rts = load_uniform(&gp->rt);
-    const int base = load_uniform(&gp->base), skip = load_uniform(&gp->skip), at = load_uniform(&gp->at);
-    const unsigned block0 = load_uniform(&gp->block0), in = x_end - 1 - block0;
+    while (gi > 0 && x_end <= same(plan.group[gi].block0)) --gi;
+    const SharedGroup* gp = plan.group + gi;
+    const int f0 = same(gp->f0), nb = same(gp->nb), rts = same(gp->rt);
+    const int base = same(gp->base), skip = same(gp->skip), at = same(gp->at);
+    const unsigned block0 = same(gp->block0), in = x_end - 1 - block0;
     const int u = __builtin_amdgcn_readfirstlane(in / (unsigned)nb), blk_end = __builtin_amdgcn_readfirstlane(in - u * (unsigned)nb) + 1;
     const unsigned unit0 = block0 + u * (unsigned)nb;  // the unit's first block
     const int blk = first > unit0 ? (int)(first - unit0) : 0;
     const int lh = u / rts, h = lh % a.Hkv, l = lh / a.Hkv, r0 = u % rts * 128;
-    const int i0 = blk * a.shared_block, i1 = min(blk_end * a.shared_block, load_uniform(&gp->tiles));
+    const int i0 = blk * a.shared_block, i1 = min(blk_end * a.shared_block, same(gp->tiles));
 
-    const SharedRow row = shared_row(a, gp, r0 + 32 * wave + q32);
+    const SharedRow row = shared_row(a, plan.seq, gp, r0 + 32 * wave + q32);
     // a row that is not there sees every key, so that it makes no tile an edge; nobody reads it
     const int pos = row.live ? row.pos : kMaxRows;
     int lo = row.live ? pos : kMaxRows, hi = row.live ? pos : -kMaxRows;
@@ -433,12 +433,14 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a) {
 // With the own rows where their units have 16 query rows (OWN); units of 32 take more registers than are left here.
 template <class DT, int D, int FMT, bool OWN>
 __global__ __launch_bounds__(256 * kWideGroups, 2) void k_shared_wide(SharedArgs a) {
-  shared_wide<DT, D, FMT, kWideGroups>(a);
-  if constexpr (OWN) own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a);
+  __shared__ PlanSpace space;
+  const Plan plan = plan_of<FMT == MPC_PAGE_E4M3>(a, space);
+  shared_wide<DT, D, FMT, kWideGroups>(a, plan);
+  if constexpr (OWN) own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a, plan);
 }
 template <class DT, int D, int FMT>
 __global__ __launch_bounds__(kOwnWaves * kWave) void k_own_rows(SharedArgs a) {
-  own_rows_of<DT, D, FMT, 2, kOwnWaves>(a);
+  own_rows_of<DT, D, FMT, 2, kOwnWaves>(a, Plan{a.group, a.seq, load_uniform(&a.total->shared), load_uniform(&a.total->own)});
 }
 
 }  // namespace dev
