@@ -491,44 +491,44 @@ __device__ __forceinline__ void walk_pages(PagedWave<DT, D, FMT, RT>& w, const A
 #pragma unroll
     for (int hf = 0; hf < TL::HALVES; ++hf) id[hf] = page_of_entry(c, e[hf], page_at(i, hf));
   };
-  // row 0 of a tile's half in the pool (page 0 where it has no page: its rows are not used)
-  auto place = [&](int i, int hf, int id) {
-    return page_unit(c, l, max(id, 0), h) * c.page + ((page_tile(i) * TL::TK + 16 * hf) & (c.page - 1));
-  };
-  // scale byte of block `blk` of a half's first row (4 bits)
-  auto mx4_at = [&](const uint8_t* x, size_t row, int blk) {
-    return x + (row >> c.log_page) * (size_t)(TL::SB * c.page) + blk * c.page + (row & (c.page - 1));
-  };
+  // This (layer, kv head)'s part of page 0 and the bytes (scales) from a page to the next; a lane's place in a half's rows.
+  const size_t unit0 = page_unit(c, l, 0, h), page_bytes = (size_t)c.Hkv * c.page * TL::RB;
+  const char *k_page = c.k + unit0 * c.page * TL::RB, *v_page = c.v + unit0 * c.page * TL::RB;
+  const unsigned k_lane = col * TL::RB + g * (TL::RB < 64 ? 8 : 16), v_lane = 4 * g * TL::RB + col * (TL::RB / 16);
+  const uint8_t *kx_page = C4 ? c.kx + unit0 * (TL::SB * c.page) : nullptr, *vx_page = C4 ? c.vx + unit0 * (TL::SB * c.page) : nullptr;
+  const unsigned kx_lane = g * TL::SB / 4 * c.page + col, vx_lane = col * TL::SB / 16 * c.page + 4 * g;
+  // a half's first row (page 0 where it has no page: its rows are not used)
+  auto slot_of = [&](int i, int hf) { return (page_tile(i) * TL::TK + 16 * hf) & (c.page - 1); };
   auto load_k = [&](int i, const int* id, uint4 (*k)[TL::KL], float* ks, uint32_t* kx) {
 #pragma unroll
     for (int hf = 0; hf < TL::HALVES; ++hf) {
-      const size_t row = place(i, hf, id[hf]);
-      const char* p = c.k + row * TL::RB + col * TL::RB + g * (TL::RB < 64 ? 8 : 16);
+      const int n = max(id[hf], 0), slot = slot_of(i, hf);
+      const char* p = k_page + (n * page_bytes + (size_t)slot * TL::RB);
       if constexpr (TL::RB < 64) {
-        const uint2 x = *(const uint2*)p;
+        const uint2 x = *(const uint2*)(p + k_lane);
         k[hf][0] = make_uint4(x.x, x.y, 0, 0);
       } else {
 #pragma unroll
-        for (int n = 0; n < TL::KL; ++n) k[hf][n] = ldg16(p + n * 64);
+        for (int m = 0; m < TL::KL; ++m) k[hf][m] = ldg16(p + k_lane + m * 64);
       }
-      if constexpr (C8) ks[hf] = load_uniform(c.ks + (row >> c.log_page));
-      if constexpr (C4) kx[hf] = mx4_at(c.kx, row, g * TL::SB / 4)[col];
+      if constexpr (C8) ks[hf] = load_uniform(c.ks + unit0 + (size_t)n * c.Hkv);
+      if constexpr (C4) kx[hf] = (kx_page + ((size_t)n * c.Hkv * (TL::SB * c.page) + slot))[kx_lane];
     }
   };
   auto load_v = [&](int i, const int* id, uint32_t (*v)[TL::VW], float* vs, uint32_t* vx) {
 #pragma unroll
     for (int hf = 0; hf < TL::HALVES; ++hf) {
-      const size_t row = place(i, hf, id[hf]);
-      const char* p = c.v + row * TL::RB + 4 * g * TL::RB + col * (TL::RB / 16);
+      const int n = max(id[hf], 0), slot = slot_of(i, hf);
+      const char* p = v_page + (n * page_bytes + (size_t)slot * TL::RB);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (TL::RB < 64)
-          v[4 * hf + j][0] = *(const uint16_t*)(p + j * TL::RB);
+          v[4 * hf + j][0] = *(const uint16_t*)(p + v_lane + j * TL::RB);
         else
-          load_words<TL::VW>(p + j * TL::RB, v[4 * hf + j]);
+          load_words<TL::VW>(p + v_lane + j * TL::RB, v[4 * hf + j]);
       }
-      if constexpr (C8) vs[hf] = load_uniform(c.vs + (row >> c.log_page));
-      if constexpr (C4) vx[hf] = *(const uint32_t*)(mx4_at(c.vx, row, col * TL::SB / 16) + 4 * g);
+      if constexpr (C8) vs[hf] = load_uniform(c.vs + unit0 + (size_t)n * c.Hkv);
+      if constexpr (C4) vx[hf] = *(const uint32_t*)(vx_page + ((size_t)n * c.Hkv * (TL::SB * c.page) + slot) + vx_lane);
     }
   };
   using Operand = std::conditional_t<TL::F, float[TL::VK][NT], uint32_t[NT][4]>;
