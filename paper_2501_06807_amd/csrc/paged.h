@@ -90,11 +90,12 @@ hipError_t launch_paged_attn_bf16(const PagedAttnArgs& a, int D, hipStream_t st)
 hipError_t launch_paged_attn_mx4(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int D, hipStream_t st);
 
-// Attention behind shared rows, four launches: the plan, made on the device; the shared rows of every group, for the rows of all
-// its sequences; each sequence's own rows; and the join. Both of the middle ones divide blocks of keys evenly over their
-// workers (workgroups there, waves here), in the order of groups or sequences, units of query rows and keys, and leave what they
-// have of each row of a unit: the worker that has a unit's first block in `head`, by row, the ones that go on with it in `more`, a
-// place for each worker (whose run goes on with one unit at most).
+// Attention behind shared rows, two launches (three beyond 64 sequences, whose plan is made by one of its own): the shared rows
+// of every group, for the rows of all its sequences, and each sequence's own rows; then the join. Both kinds of rows are divided
+// into blocks of keys, evenly over their workers (workgroups for the shared ones, waves for the own ones), in the order of groups
+// or sequences, units of query rows and keys, and leave what they have of each row of a unit: the worker that has a unit's first
+// block in `head`, by row, the ones that go on with it in `more`, a place for each worker (whose run goes on with one unit
+// at most).
 constexpr int kMaxGroups = 1024;
 constexpr int kPartTail = 4;  // maximum and sum behind a row's D accumulators, and what keeps rows 16-byte aligned
 struct Parts {
@@ -133,7 +134,6 @@ struct SharedPlan {
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
 constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
-constexpr int kOwnWaves = 4;  // waves of a workgroup that takes own rows
 SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_fp16(const SharedArgs& a, int D, hipStream_t st);

@@ -147,13 +147,13 @@ SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, i
   const long long each_seq = (long long)n * (Hq / Hkv), rows = B * each_seq, each = (rows + groups - 1) / groups, lh = (long long)L * Hkv;
   p.wide = dtype != MPC_FP32 && each > 32;
   p.shared_rows = p.wide ? 128 : each <= 16 ? 16 : 32;
-  p.own_rows = each_seq <= 16 ? 16 : 32;
+  p.own_rows = each_seq <= 16 || p.wide ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
   p.shared_block = p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16);
   p.own_block = 64 / p.tile;
   p.shared_workers = p.wide ? kNumCU * 2 / kWideGroups : kNumCU;
-  // own rows by the waves of the kernel that takes the shared ones, or by a launch of their own (wide units, 32 rows to own units)
-  p.own_workers = kNumCU * (p.wide ? (p.own_rows == 16 ? 4 * kWideGroups : kOwnWaves) : paged_waves(p.shared_rows / 16));
+  // own rows are taken by the waves of the kernel that takes the shared ones
+  p.own_workers = kNumCU * (p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16));
   auto blocks = [&](long long units, long long block) {
     const double nb = cap / (p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short
     return (double)units * nb >= 2147483648.0 ? 1ll << 31 : units * (long long)nb;

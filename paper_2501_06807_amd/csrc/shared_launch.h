@@ -9,15 +9,7 @@ template <class DT, int D, int FMT>
 hipError_t launch_shared_d(const SharedArgs& a, hipStream_t st) {
   if constexpr (DT::kElt == 2) {
     if (a.wide) {
-      const dim3 grid((unsigned)a.shared.workers), block(256 * kWideGroups);
-      if (a.own.unit_rows == 16) {
-        hipLaunchKernelGGL((k_shared_wide<DT, D, FMT, true>), grid, block, 0, st, a);
-        return hipGetLastError();
-      }
-      hipLaunchKernelGGL((k_shared_wide<DT, D, FMT, false>), grid, block, 0, st, a);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((k_own_rows<DT, D, FMT>), dim3((unsigned)(a.own.workers / kOwnWaves)), dim3(kOwnWaves * kWave), 0, st, a);
+      hipLaunchKernelGGL((k_shared_wide<DT, D, FMT>), dim3((unsigned)a.shared.workers), dim3(256 * kWideGroups), 0, st, a);
       return hipGetLastError();
     }
   }

@@ -26,6 +26,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
   constexpr int RB = C4 ? D / 2 : C8 ? D : 2 * D;            // bytes of a page's row
   __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
   __shared__ int s_bad[NS][2];     // the last round whose values, staged for an edge, were not all finite
+  __shared__ uint4 s_q2[SPLIT ? 4 : 1][KSTEPS][SPLIT ? kWave : 1];  // second parts of the queries (registers do not hold them)
   __shared__ int s_range[4][2];    // positions of the waves' rows
   const PagedCache& c = a.c;
   const int tid = threadIdx.x % THREADS, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
@@ -74,7 +75,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       s_range[wave][1] = hi;
     }
     if (threadIdx.x < 2 * NS) (&s_bad[0][0])[threadIdx.x] = -1;
-    uint4 q[KSTEPS], q2[SPLIT ? KSTEPS : 1];
+    uint4 q[KSTEPS];
     {
       const int t = row.in_seq >> a.log_g, hq = (h << a.log_g) + row.in_seq - (t << a.log_g);
       const char* p = a.q.at(l, row.b, hq, t) + hl * 16;
@@ -82,7 +83,11 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       for (int i = 0; i < KSTEPS; ++i) {
         const uint4 y = ldg16(p + i * 32);
         q[i] = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
-        if constexpr (SPLIT) split_bf16(q[i], q2[i]);
+        if constexpr (SPLIT) {
+          uint4 rest;
+          split_bf16(q[i], rest);
+          if (grp == 0) s_q2[wave][i][lane] = rest;
+        }
       }
     }
     f32x16 o[DB];
@@ -262,7 +267,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
       for (int i = 0; i < KSTEPS; ++i) {
-        if constexpr (SPLIT) s = mma32<QT>(kf[i], q2[i], s);
+        if constexpr (SPLIT) s = mma32<QT>(kf[i], s_q2[wave][i][lane], s);
         s = mma32<QT>(kf[i], q[i], s);
       }
       // the lane's keys lie 8 (r / 4) + r % 4 behind this one
@@ -430,17 +435,14 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
   }
 }
 
-// With the own rows where their units have 16 query rows (OWN); units of 32 take more registers than are left here.
-template <class DT, int D, int FMT, bool OWN>
+// Shared rows, then own ones, in units of 16 query rows (units of 32, in a launch of their own for want of registers, take as long:
+// 616 us of eight prompts' 614).
+template <class DT, int D, int FMT>
 __global__ __launch_bounds__(256 * kWideGroups, 2) void k_shared_wide(SharedArgs a) {
   __shared__ PlanSpace space;
   const Plan plan = plan_of<FMT == MPC_PAGE_E4M3>(a, space);
   shared_wide<DT, D, FMT, kWideGroups>(a, plan);
-  if constexpr (OWN) own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a, plan);
-}
-template <class DT, int D, int FMT>
-__global__ __launch_bounds__(kOwnWaves * kWave) void k_own_rows(SharedArgs a) {
-  own_rows_of<DT, D, FMT, 2, kOwnWaves>(a, Plan{a.group, a.seq, load_uniform(&a.total->shared), load_uniform(&a.total->own)});
+  own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a, plan);
 }
 
 }  // namespace dev
