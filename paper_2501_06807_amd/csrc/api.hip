@@ -203,7 +203,7 @@ mpc_status check_groups(const mpc_dims* d, int32_t n_new, int32_t n_groups) {
 }
 
 mpc::SharedPlan shared_plan_of(const mpc_dims* d, const mpc_paged_kv* kv, int n, int groups) {
-  return mpc::shared_plan(d->dtype, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
+  return mpc::shared_plan(d->dtype, kv->format, d->head_dim, d->n_layers, d->batch, d->n_q_heads, d->n_kv_heads, n,
                           kv->max_pages * kv->page_size, groups);
 }
 

@@ -134,7 +134,7 @@ struct SharedPlan {
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
 constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
-SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
+SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_fp16(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_bf16(const SharedArgs& a, int D, hipStream_t st);

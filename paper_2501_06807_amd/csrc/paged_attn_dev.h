@@ -20,9 +20,15 @@
 // such range: they are lifted by 2^14, so that only weights below 2^-28 of the largest lose bits of their first part, and the
 // scale is applied to a tile's product in fp32.
 //
+// 4-bit codes have a scale for each 32 channels of a row, so they become bf16 values with their scale (v_cvt_scalef32, exact) before they
+// are transposed; fp16, whose range does not hold code times scale, is multiplied in bf16 too, with the queries in two parts
+// (8 + 3 places, exact).
+//
 // Reading K and V bounds it: 4 x 32K rows, 2 layers of 32 heads of 128 over 8-bit pages, 2.1 GB in 371 us (5.8 TB/s); one
 // sequence of 128K rows and 8 kv heads, 268 MB in 61 us, of which about 12 are not reading: the launch, the chain of
-// lengths, table entry and first rows (4), and the joins (4 to 8). In between the dies differ: their workgroups read at rates
+// lengths, table entry and first rows (4), and the joins (4 to 8). The same rows of 4-bit codes: 1.14 GB in 201 us (5.7 TB/s; a
+// tile's 230 vector operations keep that unit busy half of the time, and tiles two ahead instead of one gain nothing, 206), three drafts
+// over 128K rows 143 MB in 46 us. In between the dies differ: their workgroups read at rates
 // 35% apart, so that the even division ends with the slowest (41 us on average, 48 on the last). Keys two tiles ahead instead
 // of one changed nothing (373 and 63 us), nor did runs of at least four blocks where there is enough work. 32 sequences of
 // four drafted tokens behind a window of 1024 (16-bit pages of 16 rows) take 32 us, 136 MB (147 fetched): each workgroup has

@@ -15,7 +15,8 @@ __global__ __launch_bounds__(kMaxGroups) void k_shared_plan(SharedArgs a) {
   make_plan<C8, kMaxGroups>(a, tmp, a.group, a.seq, a.total);
 }
 
-// The join. A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the shared ones; where
+// The join: 8.4 us for 1024 rows of 33 parts each, 25 for 54K rows of two or three (110 MB; a wave to a row, statistics before the
+// accumulators: 14 and 59). A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the shared ones; where
 // there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
 template <class DT, int D, bool ALL>
 __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
@@ -140,19 +141,23 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 
 }  // namespace
 
-// Units of as many query rows as a group has on average, up to 32, and of 128 in 16-bit types beyond that; own rows in units of 16 where a sequence's fit, else 32. Blocks
-// are a tile to each wave of a workgroup (shared rows), and 128 keys to a wave (own rows).
-SharedPlan shared_plan(int dtype, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
+// Shared rows in units of 128 query rows where a group has more than 32 on average (16-bit types), else of 32, or of 16 over codes
+// where that is enough. Measured, 16K shared rows of 8 kv heads of 128, us: 40 query rows to a kv head in units of 32 and of 128, bf16
+// 39 and 37, 8-bit codes 40 and 36, 4-bit codes 37 and 33 (fp16 39 and 40), 96 rows 54 and 42; 32 rows 32 and 37, 32 and 34, 30 and 32.
+// 16 rows in units of 16 and of 32: bf16 34 and 30, fp32 50 and 51 (1K shared rows: 38 and 30), 8-bit codes 28 and 30, 4-bit codes
+// 25 and 28. Own rows in units of 16 where a sequence's rows fit, or beside the wide units, else of 32. Blocks are a tile to each
+// wave of a workgroup (wide units: four tiles to each group of waves), and 64 keys of the own rows, which are taken by the waves
+// of the kernel that takes the shared ones.
+SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
   SharedPlan p{};
   const long long each_seq = (long long)n * (Hq / Hkv), rows = B * each_seq, each = (rows + groups - 1) / groups, lh = (long long)L * Hkv;
   p.wide = dtype != MPC_FP32 && each > 32;
-  p.shared_rows = p.wide ? 128 : each <= 16 ? 16 : 32;
+  p.shared_rows = p.wide ? 128 : each <= 16 && format != MPC_PAGE_SAME ? 16 : 32;
   p.own_rows = each_seq <= 16 || p.wide ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
   p.shared_block = p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16);
   p.own_block = 64 / p.tile;
-  p.shared_workers = p.wide ? kNumCU * 2 / kWideGroups : kNumCU;
-  // own rows are taken by the waves of the kernel that takes the shared ones
+  p.shared_workers = kNumCU;
   p.own_workers = kNumCU * (p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16));
   auto blocks = [&](long long units, long long block) {
     const double nb = cap / (p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short

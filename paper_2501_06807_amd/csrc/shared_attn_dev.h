@@ -1,7 +1,16 @@
-// Attention behind shared rows: the kernels of the shared rows for units of 16 or 32 query rows, and of the sequences' own rows.
+// Attention behind shared rows: the plan, the shared rows for units of 16 or 32 query rows, and the sequences' own rows.
 //
 // A group's query rows (all its sequences' tokens and the G heads of a kv head) are one unit's rows as far as they fit, so K and
-// V of the shared rows are read once for a unit instead of once for a sequence. The tiles' work is the paged attention's.
+// V of the shared rows are read once for a unit instead of once for a sequence; a softmax over both kinds of rows is the join of
+// its parts over each, o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p with m = max_p m_p. The tiles' work is the paged
+// attention's. Reading the keys bounds it: 64 sequences in four groups behind 8K rows of 8-bit pages, 32 heads of 128, 109 us,
+// 350 MB (54 us at the rate of a large read): 66 for the shared rows, of which one group of 17 takes two units of 16 rows and
+// reads its own twice (units of 32: 74), 28 for the own ones (100 MB), 8 for the join.
+//
+// Own rows are short and their units many, so a wave takes a run of them by itself: no LDS, no wait for another wave. Eight waves to
+// a unit, joined in LDS and through memory as in the paged attention, took 103 us of what is 32 for the own rows above (with
+// launches of their own), and 30 of 20 for 32 sequences of up to 700 rows. Blocks of 64 keys instead of 128: 20 and 16 us there.
+// The workgroups of the shared rows go on with own rows when they are done (77 to 73 us for 32 sequences behind 32K rows).
 #pragma once
 #include "paged_attn_dev.h"
 
@@ -385,9 +394,13 @@ __global__ __launch_bounds__(paged_waves(RT) * kWave) void k_shared_rows(SharedA
 template <class DT, int D, int FMT>
 hipError_t launch_narrow(const SharedArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.shared.workers);
-  if (a.shared.unit_rows == 16)  // (then a sequence's rows fit 16 too)
-    hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1, 1>), grid, dim3(paged_waves(1) * kWave), 0, st, a);
-  else if (a.own.unit_rows == 16)
+  if constexpr (FMT != MPC_PAGE_SAME) {
+    if (a.shared.unit_rows == 16) {  // (then a sequence's rows fit 16 too)
+      hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 1, 1>), grid, dim3(paged_waves(1) * kWave), 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  if (a.own.unit_rows == 16)
     hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2, 1>), grid, dim3(paged_waves(2) * kWave), 0, st, a);
   else
     hipLaunchKernelGGL((k_shared_rows<DT, D, FMT, 2, 2>), grid, dim3(paged_waves(2) * kWave), 0, st, a);
