@@ -192,8 +192,14 @@ class PagedPath:
         self._pages = [[] for _ in range(batch)]
         self._lent = [0] * batch  # pages at the front of each that belong to another sequence
         self._floor = [0] * batch  # rows that other sequences share, or that are shared with them
-        self._groups = None  # (first, shared_rows, most new tokens of a step, workspace) for mpc_shared_attn
-        self._retired = []  # those of earlier forks, which captured steps may still read: they say that nothing is shared
+        # what mpc_shared_attn takes: how many groups and the most new tokens of a step (None: nothing is shared), and their arrays, the
+        # same ones for every fork, since captured steps read them: to a step of another fork they name other groups, and what it
+        # computes does not depend on which rows are read once
+        self._groups = None
+        n = min(batch, 1024)
+        self._first = torch.zeros(n + 1, dtype=torch.int32, device=self.kv.device)
+        self._shared = torch.zeros(n, dtype=torch.int32, device=self.kv.device)
+        self._shared_ws = []  # the last one is the largest; smaller ones may be a captured step's
         self._free = list(range(n_pages - 1, -1, -1))
         # for steps of any number of tokens (the bytes do not grow beyond 32 query rows to a kv head), and cleared here, so
         # that a step may be captured before one has run
@@ -251,7 +257,9 @@ class PagedPath:
             self._pages[b] = []
         self._lent = [0] * self.kv.B
         self._floor = [0] * self.kv.B
-        self._share(None)
+        if self._groups is not None:
+            self._shared.zero_()
+            self._groups = None
         self.rows = [0] * self.kv.B
         self._kept = [0] * self.kv.B
         self.kv.table.fill_(-1)
@@ -282,8 +290,9 @@ class PagedPath:
         self.pos.add_(n if n_valid is None else n_valid)
         out = torch.zeros_like(q) if out is None else out
         kw = dict(sm_scale=self.sm_scale, window=self.window, sinks=self.sinks, n_valid=n_valid, lse=lse)
-        if self._groups is not None and n <= self._groups[2]:
-            L.mpc_shared_attn(q, self.kv, out, first=self._groups[0], shared_rows=self._groups[1], ws=self._groups[3], **kw)
+        if self._groups is not None and n <= self._groups[1]:
+            ng = self._groups[0]
+            L.mpc_shared_attn(q, self.kv, out, first=self._first[:ng + 1], shared_rows=self._shared[:ng], ws=self._shared_ws[-1], **kw)
         else:
             L.mpc_paged_attn(q, self.kv, out, ws=self.ws, **kw)
         return out
@@ -345,13 +354,6 @@ class PagedPath:
                           sinks=self.sinks, q_lens=n, k_lens=n, lse=lse)
         return out
 
-    def _share(self, groups):
-        """Makes `groups` what steps share; what was shared before says from now on that nothing is."""
-        if self._groups is not None:
-            self._groups[1].zero_()
-            self._retired.append(self._groups)
-        self._groups = groups
-
     def fork(self, first, n_new=1):
         """Groups of neighbours, sequences first[g] <= b < first[g + 1]: each of them goes on from the rows of its group's first one,
         whose whole pages they share from then on (the rows behind these are copied); the others of a group have to be empty. Steps
@@ -373,7 +375,8 @@ class PagedPath:
         if size == 0:
             raise ValueError(f"sizes that the library does not take ({L.lib().mpc_last_error().decode()})")
         shared = [self.rows[a] // page * page for a in first[:-1]]
-        groups = (self._ints(first), self._ints(shared), n_new, L.workspace(size, kv.device))
+        if not self._shared_ws or self._shared_ws[-1].numel() < size:
+            self._shared_ws.append(L.workspace(size, kv.device))
         src, dst = [], []
         for a, b in others:
             whole = self.rows[a] // page
@@ -398,7 +401,10 @@ class PagedPath:
                         t[:, d] = t[:, s]
             M = kv.table.shape[1]
             kv.table.copy_(self._ints([p + [-1] * (M - len(p)) for p in self._pages]))
-        self._share(groups)
+        spare = self._shared.numel() - len(shared)
+        self._first.copy_(self._ints(first + [first[-1]] * spare))
+        self._shared.copy_(self._ints(shared + [0] * spare))
+        self._groups = (len(shared), n_new)
 
     def held(self, n, first=None):
         """(k, v), each [L][B][Hkv][n][d] in the element type: rows first[b] .. first[b] + n - 1 of each sequence as the cache has them

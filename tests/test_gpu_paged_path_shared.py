@@ -132,6 +132,31 @@ def test_pages_are_lent_and_given_back():
     assert not a._free
 
 
+def test_forks_one_after_another_take_no_more_memory():
+    """A server forks for every batch: the arrays of the groups and the workspace are the same ones."""
+    a, b = make("mx4"), make("mx4")
+    seen = set()
+    for i, first in enumerate([[0, 5], [1, 3, 5], [0, 1, 2, 3, 4, 5], [0, 2], [2, 5]]):
+        q, k, v = start(a, 40, first, seed=i)
+        for g, z in zip(first, first[1:]):
+            for t in (q, k, v):
+                t[:, g + 1:z] = t[:, g:g + 1]
+        lens = [40 if first[0] <= s < first[-1] else 0 for s in range(5)]
+        b.prefill(q, k, v, lens)
+        x = inputs(a, 2, "bf16", 50 + i)
+        o = [p.extend(x[0].clone(), x[1], x[2]) for p in (a, b)]
+        assert close(*o, "bf16"), first
+        seen.add((a._first.data_ptr(), a._shared.data_ptr(), len(a._shared_ws), a._shared_ws[-1].data_ptr()))
+        torch.cuda.synchronize()
+        used = torch.cuda.memory_allocated()
+        if i > 2:
+            assert used <= most
+        most = used
+    assert len(seen) <= 2  # (the second fork has more groups: a larger plan)
+    a.clear()
+    assert a._groups is None and not a._shared.any()
+
+
 def test_forks_that_are_refused_change_nothing():
     a = make("e4m3", n_pages=8)
     q, k, v = inputs(a, 70, "bf16", 0)
