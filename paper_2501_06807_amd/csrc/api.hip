@@ -199,6 +199,8 @@ mpc_status check_groups(const mpc_dims* d, int32_t n_new, int32_t n_groups) {
   if (n_groups > mpc::kMaxGroups) return fail(MPC_EUNSUPPORTED, "more than %d groups", mpc::kMaxGroups);
   if ((int64_t)d->batch * n_new * (d->n_q_heads / d->n_kv_heads) > mpc::kMaxRows)
     return fail(MPC_EUNSUPPORTED, "more than 2^30 query rows to a kv head");
+  if ((int64_t)d->n_layers * d->n_q_heads * d->batch * n_new >= (int64_t)1 << 31)
+    return fail(MPC_EUNSUPPORTED, "2^31 query rows or more");
   return MPC_OK;
 }
 

@@ -20,15 +20,15 @@ __global__ __launch_bounds__(kMaxGroups) void k_shared_plan(SharedArgs a) {
 // there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
 template <class DT, int D, bool ALL>
 __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
-  constexpr int PS = D + kPartTail, LANES = D / 4, TEAMS = kJoinThreads / LANES, T = ALL ? TEAMS : 1, AHEAD = 4;
+  constexpr int PS = D + kPartTail, LANES = D / 4, TEAMS = kJoinThreads / LANES, T = ALL ? TEAMS : 1, AHEAD = ALL ? 5 : 4;
   __shared__ float4 s_x[ALL ? TEAMS : 1][LANES];
   __shared__ float2 s_ml[ALL ? TEAMS : 1];
   const PagedCache& c = a.c;
   const int team = threadIdx.x / LANES, e = threadIdx.x % LANES * 4, way = ALL ? team : 0;
   const int per = c.n_new << a.log_g;
-  const long long row = ALL ? (long long)blockIdx.x : (long long)blockIdx.x * TEAMS + team;
-  if (row >= (long long)a.L * a.Hkv * a.B * per) return;
-  const int in_seq = (int)(row % per), lhb = (int)(row / per), b = lhb % a.B, lh = lhb / a.B, t = in_seq >> a.log_g;
+  const unsigned row = ALL ? blockIdx.x : blockIdx.x * TEAMS + team;  // (below 2^31, as the host has checked)
+  if (row >= (unsigned)(a.L * a.Hkv) * (unsigned)a.B * (unsigned)per) return;
+  const int in_seq = row % (unsigned)per, lhb = row / (unsigned)per, b = (unsigned)lhb % (unsigned)a.B, lh = (unsigned)lhb / (unsigned)a.B, t = in_seq >> a.log_g;
   const int valid = c.valid(b);
   if (t >= valid) return;
   const SharedSeq q = a.seq[b];
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
     int n;
   };
   auto side = [&](const Parts& p, unsigned total, unsigned x0, int nb, int in_unit) {
-    Side s{p.head + row * PS, nullptr, 0};
+    Side s{p.head + (size_t)row * PS, nullptr, 0};
     if (nb > 0) {
       const unsigned share = (total + p.workers - 1) / p.workers, w0 = x0 / share, w1 = (x0 + nb - 1) / share;
       s.more = p.more + ((size_t)w0 * p.unit_rows + in_unit) * PS;
@@ -70,7 +70,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
     float4 y[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const float* p = at(min(n0 + k * T, all - 1));
+      if (n0 + k * T >= all) continue;
+      const float* p = at(n0 + k * T);
       ml[k] = *(const float2*)(p + D);
       y[k] = *(const float4*)(p + e);
     }

@@ -27,6 +27,7 @@ def size(d, n, kv, groups):
     (dict(d=dims(batch=2000), groups=1025), L.MPC_EUNSUPPORTED), (dict(cfg=False), L.MPC_EINVAL), (dict(window=-1), L.MPC_EINVAL),
     (dict(sm_scale=float("nan")), L.MPC_EINVAL), (dict(q=None), L.MPC_EINVAL), (dict(out=ODD), L.MPC_EINVAL),
     (dict(os_=L.MpcStrides(2048, 1024, 0, 128)), L.MPC_ESHAPE), (dict(kv=cache(format=2)), L.MPC_EINVAL), (dict(d=dims(head_dim=96)), L.MPC_EUNSUPPORTED),
+    (dict(n=1 << 26, ws_bytes=1 << 62), L.MPC_EUNSUPPORTED),  # 2^31 query rows over two layers, two sequences and eight heads
     (dict(n=1 << 28, ws_bytes=1 << 62), L.MPC_EUNSUPPORTED),  # 2^28 tokens of two sequences of four heads to a kv head
 ])
 def test_calls(kw, expect):
