@@ -15,9 +15,9 @@ __global__ __launch_bounds__(kMaxGroups) void k_shared_plan(SharedArgs a) {
   make_plan<C8, kMaxGroups>(a, tmp, a.group, a.seq, a.total);
 }
 
-// The join: 8.4 us for 1024 rows of 33 parts each, 25 for 54K rows of two or three (110 MB; a wave to a row, statistics before the
-// accumulators: 14 and 59). A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the shared ones; where
-// there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
+// The join: 8.1 us for 1024 rows of 33 parts each, 24 for 54K rows of two or three (110 MB; a wave to a row, statistics before the
+// accumulators: 14 and 59). A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the
+// shared ones; where there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
 template <class DT, int D, bool ALL>
 __global__ __launch_bounds__(kJoinThreads) void k_shared_join(SharedArgs a) {
   constexpr int PS = D + kPartTail, LANES = D / 4, TEAMS = kJoinThreads / LANES, T = ALL ? TEAMS : 1, AHEAD = ALL ? 5 : 4;
