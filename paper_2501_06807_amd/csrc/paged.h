@@ -133,7 +133,7 @@ struct SharedPlan {
   long long blocks;  // the more of both kinds, at most
   size_t total, group, seq, shared_head, shared_more, own_head, own_more, ws_bytes;
 };
-constexpr int kWideGroups = 2;  // groups of four waves, which divide the keys, of a workgroup whose units have 128 query rows
+constexpr int kWideWaves = 4;  // of a workgroup whose units have 128 query rows, two of which a compute unit has room for
 SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups);
 hipError_t launch_shared_fp32(const SharedArgs& a, int D, hipStream_t st);
 hipError_t launch_shared_fp16(const SharedArgs& a, int D, hipStream_t st);

@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kMaxGroups) void k_shared_plan(SharedArgs a) {
   make_plan<C8, kMaxGroups>(a, tmp, a.group, a.seq, a.total);
 }
 
-// The join: 8.1 us for 1024 rows of 33 parts each, 24 for 54K rows of two or three (110 MB; a wave to a row, statistics before the
+// The join: 10.6 us for 1024 rows of 66 parts each (33: 8.1), 24 for 54K rows of two or three (110 MB; a wave to a row, statistics before the
 // accumulators: 14 and 59). A team of lanes, 16 bytes to each, has a query row, whose parts are those of its own rows and of the
 // shared ones; where there are few rows, ALL teams of a workgroup have one row and every T-th part of it each.
 template <class DT, int D, bool ALL>
@@ -147,7 +147,7 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 // 39 and 37, 8-bit codes 40 and 36, 4-bit codes 37 and 33 (fp16 39 and 40), 96 rows 54 and 42; 32 rows 32 and 37, 32 and 34, 30 and 32.
 // 16 rows in units of 16 and of 32: bf16 34 and 30, fp32 50 and 51 (1K shared rows: 38 and 30), 8-bit codes 28 and 30, 4-bit codes
 // 25 and 28. Own rows in units of 16 where a sequence's rows fit, or beside the wide units, else of 32. Blocks are a tile to each
-// wave of a workgroup (wide units: four tiles to each group of waves), and 64 keys of the own rows, which are taken by the waves
+// wave of a workgroup (wide units: four tiles), and 64 keys of the own rows, which are taken by the waves
 // of the kernel that takes the shared ones.
 SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
   SharedPlan p{};
@@ -156,10 +156,10 @@ SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int H
   p.shared_rows = p.wide ? 128 : each <= 16 && format != MPC_PAGE_SAME ? 16 : 32;
   p.own_rows = each_seq <= 16 || p.wide ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
-  p.shared_block = p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16);
+  p.shared_block = p.wide ? 4 : paged_waves(p.shared_rows / 16);
   p.own_block = 64 / p.tile;
-  p.shared_workers = kNumCU;
-  p.own_workers = kNumCU * (p.wide ? 4 * kWideGroups : paged_waves(p.shared_rows / 16));
+  p.shared_workers = p.wide ? 2 * kNumCU : kNumCU;
+  p.own_workers = kNumCU * (p.wide ? 8 : paged_waves(p.shared_rows / 16));
   auto blocks = [&](long long units, long long block) {
     const double nb = cap / (p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short
     return (double)units * nb >= 2147483648.0 ? 1ll << 31 : units * (long long)nb;
@@ -172,7 +172,7 @@ SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int H
   p.seq = p.group + align256((size_t)groups * sizeof(SharedGroup));
   p.shared_head = p.seq + align256((size_t)B * sizeof(SharedSeq));
   // as many places for the workers' parts as any form has, so that a workspace made for the most tokens serves calls of fewer
-  const size_t most_shared = (size_t)kNumCU * (dtype == MPC_FP32 ? 32 : 128), most_own = (size_t)kNumCU * 128;
+  const size_t most_shared = (size_t)kNumCU * (dtype == MPC_FP32 ? 32 : 256), most_own = (size_t)kNumCU * 128;
   p.shared_more = p.shared_head + heads;
   p.own_head = p.shared_more + align256(most_shared * row);
   p.own_more = p.own_head + heads;

@@ -3,7 +3,7 @@
 // A group's query rows (all its sequences' tokens and the G heads of a kv head) are one unit's rows as far as they fit, so K and
 // V of the shared rows are read once for a unit instead of once for a sequence; a softmax over both kinds of rows is the join of
 // its parts over each, o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p with m = max_p m_p. The tiles' work is the paged
-// attention's. Reading the keys bounds it: 64 sequences in four groups behind 8K rows of 8-bit pages, 32 heads of 128, 109 us,
+// attention's. Reading the keys bounds it: 64 sequences in four groups behind 8K rows of 8-bit pages, 32 heads of 128, 108 us,
 // 350 MB (54 us at the rate of a large read): 66 for the shared rows, of which one group of 17 takes two units of 16 rows and
 // reads its own twice (units of 32: 74), 28 for the own ones (100 MB), 8 for the join.
 //

@@ -9,7 +9,7 @@ template <class DT, int D, int FMT>
 hipError_t launch_shared_d(const SharedArgs& a, hipStream_t st) {
   if constexpr (DT::kElt == 2) {
     if (a.wide) {
-      hipLaunchKernelGGL((k_shared_wide<DT, D, FMT>), dim3((unsigned)a.shared.workers), dim3(256 * kWideGroups), 0, st, a);
+      hipLaunchKernelGGL((k_shared_wide<DT, D, FMT>), dim3((unsigned)a.shared.workers), dim3(kWideWaves * kWave), 0, st, a);
       return hipGetLastError();
     }
   }

@@ -1,30 +1,56 @@
 // Attention behind shared rows, 16-bit types: the kernel of the shared rows for units of 128 query rows, and own rows after them.
 //
-// A workgroup has NS groups of four waves, a wave 32 of the unit's rows; the groups take every NS-th tile of 32 keys. A tile goes
-// through LDS once for the four waves, double-buffered, the next one in registers meanwhile; codes become 16-bit values on the
-// way. S^T = K Q^T and O^T += V^T P^T are 32x32x16 products, as in the prompt attention: a lane has 16 scores of one row for
-// each 32 keys, and its weights, packed, are the next product's operand; V comes from LDS through the transposing reads.
+// A workgroup has four waves, a wave 32 of the unit's rows; a tile of 32 keys goes through LDS once for them: rows of the element type
+// straight from memory, two tiles ahead of the one that is worked on, codes a tile ahead in registers, which become 16-bit
+// values on the way. S^T = K Q^T and O^T += V^T P^T are 32x32x16 products, as in the prompt attention: a lane has 16 scores of
+// one row for each 32 keys, and its weights, packed, are the next product's operand; V comes from LDS through the transposing
+// reads. Two workgroups to a compute unit, which wait for each other nowhere: one of eight waves, in two groups that divide the
+// keys, has all of them read, multiply and take exponentials at the same time (616, 114 and 69 us of the cases below's 603, 111 and 68).
 // A row's reference moves only when a score passes it by 2^8. Weights are rounded once to the type; over codes fp16 takes them
 // in two bf16 parts, since values times page or block scales have no place in fp16's range.
 //
-// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 614 us
-// all in all, 740 TFLOP/s (a large product of the library: 1078). The matrix unit is busy 32% of the cycles, the vector unit 34%, and a
-// third of the waves' time is waiting for one of them; 94% of the reads hit the L2. On the way there: masks and values that are
-// not finite in a loop of their own (spills: 1341 to 871 us), page ids and offsets in registers of a window of 64 halves instead
+// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 603 us
+// all in all, 753 TFLOP/s (a large product of the library: 1078). The matrix unit is busy a third of the cycles, the vector unit
+// another; 94% of the reads hit the L2. On the way there: masks and values that are not finite in a loop of their own (spills:
+// 1341 to 871 us), page ids and offsets in registers of a window of 64 halves instead
 // of scalar loads and 64-bit products (871 to 729, 646 to 614), rows of shorter prompts not padded (726 to 678), runs from
 // their end on (677 to 646; before it 93% of the reads missed the L2). Not kept: units of 256 rows (691 of 678), tiles
-// straight to LDS in rounds of two (765), priority to the matrix operations (616 of 614).
-// 32 sequences behind 32K rows of bf16 pages, 128 query rows to each of 8 kv heads: 69 us, 182 MB (28 us at the rate of a large
-// read), 36 of them for the shared rows at 3.7 TB/s, 15 for the own ones, 8 for the join of 32 parts to a row and 5 between them.
-// 192 query rows to each of 8 heads behind 20K rows of 4-bit pages (63 GFLOP): 114 us, 107 for the shared rows, whose codes are
-// widened once for 128 query rows.
+// straight to LDS in rounds of two (765), priority to the matrix operations (616 of 614), all in workgroups of eight waves. Tiles
+// straight to LDS instead of through registers: no time here, 52 to 50 us of the next case's first launch.
+// 32 sequences behind 32K rows of bf16 pages, 128 query rows to each of 8 kv heads: 68 us, 182 MB (28 us at the rate of a large
+// read), 50 of them for the shared and the own rows, 10 for the join of 65 parts to a row, and what lies between.
+// 192 query rows to each of 8 heads behind 20K rows of 4-bit pages (63 GFLOP): 111 us, most of it for the shared rows, whose
+// codes are widened once for 128 query rows.
 #pragma once
 #include "shared_attn_dev.h"
 
 namespace mpc {
 namespace dev {
 
-template <class DT, int D, int FMT, int NS>
+// 16 bytes from p + off to the lane's place behind `at` (p and `at` the same over the wave), without a register between.
+__device__ __forceinline__ void load_to_lds(const char* p, int off, uint4* at) {
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)at);
+  uint32_t was;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(was)
+      : "s"(lds), "v"(off), "s"(p)
+      : "memory");
+}
+// Waits for a wave's loads but the last N (`some`) or for all of them, and for its LDS operations, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void wait_loads(bool some) {
+  if (some)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <class DT, int D, int FMT>
 __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& plan) {
   constexpr bool C8 = FMT == MPC_PAGE_E4M3, C4 = FMT == MPC_PAGE_MX4, CODES = C8 || C4;
   constexpr bool H = DT::kCode == MPC_FP16, SPLIT = C4 && H, TWO = CODES && H;
@@ -36,13 +62,14 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
   constexpr int PER = CODES ? 1 : KT * CH / THREADS;         // pieces of K (and of V) that a thread stages
   constexpr int PCH = CODES ? D / 8 : 8;                     // channels of a piece
   constexpr int RB = C4 ? D / 2 : C8 ? D : 2 * D;            // bytes of a page's row
-  __shared__ uint4 s_k[NS][2][KT * CH], s_v[NS][2][KT * CH];
-  __shared__ int s_bad[NS][2];     // the last round whose values, staged for an edge, were not all finite
+  // Codes: a tile in registers and two in LDS; others go straight to LDS, two tiles ahead of the one that is worked on.
+  constexpr int NB = CODES ? 2 : 3;
+  __shared__ uint4 s_k[NB][KT * CH], s_v[NB][KT * CH];
+  __shared__ int s_bad[NB];        // codes: the last round whose values, staged for an edge, were not all finite
   __shared__ uint4 s_q2[SPLIT ? 4 : 1][KSTEPS][SPLIT ? kWave : 1];  // second parts of the queries (registers do not hold them)
   __shared__ int s_range[4][2];    // positions of the waves' rows
   const PagedCache& c = a.c;
-  const int tid = threadIdx.x % THREADS, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
-  const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  const int tid = threadIdx.x, lane = tid % kWave, q32 = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
 
   const unsigned total = plan.shared, id = by_die(blockIdx.x, gridDim.x);
@@ -82,11 +109,11 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
-    if (lane == 0 && grp == 0) {
+    if (lane == 0) {
       s_range[wave][0] = lo;
       s_range[wave][1] = hi;
     }
-    if (threadIdx.x < 2 * NS) (&s_bad[0][0])[threadIdx.x] = -1;
+    if (tid < NB) s_bad[tid] = -1;
     uint4 q[KSTEPS];
     {
       const int t = row.in_seq >> a.log_g, hq = (h << a.log_g) + row.in_seq - (t << a.log_g);
@@ -98,7 +125,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
         if constexpr (SPLIT) {
           uint4 rest;
           split_bf16(q[i], rest);
-          if (grp == 0) s_q2[wave][i][lane] = rest;
+          s_q2[wave][i][lane] = rest;
         }
       }
     }
@@ -156,13 +183,16 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
         w_vs = c.vs[page0 + (size_t)max(id, 0) * c.Hkv];
       }
     };
-    uint4 kr[PER], vr[PER];
+    uint4 kr[CODES ? PER : 1], vr[CODES ? PER : 1];
     uint32_t kx = 0, vx = 0;                       // 4-bit codes: the piece's scale bytes
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};  // 8-bit codes: the halves' page scales
-    const int lane_row = CODES ? (tid / 8 & 15) * RB + tid % 8 * (RB / 8) : (tid / CH & 15) * RB + tid % CH * 16;
+    const int lane_row = (tid / 8 & 15) * RB + tid % 8 * (RB / 8);
+    // a lane's place in LDS is fixed: which chunk of the row it asks for puts it where the exchange within the row wants it
+    const int k_lane = (tid / CH & 15) * RB + tile_chunk_k<D>(tid / CH, tid % CH) % CH * 16;
+    const int v_lane = (tid / CH & 15) * RB + tile_chunk_v<D>(tid / CH, tid % CH) % CH * 16;
     int k_at = 0;         // the fetched tile's first key
     unsigned has_at = 0;  // and whether its halves have a page
-    auto fetch = [&](int k0) {
+    auto fetch = [&](int k0, int buf) {
       int i = (k0 >> 4) - win;
       if ((unsigned)i >= kWave - 1) {
         load_window(k0 >> 4);
@@ -204,9 +234,14 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       } else {
 #pragma unroll
         for (int n = 0; n < PER; ++n) {  // (a half to each n, or to each pair of waves)
-          const size_t from = (PER == 2 ? n == 1 : wave >= 2) ? at[1] : at[0];
-          kr[n] = ldg16(k_page + from + lane_row);
-          vr[n] = ldg16(v_page + from + lane_row);
+          const bool second = PER == 2 ? n == 1 : wave >= 2;
+          const size_t from = second ? at[1] : at[0];
+          const int y = wave * kWave + n * THREADS;
+          load_to_lds(k_page + from, k_lane, s_k[buf] + y);
+          if (has_at >> (second ? 1 : 0) & 1)
+            load_to_lds(v_page + from, v_lane, s_v[buf] + y);
+          else  // values that have no page must not be anything
+            s_v[buf][y + lane] = make_uint4(0, 0, 0, 0);
         }
       }
     };
@@ -220,7 +255,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
         return make_uint4(widen2<T, false>(w0), widen2<T, true>(w0), widen2<T, false>(w1), widen2<T, true>(w1));
       }
     };
-    // Stages the fetched tile, with zeros for values that have no page; whether it held values that are not finite (edge).
+    // Codes: stages the fetched tile, with zeros for values that have no page; whether it held values that are not finite (edge).
     auto stash = [&](auto edge_, int buf, const bool* have) {
       constexpr bool edge = decltype(edge_)::value;
       uint32_t top = 0;
@@ -233,17 +268,8 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
           uint4 y = widened(PV{}, vr[0], n, vx);
           if (!(wave >= 2 ? have[1] : have[0])) y = make_uint4(0, 0, 0, 0);
           if (edge) seen(y);
-          s_k[grp][buf][tile_chunk_k<D>(r, chunk)] = widened(QT{}, kr[0], n, kx);
-          s_v[grp][buf][tile_chunk_v<D>(r, chunk)] = y;
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < PER; ++n) {
-          const int y = tid + n * THREADS;
-          if (!((PER == 2 ? n == 1 : wave >= 2) ? have[1] : have[0])) vr[n] = make_uint4(0, 0, 0, 0);
-          if (edge) seen(vr[n]);
-          s_k[grp][buf][tile_chunk_k<D>(y / CH, y % CH)] = kr[n];
-          s_v[grp][buf][tile_chunk_v<D>(y / CH, y % CH)] = vr[n];
+          s_k[buf][tile_chunk_k<D>(r, chunk)] = widened(QT{}, kr[0], n, kx);
+          s_v[buf][tile_chunk_v<D>(r, chunk)] = y;
         }
       }
       return not_finite<PV>(top);
@@ -251,12 +277,12 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
     // The tile of round n at key k0; EDGE: some row of the wave may not see some key of it.
     auto tile = [&](auto edge, int k0, int buf, int n, const bool* have, const float* kss, const float* vss) {
       constexpr bool EDGE = decltype(edge)::value;
-      const uint4* sk = s_k[grp][buf];
-      const char* sv = (const char*)s_v[grp][buf];
+      const uint4* sk = s_k[buf];
+      const char* sv = (const char*)s_v[buf];
       // places 0..3 and 4..7 of half hl in a product over 16 keys are keys 4 hl .. and 8 + 4 hl ..
       const int vrow = 4 * hl + ((lane & 15) >> 2);  // row whose piece this lane asks for, and the piece's 16-byte chunk
       const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
-      const int bad = EDGE ? s_bad[grp][buf] : 0;
+      bool bad = EDGE && CODES && __builtin_amdgcn_readfirstlane(s_bad[buf]) == n;
       uint4 kf[KSTEPS];
 #pragma unroll
       for (int i = 0; i < KSTEPS; ++i) kf[i] = sk[tile_chunk_k<D>(q32, 2 * i + hl)];
@@ -334,6 +360,12 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
         p[r / 2] = pack2<PV>(w0, w1);
         if constexpr (TWO) p2[r / 2] = pack2<PV>(w0 - bf16_to_f32(p[r / 2] & 0xFFFFu), w1 - bf16_to_f32(p[r / 2] >> 16));
       }
+      if constexpr (EDGE && !CODES) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 8 * DB; ++i) most = max_magnitude(most, vf[i / (4 * DB)][i / 4 % DB][i % 4]);
+        bad = __any(not_finite<PV>(most));
+      }
       // O^T += V^T P^T, 16 keys at a time
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
@@ -342,7 +374,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
         if constexpr (EDGE) {
           // Values that are not finite, in keys that some row does not see, must not meet that row's weight of zero: they are
           // added apart, to the rows that see them
-          if (__builtin_amdgcn_readfirstlane(bad) == n) {
+          if (bad) {
             float one[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) one[e] = sees(j0 + 16 * st + (e >= 4 ? 8 : 0) + (e & 3)) ? 1.f : 0.f;
@@ -370,71 +402,49 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       }
     };
 
-    const int tiles = i1 - i0, rounds = (tiles + NS - 1) / NS, edge_rounds = (edges + NS - 1) / NS;
-    if (grp < tiles) {
-      fetch(key0(grp));
+    const int tiles = i1 - i0;
+    int place = 0, k_next = 0;  // straight to LDS: the tile's place there, and the tile that is on its way behind it
+    unsigned has_next = 0;
+    fetch(key0(0), 0);
+    int k_now = k_at;
+    unsigned has_now = has_at;
+    if (!CODES && tiles > 1) {
+      fetch(key0(1), 1);
+      k_next = k_at;
+      has_next = has_at;
     }
     auto round = [&](auto edge, int n) {
       constexpr bool EDGE = decltype(edge)::value;
-      const int j = n * NS + grp, buf = n & 1;
-      const int k0 = k_at;
-      const bool have[2] = {(has_at & 1) != 0, (has_at & 2) != 0};
+      const int ahead = n + NB - 1, k0 = k_now, buf = CODES ? n & 1 : place;
+      const bool have[2] = {(has_now & 1) != 0, (has_now & 2) != 0};
       const float kss[2] = {ks[0], ks[1]}, vss[2] = {vs[0], vs[1]};
-      if (j < tiles && stash(edge, buf, have) && EDGE) s_bad[grp][buf] = n;
-      __syncthreads();
-      if (j + NS < tiles) {
-        int next = k0 + NS * KT;
+      if constexpr (CODES) {
+        if (stash(edge, buf, have) && EDGE) s_bad[buf] = n;
+        __syncthreads();
+      } else {
+        // this tile's loads have arrived when no more than the next one's are on their way (fewer than 2 PER where it has zeros)
+        wait_loads<2 * PER>(n + 1 < tiles && has_next == 3);
+        k_now = k_next;
+        has_now = has_next;
+      }
+      if (ahead < tiles) {
+        int next = (CODES ? k0 : k_next) + KT;
         if (EDGE)
-          next = key0(j + NS);
+          next = key0(ahead);
         else if (next >= whole_end)
           next -= n_whole * KT;
-        fetch(next);
+        fetch(next, buf == 0 ? NB - 1 : buf - 1);  // (where the tile before this one was)
+        (CODES ? k_now : k_next) = k_at;
+        (CODES ? has_now : has_next) = has_at;
       }
-      if (j < tiles && lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
+      if (lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
+      if (!CODES) place = buf == NB - 1 ? 0 : buf + 1;
     };
-    for (int n = 0; n < edge_rounds; ++n) round(std::true_type{}, n);
-    for (int n = edge_rounds; n < rounds; ++n) round(std::false_type{}, n);
+    for (int n = 0; n < edges; ++n) round(std::true_type{}, n);
+    for (int n = edges; n < tiles; ++n) round(std::false_type{}, n);
 
     sum = xor_combine<32>(sum, [](float p, float q) { return p + q; });
-    if constexpr (NS == 2) {
-      // the second group's part to the first, through the tiles' LDS
-      constexpr int HALF = DB / 2;
-      float* s_o = (float*)&s_k[0][0][0];  // [4 waves][HALF * 16][64 lanes] each for a half of the channels
-      float* s_st = (float*)&s_v[0][0][0];
-      const float mine = ref;
-      __syncthreads();
-      if (grp == 1) {
-        s_st[(wave * 2) * kWave + lane] = ref;
-        s_st[(wave * 2 + 1) * kWave + lane] = sum;
-      }
-      __syncthreads();
-      float p0 = 1.f, p1 = 0.f;
-      if (grp == 0) {
-        const float r1 = s_st[(wave * 2) * kWave + lane], sum1 = s_st[(wave * 2 + 1) * kWave + lane];
-        ref = fmaxf(mine, r1);
-        const float b0 = ref == -INFINITY ? 0.f : ref;
-        p0 = fast_exp2(mine - b0);
-        p1 = fast_exp2(r1 - b0);
-        sum = sum * p0 + sum1 * p1;
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        __syncthreads();
-        if (grp == 1)
-#pragma unroll
-          for (int d = 0; d < HALF; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s_o[((wave * HALF + d) * 16 + r) * kWave + lane] = o[e * HALF + d][r];
-        __syncthreads();
-        if (grp == 0)
-#pragma unroll
-          for (int d = 0; d < HALF; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              o[e * HALF + d][r] = o[e * HALF + d][r] * p0 + s_o[((wave * HALF + d) * 16 + r) * kWave + lane] * p1;
-      }
-    }
-    if (grp == 0 && row.live) {
+    if (row.live) {
       float* part = blk == 0 ? a.shared.head + part_row(a, lh, row.b, row.in_seq) * PS : a.shared.more + ((size_t)id * 128 + 32 * wave + q32) * PS;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -447,14 +457,14 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
   }
 }
 
-// Shared rows, then own ones, in units of 16 query rows (units of 32, in a launch of their own for want of registers, take as long:
-// 616 us of eight prompts' 614).
+// Shared rows, then own ones, in units of 16 query rows (units of 32, in a launch of their own for want of registers, took as long:
+// 616 us of what then was 614 for the eight prompts).
 template <class DT, int D, int FMT>
-__global__ __launch_bounds__(256 * kWideGroups, 2) void k_shared_wide(SharedArgs a) {
+__global__ __launch_bounds__(kWideWaves * kWave, 2) void k_shared_wide(SharedArgs a) {
   __shared__ PlanSpace space;
   const Plan plan = plan_of<FMT == MPC_PAGE_E4M3>(a, space);
-  shared_wide<DT, D, FMT, kWideGroups>(a, plan);
-  own_rows_of<DT, D, FMT, 1, 4 * kWideGroups>(a, plan);
+  shared_wide<DT, D, FMT>(a, plan);
+  own_rows_of<DT, D, FMT, 1, kWideWaves>(a, plan);
 }
 
 }  // namespace dev
