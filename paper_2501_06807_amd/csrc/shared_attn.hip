@@ -144,7 +144,8 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 
 // Shared rows in units of 128 query rows where a group has more than 32 on average (16-bit types), else of 32, or of 16 over codes
 // where that is enough. Measured, 16K shared rows of 8 kv heads of 128, us: 40 query rows to a kv head in units of 32 and of 128, bf16
-// 39 and 37, 8-bit codes 40 and 36, 4-bit codes 37 and 33 (fp16 39 and 40), 96 rows 54 and 42; 32 rows 32 and 37, 32 and 34, 30 and 32.
+// 38 and 35, 8-bit codes 39 and 33, 4-bit codes 37 and 32 (fp16 38 and 37), 96 rows 54 and 41; 32 rows 32 and 30, 32 and 29, 30 and 29
+// (fp16 31 and 32), but 24 and 30 for 40 rows behind 1K shared ones, and nothing gained by fewer tiles to a block.
 // 16 rows in units of 16 and of 32: bf16 34 and 30, fp32 50 and 51 (1K shared rows: 38 and 30), 8-bit codes 28 and 30, 4-bit codes
 // 25 and 28. Own rows in units of 16 where a sequence's rows fit, or beside the wide units, else of 32. Blocks are a tile to each
 // wave of a workgroup (wide units: four tiles), and 64 keys of the own rows, which are taken by the waves
