@@ -5,20 +5,21 @@
 // values on the way. S^T = K Q^T and O^T += V^T P^T are 32x32x16 products, as in the prompt attention: a lane has 16 scores of
 // one row for each 32 keys, and its weights, packed, are the next product's operand; V comes from LDS through the transposing
 // reads. Two workgroups to a compute unit, which wait for each other nowhere: one of eight waves, in two groups that divide the
-// keys, has all of them read, multiply and take exponentials at the same time (616, 114 and 69 us of the cases below's 603, 111 and 68).
+// keys and join in LDS, took 114 us of the last case's 109 below in turn on one card, and as long in the other two.
 // A row's reference moves only when a score passes it by 2^8. Weights are rounded once to the type; over codes fp16 takes them
 // in two bf16 parts, since values times page or block scales have no place in fp16's range.
 //
-// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 603 us
-// all in all, 753 TFLOP/s (a large product of the library: 1078). The matrix unit is busy a third of the cycles, the vector unit
+// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 603 to
+// 622 us on different cards, up to 753 TFLOP/s (a large product of the library: 1078). The matrix unit is busy a third of the cycles, the vector unit
 // another; 94% of the reads hit the L2. On the way there: masks and values that are not finite in a loop of their own (spills:
 // 1341 to 871 us), page ids and offsets in registers of a window of 64 halves instead
 // of scalar loads and 64-bit products (871 to 729, 646 to 614), rows of shorter prompts not padded (726 to 678), runs from
 // their end on (677 to 646; before it 93% of the reads missed the L2). Not kept: units of 256 rows (691 of 678), tiles
-// straight to LDS in rounds of two (765), priority to the matrix operations (616 of 614), all in workgroups of eight waves. Tiles
-// straight to LDS instead of through registers: no time here, 52 to 50 us of the next case's first launch.
+// straight to LDS in rounds of two (765), priority to the matrix operations (616 of 614), all in workgroups of eight waves; the
+// next tile's scores beside this one's weights (681 of 664 under the profiler). Tiles straight to LDS instead of through
+// registers: no time here, 52 to 50 us of the next case's first launch.
 // 32 sequences behind 32K rows of bf16 pages, 128 query rows to each of 8 kv heads: 68 us, 182 MB (28 us at the rate of a large
-// read), 50 of them for the shared and the own rows, 10 for the join of 65 parts to a row, and what lies between.
+// read), 50 of them for the shared and the own rows, 10 for the join of 66 parts to a row, and what lies between.
 // 192 query rows to each of 8 heads behind 20K rows of 4-bit pages (63 GFLOP): 111 us, most of it for the shared rows, whose
 // codes are widened once for 128 query rows.
 #pragma once
