@@ -356,8 +356,9 @@ class PagedPath:
 
     def fork(self, first, n_new=1):
         """Groups of neighbours, sequences first[g] <= b < first[g + 1]: each of them goes on from the rows of its group's first one,
-        whose whole pages they share from then on (the rows behind these are copied); the others of a group have to be empty. Steps
-        of up to n_new tokens read the shared rows once for a group (mpc_shared_attn), longer ones once for each sequence."""
+        whose whole pages they share from then on (the rows behind these are copied); the others of a group have to be empty. A
+        sequence alone in its group shares nothing, as one outside all groups. Steps of up to n_new tokens read the shared rows once
+        for a group (mpc_shared_attn), longer ones once for each sequence."""
         kv, page = self.kv, self.kv.page
         first, n_new = [operator.index(b) for b in first], operator.index(n_new)
         if not 2 <= len(first) <= 1025 or first[0] < 0 or first[-1] > kv.B or any(x >= y for x, y in zip(first, first[1:])) or n_new < 1:
@@ -374,7 +375,9 @@ class PagedPath:
         size = L.shared_attn_workspace_bytes(shape, kv, len(first) - 1)
         if size == 0:
             raise ValueError(f"sizes that the library does not take ({L.lib().mpc_last_error().decode()})")
-        shared = [self.rows[a] // page * page for a in first[:-1]]
+        # (a sequence alone in its group shares nothing: its rows may be taken back, and 8-bit pages that end up incomplete must
+        # not be read as shared ones)
+        shared = [self.rows[a] // page * page if z > a + 1 else 0 for a, z in zip(first, first[1:])]
         if not self._shared_ws or self._shared_ws[-1].numel() < size:
             self._shared_ws.append(L.workspace(size, kv.device))
         src, dst = [], []
