@@ -66,7 +66,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
   // Codes: a tile in registers and two in LDS; others go straight to LDS, two tiles ahead of the one that is worked on.
   constexpr int NB = CODES ? 2 : 3;
   __shared__ uint4 s_k[NB][KT * CH], s_v[NB][KT * CH];
-  __shared__ int s_bad[NB];        // codes: the last round whose values, staged for an edge, were not all finite
+  __shared__ int s_bad[NB];        // codes: the last round whose values, staged for an edge, were not all finite; else [0]: the run is taken again
   __shared__ uint4 s_q2[SPLIT ? 4 : 1][KSTEPS][SPLIT ? kWave : 1];  // second parts of the queries (registers do not hold them)
   __shared__ int s_range[4][2];    // positions of the waves' rows
   const PagedCache& c = a.c;
@@ -131,11 +131,7 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       }
     }
     f32x16 o[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    float ref = -INFINITY, sum = 0.f;  // reference (in units of the exponent) and sum over this lane's keys
+    float ref, sum;  // reference (in units of the exponent) and sum over this lane's keys
     __syncthreads();
     int g_lo = kMaxRows, g_hi = -kMaxRows;
 #pragma unroll
@@ -404,16 +400,8 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
     };
 
     const int tiles = i1 - i0;
-    int place = 0, k_next = 0;  // straight to LDS: the tile's place there, and the tile that is on its way behind it
-    unsigned has_next = 0;
-    fetch(key0(0), 0);
-    int k_now = k_at;
-    unsigned has_now = has_at;
-    if (!CODES && tiles > 1) {
-      fetch(key0(1), 1);
-      k_next = k_at;
-      has_next = has_at;
-    }
+    int place, k_next = 0, k_now;  // straight to LDS: the tile's place there, and the tile that is on its way behind it
+    unsigned has_next = 0, has_now;
     auto round = [&](auto edge, int n) {
       constexpr bool EDGE = decltype(edge)::value;
       const int ahead = n + NB - 1, k0 = k_now, buf = CODES ? n & 1 : place;
@@ -441,10 +429,41 @@ __device__ __forceinline__ void shared_wide(const SharedArgs& a, const Plan& pla
       if (lo <= hi) tile(edge, k0, buf, n, have, kss, vss);
       if (!CODES) place = buf == NB - 1 ? 0 : buf + 1;
     };
-    for (int n = 0; n < edges; ++n) round(std::true_type{}, n);
-    for (int n = edges; n < tiles; ++n) round(std::false_type{}, n);
+    // Whole tiles multiply every value with every weight. An infinity times a weight that is zero in its type would be NaN: where an
+    // accumulator ends up not finite beside a finite sum, the run is taken once more with every tile as an edge (a check of
+    // every tile's values would cost all of them). Codes hold no infinities, and a NaN needs no sign.
+    int n_edge = edges;
+    for (;;) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+      ref = -INFINITY;
+      sum = 0.f;
+      place = 0;
+      fetch(key0(0), 0);
+      k_now = k_at;
+      has_now = has_at;
+      if (!CODES && tiles > 1) {
+        fetch(key0(1), 1);
+        k_next = k_at;
+        has_next = has_at;
+      }
+      for (int n = 0; n < n_edge; ++n) round(std::true_type{}, n);
+      for (int n = n_edge; n < tiles; ++n) round(std::false_type{}, n);
+      sum = xor_combine<32>(sum, [](float p, float q) { return p + q; });
+      if (CODES || n_edge == tiles) break;
+      float zero = 0.f;  // NaN where an accumulator is not finite
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = fmaf(o[d][r], 0.f, zero);
+      if (row.live && zero != 0.f && sum * 0.f == 0.f) s_bad[0] = 0;
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(s_bad[0]) != 0) break;
+      n_edge = tiles;
+    }
 
-    sum = xor_combine<32>(sum, [](float p, float q) { return p + q; });
     if (row.live) {
       float* part = blk == 0 ? a.shared.head + part_row(a, lh, row.b, row.in_seq) * PS : a.shared.more + ((size_t)id * 128 + 32 * wave + q32) * PS;
 #pragma unroll
