@@ -60,6 +60,14 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2_t));
 }
 
+template <class DT>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (DT::kCode == MPC_BF16)
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  else
+    return make_float2(f16_to_f32(w & 0xFFFFu), f16_to_f32(w >> 16));
+}
+
 // fp16 values as the sum of two bf16 ones, 8 places and the 3 that they leave (exact; what is not finite is in the first).
 __device__ __forceinline__ void split_bf16(uint4& x, uint4& rest) {
   float f[8], hi[8];
