@@ -446,7 +446,7 @@ typedef struct {
  * call leaves it ready for the next, of this or any other sizes whose bytes it has, and for mpc_paged_attn (calls sharing
  * it must not overlap). The bytes never fall with n_new, batch, n_layers, the heads or n_groups. The sizes, not the lengths or the groups' contents, give the launches, so a captured call follows
  * lengths, tables and groups as they change.
- * Limits: those of mpc_paged_attn, B * n_new * G <= 2^30, L * B * Hq * n_new < 2^31. */
+ * Limits: those of mpc_paged_attn, B * n_new * G <= 2^30, L * B * Hq * n_new < 2^31, L * Hkv * n_groups < 2^29. */
 mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                            const mpc_shared* shared, const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides,
                            void* out, const mpc_strides* out_strides, float* lse, void* ws, size_t ws_bytes, void* stream);

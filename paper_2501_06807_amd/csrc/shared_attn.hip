@@ -149,7 +149,7 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 // 16 rows in units of 16 and of 32: bf16 34 and 30, fp32 50 and 51 (1K shared rows: 38 and 30), 8-bit codes 28 and 30, 4-bit codes
 // 25 and 28. Own rows in units of 16 where a sequence's rows fit, or beside the wide units, else of 32. Blocks are a tile to each
 // wave of a workgroup (wide units: four tiles), and 64 keys of the own rows, which are taken by the waves
-// of the kernel that takes the shared ones.
+// of the kernel that takes the shared ones (more where the table has room for 2^31 such blocks).
 SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
   SharedPlan p{};
   const long long each_seq = (long long)n * (Hq / Hkv), rows = B * each_seq, each = (rows + groups - 1) / groups, lh = (long long)L * Hkv;
@@ -161,12 +161,18 @@ SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int H
   p.own_block = 64 / p.tile;
   p.shared_workers = p.wide ? 2 * kNumCU : kNumCU;
   p.own_workers = kNumCU * (p.wide ? 8 : paged_waves(p.shared_rows / 16));
-  auto blocks = [&](long long units, long long block) {
-    const double nb = cap / (p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short
-    return (double)units * nb >= 2147483648.0 ? 1ll << 31 : units * (long long)nb;
+  const PagedPlan unshared = paged_plan(dtype, D, L, B, Hq, Hkv, n, cap);
+  // Fewer than 2^31 blocks: what the paged attention takes (fewer of them, of 256 keys) is taken here too, in blocks as much larger
+  auto blocks = [&](long long units, int& block) {
+    for (;; block *= 2) {
+      const long long nb = cap / ((long long)p.tile * block) + 2;  // complete pages' tiles and the ring's may each be cut short
+      if ((double)units * (double)nb < 2147483648.0) return units * nb;
+      if (nb == 2 || unshared.blocks >= 1ll << 31) return 1ll << 31;
+    }
   };
   p.blocks = std::max(blocks((rows / p.shared_rows + groups) * lh, p.shared_block),
                       blocks(B * ((each_seq + p.own_rows - 1) / p.own_rows) * lh, p.own_block));
+  if (unshared.blocks >= 1ll << 31) p.blocks = unshared.blocks;
   const size_t row = (D + kPartTail) * sizeof(float), heads = align256((size_t)lh * rows * row);
   p.total = kPagedCntBytes;  // behind the counters of the paged attention, which a workspace of this serves too
   p.group = p.total + align256(sizeof(SharedTotals));
@@ -177,7 +183,7 @@ SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int H
   p.shared_more = p.shared_head + heads;
   p.own_head = p.shared_more + align256(most_shared * row);
   p.own_more = p.own_head + heads;
-  p.ws_bytes = std::max(p.own_more + most_own * row, paged_plan(dtype, D, L, B, Hq, Hkv, n, cap).ws_bytes);
+  p.ws_bytes = std::max(p.own_more + most_own * row, unshared.ws_bytes);
   return p;
 }
 

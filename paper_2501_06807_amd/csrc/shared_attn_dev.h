@@ -315,7 +315,7 @@ __device__ __forceinline__ void shared_rows(const SharedArgs& a, const Plan& pla
       }
     };
     const PageRows rows{same(gp->skip), same(gp->at), 0, 0, same(gp->base)};
-    walk_pages<DT, D, FMT, RT, NW>(w, a, c, f0, l, h, rows, blk * NW + wave, min(blk_end * NW, same(gp->tiles)), lo, hi, load_queries);
+    walk_pages<DT, D, FMT, RT, NW>(w, a, c, f0, l, h, rows, blk * a.shared_block + wave, min(blk_end * a.shared_block, same(gp->tiles)), lo, hi, load_queries);
     float M[RT], Lsum[RT];
     join_waves<DT, D, FMT, RT>(w, wave, s_ml, s_o, M, Lsum);
     if (wave == 0) {
