@@ -142,10 +142,13 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 
 }  // namespace
 
-// Shared rows in units of 128 query rows where a group has more than 32 on average (16-bit types), else of 32, or of 16 over codes
-// where that is enough. Measured, 16K shared rows of 8 kv heads of 128, us: 40 query rows to a kv head in units of 32 and of 128, bf16
-// 38 and 35, 8-bit codes 39 and 33, 4-bit codes 37 and 32 (fp16 38 and 37), 96 rows 54 and 41; 32 rows 32 and 30, 32 and 29, 30 and 29
-// (fp16 31 and 32), but 24 and 30 for 40 rows behind 1K shared ones, and nothing gained by fewer tiles to a block.
+// Shared rows in units of 128 query rows (16-bit types) where a group has more than 32 on average and units of 32 would have 2^18
+// keys or more to read together, else of 32, or of 16 over codes where that is enough. Units of 32 and of 128, us, for 8 kv heads of
+// 128 in bf16 (8-bit codes in fp16; 4-bit codes in bf16): 40 query rows to a kv head behind 1K shared rows 24 and 31 (25 and 29; 23
+// and 27), behind 16K 37 and 37 (39 and 36; 37 and 34); 96 behind 4K 34 and 37 (34 and 36; 32 and 32), behind 16K 54 and 44 (52
+// and 42; 49 and 41); 512 behind 1K 38 and 42 (40 and 41; 38 and 40), behind 8K 84 and 61 (93 and 63; 86 and 61); two groups of 1024
+// behind 1K 78 and 59 (83 and 58; 79 and 55). 32 rows behind 16K: 32 and 31 (31 and 31; 30 and 30). The lengths are on the device:
+// the table's room stands for the shared rows, so a short prompt in a large table is taken in units of 128.
 // 16 rows in units of 16 and of 32: bf16 34 and 30, fp32 50 and 51 (1K shared rows: 38 and 30), 8-bit codes 28 and 30, 4-bit codes
 // 25 and 28. Own rows in units of 16 where a sequence's rows fit, or beside the wide units, else of 32. Blocks are a tile to each
 // wave of a workgroup (wide units: four tiles), and 64 keys of the own rows, which are taken by the waves
@@ -153,7 +156,7 @@ hipError_t launch_join(const SharedArgs& a, int D, hipStream_t st) {
 SharedPlan shared_plan(int dtype, int format, int D, int L, int B, int Hq, int Hkv, int n, int cap, int groups) {
   SharedPlan p{};
   const long long each_seq = (long long)n * (Hq / Hkv), rows = B * each_seq, each = (rows + groups - 1) / groups, lh = (long long)L * Hkv;
-  p.wide = dtype != MPC_FP32 && each > 32;
+  p.wide = dtype != MPC_FP32 && each > 32 && (double)lh * groups * ((each + 31) / 32) * cap >= 1 << 18;
   p.shared_rows = p.wide ? 128 : each <= 16 && format != MPC_PAGE_SAME ? 16 : 32;
   p.own_rows = each_seq <= 16 || p.wide ? 16 : 32;
   p.tile = dtype == MPC_FP32 ? 16 : 32;
