@@ -392,8 +392,9 @@ mpc_status mpc_paged_append(const mpc_dims* dims, const mpc_paged_kv* kv, int32_
 /* Rows of a paged cache of any format, in the element type: row t < n_valid[b] (NULL: n; values are brought into [0, n]) of
  * sequence b is row first[b] + t of the cache (NULL: lens[b] - n_valid[b] + t, the newest ones), for the prompt
  * attention over what the cache keeps, for eviction from it, or to move it. A value is code * scale, rounded once to the
- * element type. Rows from n_valid[b] on, and rows that the cache does not have (outside [0, lens[b]) or
- * [0, M * page_size), or in a page whose table entry lies outside [0, P)), are left as they were.
+ * element type (one beyond fp16's range, which 4-bit codes of its largest values may have, becomes an infinity). Rows from
+ * n_valid[b] on, and rows that the cache does not have (outside [0, lens[b]) or [0, M * page_size), or in a page whose table
+ * entry lies outside [0, P)), are left as they were.
  *   k_out, v_out [L][B][Hkv][n][d] (strides; NULL: contiguous), either of which may be NULL. They may overlap neither
  *   each other nor the cache. No workspace. */
 mpc_status mpc_paged_read(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n, const int32_t* n_valid,
@@ -439,13 +440,15 @@ typedef struct {
 } mpc_shared_sizes;
 
 /* mpc_paged_attn, with the shared rows of a group read once for all its sequences, through the table of the group's first
- * sequence and from its pages (with MPC_PAGE_E4M3 these have to be complete; the others' tables are not read for
- * them). What a row sees, its weights, empty rows, NaN and lse are as there; so are the outputs, up to the
- * roundings of another order of summation.
+ * sequence and from its pages (with MPC_PAGE_E4M3 these have to be complete; the others' tables are not read for them, nor
+ * is the tail of a sequence that ends among them). What a row sees, its weights, empty rows, NaN and lse are as there; so
+ * are the outputs, up to the roundings of another order of summation.
  * ws: mpc_workspace_bytes(MPC_OP_SHARED_ATTN, dims, n_new, &sizes) bytes, zero-filled before its first use; every completed
  * call leaves it ready for the next, of this or any other sizes whose bytes it has, and for mpc_paged_attn (calls sharing
- * it must not overlap). The bytes never fall with n_new, batch, n_layers, the heads or n_groups. The sizes, not the lengths or the groups' contents, give the launches, so a captured call follows
- * lengths, tables and groups as they change.
+ * it must not overlap). It holds fp32 parts of every query row: about 8 (d + 4) L * B * Hq * n_new bytes, and up to 26 (d 64) or
+ * 50 MiB beside them (32 layers, 8 sequences, 32 heads of 128: 58 MiB for a token, 2.1 GiB for 256). Layers may come in calls of
+ * their own, with one workspace. The bytes never fall with n_new, batch, n_layers, the heads or n_groups. The sizes, not the lengths
+ * or the groups' contents, give the launches, so a captured call follows lengths, tables and groups as they change.
  * Limits: those of mpc_paged_attn, B * n_new * G <= 2^30, L * B * Hq * n_new < 2^31, L * Hkv * n_groups < 2^29. */
 mpc_status mpc_shared_attn(const mpc_dims* dims, const mpc_paged_kv* kv, int32_t n_new, const int32_t* n_valid,
                            const mpc_shared* shared, const mpc_attn_cfg* cfg, const void* q, const mpc_strides* q_strides,

@@ -358,7 +358,9 @@ class PagedPath:
         """Groups of neighbours, sequences first[g] <= b < first[g + 1]: each of them goes on from the rows of its group's first one,
         whose whole pages they share from then on (the rows behind these are copied); the others of a group have to be empty. A
         sequence alone in its group shares nothing, as one outside all groups. Steps of up to n_new tokens read the shared rows once
-        for a group (mpc_shared_attn), longer ones once for each sequence."""
+        for a group (mpc_shared_attn), longer ones once for each sequence. The workspace grows with n_new, by about
+        8 (head_dim + 4) bytes for each token, query head, layer and sequence; one that a fork of fewer tokens made stays, since
+        captured steps may use it."""
         kv, page = self.kv, self.kv.page
         first, n_new = [operator.index(b) for b in first], operator.index(n_new)
         if not 2 <= len(first) <= 1025 or first[0] < 0 or first[-1] > kv.B or any(x >= y for x, y in zip(first, first[1:])) or n_new < 1:
