@@ -4,8 +4,9 @@
 // V of the shared rows are read once for a unit instead of once for a sequence; a softmax over both kinds of rows is the join of
 // its parts over each, o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p with m = max_p m_p. The tiles' work is the paged
 // attention's. Reading the keys bounds it: 64 sequences in four groups behind 8K rows of 8-bit pages, 32 heads of 128, 108 us,
-// 350 MB (54 us at the rate of a large read): 66 for the shared rows, of which one group of 17 takes two units of 16 rows and
-// reads its own twice (units of 32: 74), 28 for the own ones (100 MB), 8 for the join.
+// 350 MB (54 us at the rate of a large read): 66 for the shared rows, of which the two groups of 17 take two units of 16 rows and
+// ask for theirs twice (units of 32: 74), 28 for the own ones (100 MB), 8 for the join. More than 64 sequences wait for
+// the plan's launch: 64 behind 4K rows of bf16 pages, 8 kv heads, 42 us, 65 of them 54.
 //
 // Own rows are short and their units many, so a wave takes a run of them by itself: no LDS, no wait for another wave. Eight waves to
 // a unit, joined in LDS and through memory as in the paged attention, took 103 us of what is 32 for the own rows above (with

@@ -5,25 +5,26 @@
 // values on the way. S^T = K Q^T and O^T += V^T P^T are 32x32x16 products, as in the prompt attention: a lane has 16 scores of
 // one row for each 32 keys, and its weights, packed, are the next product's operand; V comes from LDS through the transposing
 // reads. Two workgroups to a compute unit, which wait for each other nowhere: one of eight waves, in two groups that divide the
-// keys and join in LDS, took 114 us of the last case's 109 below in turn on one card, and as long in the other two.
+// keys and join in LDS, took 114 us against 109 in the last case below in turn on one card, and as long in the other two.
 // A row's reference moves only when a score passes it by 2^8. A weight is multiplied in two parts of the type, as in the paged
 // attention (over codes in bf16 ones for both types, since values times page or block scales have no place in fp16's range).
-// The second part's products cost 611 us against 763, 110 against 129 and 62 against 67 in the cases below; without them outputs
-// are off by 0.0020 of their size instead of 0.0017 in bf16 and by 0.00027 instead of 0.00021 in fp16.
+// In turn on one card, weights rounded once and in two parts: 611 and 763 us, 62 and 67, 110 and 129 in the cases below; rounded
+// once, outputs are off by 0.0020 of their size instead of 0.0017 in bf16 and by 0.00027 instead of 0.00021 in fp16. Figures
+// of what else was tried are of the kernel with weights rounded once.
 //
-// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 603 to
-// 622 us on different cards, up to 753 TFLOP/s (a large product of the library: 1078). The matrix unit is busy a third of the cycles, the vector unit
-// another; 94% of the reads hit the L2. On the way there: masks and values that are not finite in a loop of their own (spills:
-// 1341 to 871 us), page ids and offsets in registers of a window of 64 halves instead
+// Eight prompts of up to 256 tokens behind 16K rows of fp16 pages (8 kv heads of 128, 6736 query rows to each), 454 GFLOP: 746 to
+// 775 us on different cards, up to 608 TFLOP/s, 912 with the second parts' products (a large product of the library: 1078). The matrix unit
+// is busy 43% of the cycles, the vector unit as much; 94% of the reads hit the L2. On the way there: masks and values that are not
+// finite in a loop of their own (spills: 1341 to 871 us), page ids and offsets in registers of a window of 64 halves instead
 // of scalar loads and 64-bit products (871 to 729, 646 to 614), rows of shorter prompts not padded (726 to 678), runs from
 // their end on (677 to 646; before it 93% of the reads missed the L2). Not kept: units of 256 rows (691 of 678), tiles
 // straight to LDS in rounds of two (765), priority to the matrix operations (616 of 614), all in workgroups of eight waves; the
 // next tile's scores beside this one's weights (681 of 664 under the profiler). Tiles straight to LDS instead of through
 // registers: no time here, 52 to 50 us of the next case's first launch.
-// 32 sequences behind 32K rows of bf16 pages, 128 query rows to each of 8 kv heads: 68 us, 182 MB (28 us at the rate of a large
-// read), 50 of them for the shared and the own rows, 10 for the join of 66 parts to a row, and what lies between.
-// 192 query rows to each of 8 heads behind 20K rows of 4-bit pages (63 GFLOP): 111 us, most of it for the shared rows, whose
-// codes are widened once for 128 query rows.
+// 32 sequences behind 32K rows of bf16 pages, 128 query rows to each of 8 kv heads: 65 to 71 us, 182 MB (28 us at the rate of a
+// large read), 10 of them for the join of 66 parts to a row, the rest for the shared rows, the own ones and what lies between.
+// 48 sequences of four drafts behind 20K rows of 4-bit pages, 768 query rows to each of 8 kv heads (63 GFLOP): 128 to 130 us, most of
+// it for the shared rows, whose codes are widened once for 128 query rows.
 #pragma once
 #include "shared_attn_dev.h"
 
